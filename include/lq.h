@@ -302,6 +302,134 @@ lq_status lq_ref_decode_step_bf16(const lq_shape *shape, uint16_t *S, const uint
                                   lq_stream stream);
 
 /*
+ * ---- What surrounds the decode step in a layer ----------------------------------------------------------------
+ *
+ * The projections of a layer with a recurrent state go through a short causal convolution, q and k are normalised
+ * per head (and rotated, where the layer's instance rotates), and a prompt's tokens are scanned before the first
+ * token is decoded:
+ *     prompt:  lq_conv_prompt -> lq_norm_rotate -> lq_scan_prompt -> lq_quantize_state
+ *     token:   lq_conv_step   -> lq_norm_rotate -> lq_decode_step (or, on the dense state, lq_scan_step)
+ *
+ * Conventions of these entry points, next to those at the top of this file:
+ *  - Tokens are ROWS.  The rows of the sequences of a call lie back to back: sequence n has rows seq_start[n] to
+ *    seq_start[n+1] - 1 (int32 [seqs + 1] in device memory, not decreasing; rows in front of seq_start[0] and from
+ *    seq_start[seqs] on belong to nobody: nothing of them is read or written).  The single-token forms have one row
+ *    per sequence, row n.
+ *  - A row's channels are contiguous, `..._stride` is the distance between rows in elements, at least a row long:
+ *    slices of a wider projection are taken as they are.  Such arrays need the alignment of their element type only,
+ *    except for q, k, v of the scan: 16 bytes, and strides that are multiples of 8.  All other arrays are dense.
+ *  - States are kept in SLOTS: sequence n has slot slots[n] (int32 [seqs] in device memory; null: slot n).  Where slots[n] is
+ *    negative or not below n_slots, the sequence is padding: none of its rows is written and no state is touched.  No two
+ *    sequences of a call may share a slot.
+ *  - resume (int32 [seqs] in device memory; null: zero): where it is zero the prompt starts from an empty state (what the
+ *    slot holds is not read), elsewhere it goes on from what its slot holds.
+ *  - Sums are taken in binary32 (of a position's rotation: in binary64), in an order that depends on the shapes alone:
+ *    the same call gives the same bits again.
+ */
+typedef enum { LQ_BF16 = 0, LQ_F16 = 1, LQ_F32 = 2 } lq_type;
+
+/*
+ * Short causal depthwise convolution with an optional bias and SiLU:
+ *     out[t][c] = f( bias[c] + sum_{i < width} w[c][i] x[t - (width-1) + i][c] ),    f(y) = y or y / (1 + exp(-y))
+ * in binary32, rounded once to `type`.  Rows in front of the sequence's first are the state's (resumed) or zero.
+ *   x, out : [tokens][channels], strided rows     w : [channels][width]     bias : [channels] or null
+ *   state  : [n_slots][width-1][channels], the last width-1 rows of x, oldest first, in and out (lq_conv_prompt: null
+ *            if the prompts are fresh and no state is wanted)                                          - all of `type`
+ * The slot of a sequence without rows is left as it is.
+ * lq_conv_step's out may be its x (same pointer and stride).  Otherwise out must not overlap x: LQ_ERR_UNSUPPORTED where
+ * the two ranges show that it does.
+ */
+typedef struct {
+  int tokens;   /* rows (lq_conv_step: equal to seqs)  */
+  int seqs;
+  int channels;
+  int width;    /* taps: 2, 3 or 4                      */
+  int n_slots;
+  int silu;     /* 1: f is SiLU; 0: f is the identity   */
+  int type;     /* lq_type of all arrays                */
+} lq_conv;
+lq_status lq_conv_prompt(const lq_conv *shape, const void *x, int64_t x_stride, const void *w, const void *bias, void *state,
+                         void *out, int64_t out_stride, const int32_t *seq_start, const int32_t *slots,
+                         const int32_t *resume, lq_stream stream);
+lq_status lq_conv_step(const lq_conv *shape, const void *x, int64_t x_stride, const void *w, const void *bias, void *state,
+                       void *out, int64_t out_stride, const int32_t *slots, lq_stream stream);
+
+/*
+ * Queries and keys of every row normalised per head and rotated by the row's position, in one pass:
+ *     y = x                                           (LQ_NORM_NONE)
+ *     y = x / sqrt(sum_i x_i^2 + eps)                 (LQ_NORM_L2)
+ *     y = x / sqrt(sum_i x_i^2 / dim + eps) * w       (LQ_NORM_RMS; w null: 1)
+ *     y = scale * y
+ *     (y_a, y_b) <- (y_a cos - y_b sin, y_b cos + y_a sin),  angle = position * inv_freq[i],  i < rot/2,
+ * with (a, b) = (i, i + rot/2), or (2i, 2i + 1) with `pairs`; channels from `rot` on are not rotated.  Rounded once to `type`.
+ *   q, out_q : [tokens][heads_q][dim]   k, out_k : [tokens][heads_k][dim], strided rows (heads of a row back to back)
+ *   w_q, w_k : fp32 [dim] or null       positions : int32 [tokens]      inv_freq : fp32 [rot/2] (positions, inv_freq: null if
+ *                                                                        rot = 0)
+ * A row with a negative position is padding: it is not written.  An output may be its own input (same pointer and stride);
+ * no other overlap is allowed.  The angle is taken in binary64, so far positions lose nothing.
+ * heads_q or heads_k may be zero (its pointers are not looked at then).
+ */
+enum { LQ_NORM_NONE = 0, LQ_NORM_L2 = 1, LQ_NORM_RMS = 2 };
+typedef struct {
+  int tokens;
+  int heads_q, heads_k;
+  int dim;      /* channels of a head: 64, 128 or 256                    */
+  int rot;      /* channels that are rotated: 0 .. dim, a multiple of 16 */
+  int pairs;    /* 1: neighbouring channels are a pair; 0: i and i + rot/2 */
+  int norm;
+  int type;     /* lq_type of q, k and the outputs                       */
+  float eps;
+  float scale_q, scale_k;
+} lq_norm;
+lq_status lq_norm_rotate(const lq_norm *shape, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                         void *out_q, int64_t out_q_stride, void *out_k, int64_t out_k_stride, const float *w_q,
+                         const float *w_k, const int32_t *positions, const float *inv_freq, lq_stream stream);
+
+/*
+ * Selective state space scan with a scalar decay per head (the instances with b = 0 of lq_shape.delta: Mamba2, RetNet, linear
+ * attention), on dense states:
+ *     S_t = alpha_t S_{t-1} + beta_t k_t v_t^T,      o_t = S_t^T q_t + skip v_t
+ * Value head h reads q/k head h/(Hv/Hqk), as in lq_decode_step.  With `select`, beta holds the raw step dt and
+ *     dt' = log(1 + exp(dt + dt_bias_h)),   beta_t = dt',   alpha_t = exp(dt' A_h)      (alpha is not looked at).
+ *   q, k : bf16 [tokens][Hqk][d_k]    v : bf16 [tokens][Hv][d_v]      strided rows, 16-byte aligned, strides multiples of 8
+ *   beta, alpha : [tokens][Hv] of gate_type, strided rows; alpha in [0, 1]
+ *   A, dt_bias, skip : fp32 [Hv]; dt_bias and skip may be null (0); A is needed with `select` only, and is not positive
+ *   S : fp32 [n_slots][Hv][d_k][d_v], in and out - what lq_quantize_state takes
+ * lq_scan_prompt: o is bf16.  The outputs are rounded to bf16 once; in front of that the state and the weighted scores of a
+ * block of tokens are rounded to bf16 where they enter a product, as the inputs are; S is held and updated in binary32.
+ * A NaN or an infinity in a row makes o undefined from the first row of its block (128 rows from the sequence's first on) to
+ * the end of its sequence, and S of that sequence; other sequences never see it.
+ * lq_scan_step: one row per sequence (tokens = seqs), every slot is resumed, o is fp32 [seqs][Hv][d_v] in strided rows.
+ * A sequence without rows leaves its slot as it is if it is resumed, and empties it (zeros) if it is not.
+ * Neither may have S, o and the inputs overlap.
+ *
+ * `work`: lq_scan_prompt_bytes(shape) bytes of device memory, 16-byte aligned, for the states between the pieces that long prompts are
+ * cut into (null if that is 0).  Its contents mean nothing between calls; calls that may run at the same time need one each.
+ */
+typedef struct {
+  int tokens;    /* rows (lq_scan_step: equal to seqs)                                                      */
+  int seqs;
+  int max_len;   /* lq_scan_prompt: at least the length of the longest sequence; rows of a sequence beyond it are left out */
+  int heads_v, heads_qk;
+  int d_k, d_v;  /* 128, 128                                                                                */
+  int n_slots;
+  int select;
+  int gate_type; /* lq_type of beta and alpha: LQ_BF16 or LQ_F32                                            */
+} lq_scan;
+typedef struct {
+  const uint16_t *q, *k, *v;
+  int64_t q_stride, k_stride, v_stride;
+  const void *beta, *alpha;
+  int64_t beta_stride, alpha_stride;
+  const float *A, *dt_bias, *skip;
+  float *S;
+  const int32_t *seq_start, *slots, *resume;   /* lq_scan_step: seq_start and resume are not looked at */
+} lq_scan_io;
+uint64_t lq_scan_prompt_bytes(const lq_scan *shape);
+lq_status lq_scan_prompt(const lq_scan *shape, const lq_scan_io *io, uint16_t *o, int64_t o_stride, void *work, lq_stream stream);
+lq_status lq_scan_step(const lq_scan *shape, const lq_scan_io *io, float *o, int64_t o_stride, lq_stream stream);
+
+/*
  * Device-side error flags of the current device (0 = none), written to *flags (a host pointer).  Waits inside
  * the kernels are bounded; bit 0 is set when a warp gave up waiting for its asynchronous copies.  After
  * that, neither the outputs of that launch NOR THE STATE it worked on are valid (records may be missing or

@@ -6,6 +6,7 @@ kernels write fmaf(), which is what makes results reproducible bit for bit.
 from __future__ import annotations
 
 import os
+import re
 import subprocess
 import sys
 
@@ -14,32 +15,54 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblq.so")
 # the same library with per-CTA time stamps compiled in (a development aid: bench.py --timeline reads them)
 LIB_STAMPS = os.path.join(HERE, "liblq_stamps.so")
-SOURCES = ["lq_api.cu"]
+SOURCES = ["lq_api.cu", "lq_ops.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-fmad=false", "-std=c++17",
-              "--shared", "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
+              "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
 
 
-def _newest_source() -> float:
-    inc = os.path.join(os.path.dirname(HERE), "include")
-    paths = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(inc, f) for f in os.listdir(inc)]
-    return max(os.path.getmtime(p) for p in paths)
+def _headers(source: str, seen=None) -> set:
+    """A source file and every file of this repository that it includes."""
+    seen = set() if seen is None else seen
+    if source not in seen:
+        seen.add(source)
+        with open(source) as f:
+            for name in re.findall(r'^#include "([^"]+)"', f.read(), re.M):
+                _headers(os.path.normpath(os.path.join(os.path.dirname(source), name)), seen)
+    return seen
+
+
+def _newest_source(source: str) -> float:
+    return max(os.path.getmtime(p) for p in _headers(source))
 
 
 def build(force: bool = False, verbose: bool = False, stamps: bool = False) -> str:
     """Compile if the library is missing or older than its sources; returns the library path.
     ``stamps``: the variant with the time stamps (-DLQ_TIMING -DLQ_STAMPS_ONLY) instead of the product."""
     LIB = LIB_STAMPS if stamps else globals()["LIB"]
-    if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= _newest_source():
+    sources = [os.path.join(CSRC, f) for f in SOURCES]
+    if not force and os.path.exists(LIB) and all(os.path.getmtime(LIB) >= _newest_source(s) for s in sources):
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     extra = ["-DLQ_TIMING", "-DLQ_STAMPS_ONLY"] if stamps else []
-    cmd = [nvcc, *NVCC_FLAGS, *extra, *[os.path.join(CSRC, s) for s in SOURCES], "-o", LIB + ".tmp"]
-    res = subprocess.run(cmd, capture_output=True, text=True)
+    objects, running = [], []
+    for s in sources:                        # (an object that is newer than its sources is kept)
+        o = s[:-3] + (".stamps.o" if stamps else ".o")
+        objects.append(o)
+        if force or not os.path.exists(o) or os.path.getmtime(o) < _newest_source(s):
+            running.append((o, subprocess.Popen([nvcc, *NVCC_FLAGS, *extra, "-c", s, "-o", o + ".tmp"], stdout=subprocess.PIPE,
+                                                stderr=subprocess.STDOUT, text=True)))
+    said = [(o, p.communicate()[0], p.returncode) for o, p in running]
+    for o, text, rc in said:
+        if rc != 0:
+            sys.stderr.write(text)
+            raise RuntimeError("nvcc failed")
+        if verbose:
+            sys.stderr.write(text)
+        os.replace(o + ".tmp", o)
+    res = subprocess.run([nvcc, *NVCC_FLAGS[:2], "--shared", *objects, "-o", LIB + ".tmp"], capture_output=True, text=True)
     if res.returncode != 0:
         sys.stderr.write(res.stdout + res.stderr)
         raise RuntimeError("nvcc failed")
-    if verbose:
-        sys.stderr.write(res.stderr)
     os.replace(LIB + ".tmp", LIB)
     return LIB
 

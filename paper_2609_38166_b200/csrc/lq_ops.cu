@@ -1,0 +1,240 @@
+// C boundary of the operators around the decode step: argument checks and launches.  Declarations and contracts: include/lq.h.
+#include <initializer_list>
+
+#include "lq_conv.cuh"
+#include "lq_norm.cuh"
+#include "lq_scan.cuh"
+
+namespace lq {
+
+static cudaStream_t cuda_stream(lq_stream s) { return reinterpret_cast<cudaStream_t>(s); }
+
+static bool aligned(const void *p, unsigned bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+static lq_status launched() { return cudaGetLastError() == cudaSuccess ? LQ_OK : LQ_ERR_CUDA; }
+
+static unsigned type_size(int type) { return type == LQ_F32 ? 4 : 2; }
+
+static long ceil_div(long a, long b) { return (a + b - 1) / b; }
+
+static bool bad_count(int n) { return n < 0; }
+
+// Required and optional (may be null) arrays with elements of `bytes` bytes.
+static lq_status check_arrays(unsigned bytes, std::initializer_list<const void *> required, std::initializer_list<const void *> optional = {}) {
+  for (const void *p : required) {
+    if (!p) return LQ_ERR_NULL;
+    if (!aligned(p, bytes)) return LQ_ERR_ALIGN;
+  }
+  for (const void *p : optional)
+    if (!aligned(p, bytes)) return LQ_ERR_ALIGN;
+  return LQ_OK;
+}
+
+// Whether two arrays of strided rows have an element in common.  Exact where the strides are equal (slices of one buffer), else
+// by the ranges they span.
+static bool rows_overlap(const void *a, int64_t sa, long wa, const void *b, int64_t sb, long wb, long rows, unsigned bytes) {
+  if (rows <= 0) return false;
+  const intptr_t x = reinterpret_cast<intptr_t>(a), y = reinterpret_cast<intptr_t>(b);
+  const intptr_t ex = x + ((rows - 1) * sa + wa) * (intptr_t)bytes, ey = y + ((rows - 1) * sb + wb) * (intptr_t)bytes;
+  if (ex <= y || ey <= x) return false;
+  if (sa != sb) return true;
+  const intptr_t period = sa * (intptr_t)bytes, d = ((y - x) % period + period) % period;   // b's rows start d bytes into a's
+  return d < wa * (intptr_t)bytes || d + wb * (intptr_t)bytes > period;
+}
+
+// ---- short causal convolution ----
+
+static lq_status check_conv(const lq_conv *s, bool step) {
+  if (!s) return LQ_ERR_NULL;
+  if (bad_count(s->tokens) || bad_count(s->seqs) || s->channels <= 0 || s->width <= 0 || bad_count(s->n_slots)) return LQ_ERR_SHAPE;
+  if (s->type < LQ_BF16 || s->type > LQ_F32 || (s->silu != 0 && s->silu != 1)) return LQ_ERR_SHAPE;
+  if (step && s->tokens != s->seqs) return LQ_ERR_SHAPE;
+  if (s->width < 2 || s->width > 4) return LQ_ERR_UNSUPPORTED;
+  return LQ_OK;
+}
+
+template <typename T, int W, int VEC>
+static lq_status launch_conv_t(const lq_conv *s, ConvArgs a, bool step, cudaStream_t stream) {
+  const long blocks_c = ceil_div(s->channels, CONV_THREADS * VEC);
+  if (blocks_c > 65535) return LQ_ERR_UNSUPPORTED;
+  if (step) {
+    conv_step_kernel<T, W, VEC><<<dim3(s->seqs, blocks_c), CONV_THREADS, 0, stream>>>(a);
+  } else {
+    a.rows_per_tile = 32;
+    conv_prompt_kernel<T, W, VEC><<<dim3(ceil_div(s->tokens, a.rows_per_tile), blocks_c), CONV_THREADS, 0, stream>>>(a);
+  }
+  return launched();
+}
+
+template <typename T>
+static lq_status launch_conv(const lq_conv *s, const ConvArgs &a, bool step, cudaStream_t stream) {
+  constexpr int VEC = 16 / sizeof(T);
+  bool wide = s->channels % VEC == 0 && a.x_stride % VEC == 0 && a.out_stride % VEC == 0;
+  for (const void *p : {a.x, a.w, (const void *)a.state, (const void *)a.out}) wide = wide && aligned(p, 16);
+#define LQ_CONV(W) return wide ? launch_conv_t<T, W, VEC>(s, a, step, stream) : launch_conv_t<T, W, 1>(s, a, step, stream)
+  if (s->width == 2) LQ_CONV(2);
+  if (s->width == 3) LQ_CONV(3);
+  LQ_CONV(4);
+#undef LQ_CONV
+}
+
+static lq_status conv(const lq_conv *s, const void *x, int64_t x_stride, const void *w, const void *bias, void *state, void *out,
+                      int64_t out_stride, const int32_t *seq_start, const int32_t *slots, const int32_t *resume, bool step,
+                      lq_stream stream) {
+  lq_status rc = check_conv(s, step);
+  if (rc != LQ_OK) return rc;
+  if (s->tokens == 0 || s->seqs == 0) return LQ_OK;
+  const unsigned bytes = type_size(s->type);
+  if ((rc = check_arrays(bytes, {x, w, out}, {bias, state})) != LQ_OK) return rc;
+  if ((rc = check_arrays(4, {}, {seq_start, slots, resume})) != LQ_OK) return rc;
+  if (step ? !state : !seq_start) return LQ_ERR_NULL;
+  if (!step && resume && !state) return LQ_ERR_NULL;
+  if (x_stride < s->channels || out_stride < s->channels) return LQ_ERR_SHAPE;
+  if (!(step && x == out && x_stride == out_stride) &&
+      rows_overlap(x, x_stride, s->channels, out, out_stride, s->channels, s->tokens, bytes))
+    return LQ_ERR_UNSUPPORTED;
+  ConvArgs a{x, w, bias, state, out, x_stride, out_stride, {seq_start, slots, resume, s->tokens, s->seqs, state ? s->n_slots : INT32_MAX},
+             s->channels, s->silu, 0};
+  if (s->type == LQ_F32) return launch_conv<float>(s, a, step, cuda_stream(stream));
+  if (s->type == LQ_F16) return launch_conv<__half>(s, a, step, cuda_stream(stream));
+  return launch_conv<__nv_bfloat16>(s, a, step, cuda_stream(stream));
+}
+
+// ---- norms of queries and keys with the rotation ----
+
+template <typename T, int DIM>
+static lq_status launch_norm_t(const lq_norm *s, NormArgs a, bool wide, cudaStream_t stream) {
+  a.rows_per_cta = 1;
+  const long grid = ceil_div(s->tokens, a.rows_per_cta);
+  if (wide) norm_rotate_kernel<T, DIM, true><<<grid, NORM_THREADS, 0, stream>>>(a);
+  else norm_rotate_kernel<T, DIM, false><<<grid, NORM_THREADS, 0, stream>>>(a);
+  return launched();
+}
+
+template <typename T>
+static lq_status launch_norm(const lq_norm *s, const NormArgs &a, cudaStream_t stream) {
+  constexpr int VEC = 16 / sizeof(T);
+  bool wide = true;
+  for (const void *p : {a.q, a.k, (const void *)a.out_q, (const void *)a.out_k}) wide = wide && aligned(p, 16);
+  for (int64_t stride : {a.q_stride, a.k_stride, a.out_q_stride, a.out_k_stride}) wide = wide && stride % VEC == 0;
+  if (s->dim == 64) return launch_norm_t<T, 64>(s, a, wide, stream);
+  if (s->dim == 128) return launch_norm_t<T, 128>(s, a, wide, stream);
+  return launch_norm_t<T, 256>(s, a, wide, stream);
+}
+
+// ---- selective scan ----
+
+static lq_status check_scan(const lq_scan *s, bool step) {
+  if (!s) return LQ_ERR_NULL;
+  if (bad_count(s->tokens) || bad_count(s->seqs) || bad_count(s->n_slots) || s->heads_v <= 0 || s->heads_qk <= 0 || s->d_k <= 0 || s->d_v <= 0)
+    return LQ_ERR_SHAPE;
+  if (s->heads_v % s->heads_qk != 0 || (s->select != 0 && s->select != 1)) return LQ_ERR_SHAPE;
+  if (step ? s->tokens != s->seqs : s->max_len < 0) return LQ_ERR_SHAPE;
+  if (s->gate_type != LQ_BF16 && s->gate_type != LQ_F32) return LQ_ERR_UNSUPPORTED;
+  if (s->d_k != SD || s->d_v != SD || (long)s->seqs * s->heads_v > INT32_MAX) return LQ_ERR_UNSUPPORTED;
+  return LQ_OK;
+}
+
+static lq_status check_scan_io(const lq_scan *s, const lq_scan_io *io, const void *o, int64_t o_stride, bool step) {
+  lq_status rc;
+  if (!io) return LQ_ERR_NULL;
+  if ((rc = check_arrays(16, {io->S})) != LQ_OK) return rc;
+  if (!step && !io->seq_start) return LQ_ERR_NULL;
+  if ((rc = check_arrays(4, {}, {io->A, io->dt_bias, io->skip, io->seq_start, io->slots, io->resume})) != LQ_OK) return rc;
+  if (s->tokens == 0) return LQ_OK;
+  if ((rc = check_arrays(16, {io->q, io->k, io->v})) != LQ_OK) return rc;
+  if ((rc = check_arrays(step ? 4 : 2, {o})) != LQ_OK) return rc;
+  if ((rc = check_arrays(type_size(s->gate_type), {io->beta}, {io->alpha})) != LQ_OK) return rc;
+  if (s->select ? !io->A : !io->alpha) return LQ_ERR_NULL;
+  const int64_t wq = (int64_t)s->heads_qk * SD, wv = (int64_t)s->heads_v * SD;
+  if (io->q_stride < wq || io->k_stride < wq || io->v_stride < wv || o_stride < wv) return LQ_ERR_SHAPE;
+  if (io->beta_stride < s->heads_v || (!s->select && io->alpha_stride < s->heads_v)) return LQ_ERR_SHAPE;
+  if (io->q_stride % 8 || io->k_stride % 8 || io->v_stride % 8) return LQ_ERR_ALIGN;
+  return LQ_OK;
+}
+
+static ScanArgs scan_args(const lq_scan *s, const lq_scan_io *io, void *o, int64_t o_stride) {
+  auto bf = [](const uint16_t *p) { return reinterpret_cast<const __nv_bfloat16 *>(p); };
+  return {bf(io->q), bf(io->k), bf(io->v), io->q_stride, io->k_stride, io->v_stride, io->beta_stride, io->alpha_stride, o_stride, io->beta, io->alpha,
+          io->A, io->dt_bias, io->skip, io->S, o, {io->seq_start, io->slots, io->resume, s->tokens, s->seqs, s->n_slots}, s->heads_v,
+          s->heads_qk, s->max_len, s->select, s->gate_type == LQ_F32};
+}
+
+}  // namespace lq
+
+using namespace lq;
+
+extern "C" {
+
+lq_status lq_conv_prompt(const lq_conv *shape, const void *x, int64_t x_stride, const void *w, const void *bias, void *state,
+                         void *out, int64_t out_stride, const int32_t *seq_start, const int32_t *slots,
+                         const int32_t *resume, lq_stream stream) {
+  return conv(shape, x, x_stride, w, bias, state, out, out_stride, seq_start, slots, resume, false, stream);
+}
+
+lq_status lq_conv_step(const lq_conv *shape, const void *x, int64_t x_stride, const void *w, const void *bias, void *state,
+                       void *out, int64_t out_stride, const int32_t *slots, lq_stream stream) {
+  return conv(shape, x, x_stride, w, bias, state, out, out_stride, nullptr, slots, nullptr, true, stream);
+}
+
+lq_status lq_norm_rotate(const lq_norm *s, const void *q, int64_t q_stride, const void *k, int64_t k_stride, void *out_q,
+                         int64_t out_q_stride, void *out_k, int64_t out_k_stride, const float *w_q, const float *w_k,
+                         const int32_t *positions, const float *inv_freq, lq_stream stream) {
+  if (!s) return LQ_ERR_NULL;
+  if (bad_count(s->tokens) || bad_count(s->heads_q) || bad_count(s->heads_k) || s->dim <= 0 || s->rot < 0 || s->rot > s->dim) return LQ_ERR_SHAPE;
+  if (s->norm < LQ_NORM_NONE || s->norm > LQ_NORM_RMS || (s->pairs != 0 && s->pairs != 1) || s->type < LQ_BF16 || s->type > LQ_F32) return LQ_ERR_SHAPE;
+  if ((s->dim != 64 && s->dim != 128 && s->dim != 256) || s->rot % 16 != 0) return LQ_ERR_UNSUPPORTED;
+  if ((long)s->heads_q + s->heads_k > (1 << 16)) return LQ_ERR_UNSUPPORTED;
+  if (s->tokens == 0 || s->heads_q + s->heads_k == 0) return LQ_OK;
+  const unsigned bytes = type_size(s->type);
+  lq_status rc;
+  struct { const void *in; int64_t in_stride; void *out; int64_t out_stride; int heads; } side[2] = {
+      {q, q_stride, out_q, out_q_stride, s->heads_q}, {k, k_stride, out_k, out_k_stride, s->heads_k}};
+  for (auto &x : side) {
+    if (x.heads == 0) {
+      x = {nullptr, 0, nullptr, 0, 0};
+      continue;
+    }
+    if ((rc = check_arrays(bytes, {x.in, x.out})) != LQ_OK) return rc;
+    if (x.in_stride < (int64_t)x.heads * s->dim || x.out_stride < (int64_t)x.heads * s->dim) return LQ_ERR_SHAPE;
+  }
+  if ((rc = check_arrays(4, {}, {w_q, w_k, positions, inv_freq})) != LQ_OK) return rc;
+  if (s->rot > 0 && (!positions || !inv_freq)) return LQ_ERR_NULL;
+  for (auto &out : side)                       // an output may be its own input, and nothing else
+    for (auto &in : side) {
+      if (!in.heads || !out.heads || (&in == &out && in.in == in.out && in.in_stride == in.out_stride)) continue;
+      if (rows_overlap(in.in, in.in_stride, (long)in.heads * s->dim, out.out, out.out_stride, (long)out.heads * s->dim, s->tokens, bytes))
+        return LQ_ERR_UNSUPPORTED;
+    }
+  if (s->heads_q && s->heads_k &&
+      rows_overlap(out_q, out_q_stride, (long)s->heads_q * s->dim, out_k, out_k_stride, (long)s->heads_k * s->dim, s->tokens, bytes))
+    return LQ_ERR_UNSUPPORTED;
+  const NormArgs a{side[0].in, side[1].in, side[0].out, side[1].out, side[0].in_stride, side[1].in_stride, side[0].out_stride, side[1].out_stride,
+                   w_q, w_k, inv_freq, positions, s->tokens, s->heads_q, s->heads_k, s->rot, s->pairs, s->norm, 0, s->eps, s->scale_q, s->scale_k};
+  if (s->type == LQ_F32) return launch_norm<float>(s, a, cuda_stream(stream));
+  if (s->type == LQ_F16) return launch_norm<__half>(s, a, cuda_stream(stream));
+  return launch_norm<__nv_bfloat16>(s, a, cuda_stream(stream));
+}
+
+uint64_t lq_scan_prompt_bytes(const lq_scan *) { return 0; }
+
+lq_status lq_scan_prompt(const lq_scan *s, const lq_scan_io *io, uint16_t *o, int64_t o_stride, void *work, lq_stream stream) {
+  lq_status rc = check_scan(s, false);
+  if (rc != LQ_OK) return rc;
+  if (s->seqs == 0) return LQ_OK;
+  if ((rc = check_scan_io(s, io, o, o_stride, false)) != LQ_OK) return rc;
+  (void)work;
+  scan_tokens_kernel<<<s->seqs * s->heads_v, 256, 0, cuda_stream(stream)>>>(scan_args(s, io, o, o_stride));
+  return launched();
+}
+
+lq_status lq_scan_step(const lq_scan *s, const lq_scan_io *io, float *o, int64_t o_stride, lq_stream stream) {
+  lq_status rc = check_scan(s, true);
+  if (rc != LQ_OK) return rc;
+  if (s->seqs == 0) return LQ_OK;
+  if ((rc = check_scan_io(s, io, o, o_stride, true)) != LQ_OK) return rc;
+  scan_step_kernel<<<s->seqs * s->heads_v, 256, 0, cuda_stream(stream)>>>(scan_args(s, io, o, o_stride));
+  return launched();
+}
+
+}  // extern "C"

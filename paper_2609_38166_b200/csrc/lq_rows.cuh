@@ -1,0 +1,70 @@
+// What the operators on packed rows share: element types, wide loads and stores, the sequences of a packed batch.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/lq.h"
+
+namespace lq {
+
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <typename T> __device__ __forceinline__ T from_float(float x);
+template <> __device__ __forceinline__ float from_float<float>(float x) { return x; }
+template <> __device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+
+// N consecutive elements at `src`; with WIDE in 16-byte pieces (N * sizeof(T) a multiple of 16, src 16-byte aligned).
+template <bool WIDE, typename T, int N>
+__device__ __forceinline__ void load_row(const T *src, T (&x)[N]) {
+  if constexpr (WIDE) {
+    static_assert(N * sizeof(T) % 16 == 0, "");
+    uint4 *d = reinterpret_cast<uint4 *>(x);
+#pragma unroll
+    for (int i = 0; i < (int)(N * sizeof(T) / 16); i++) d[i] = reinterpret_cast<const uint4 *>(src)[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i++) x[i] = src[i];
+  }
+}
+template <bool WIDE, typename T, int N>
+__device__ __forceinline__ void store_row(T *dst, const T (&x)[N]) {
+  if constexpr (WIDE) {
+    const uint4 *s = reinterpret_cast<const uint4 *>(x);
+#pragma unroll
+    for (int i = 0; i < (int)(N * sizeof(T) / 16); i++) reinterpret_cast<uint4 *>(dst)[i] = s[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i++) dst[i] = x[i];
+  }
+}
+
+// The sequences of a packed batch.  What the arrays hold is not checked by the host, so every row number is brought into
+// [0, tokens] and every slot is compared with n_slots here: nothing outside of the arrays is touched whatever they hold.
+struct Sequences {
+  const int32_t *start, *slots, *resume;
+  int tokens, seqs, n_slots;
+
+  __device__ __forceinline__ int first(int n) const { return min(max(start[n], 0), tokens); }
+  // slot of sequence n, or -1 where it is padding
+  __device__ __forceinline__ int slot(int n) const {
+    const int s = slots ? slots[n] : n;
+    return s >= 0 && s < n_slots ? s : -1;
+  }
+  __device__ __forceinline__ bool resumed(int n) const { return resume && resume[n] != 0; }
+};
+
+// The last sequence that starts at row t or before it (-1: none), found by all threads of the CTA together.
+__device__ __forceinline__ int sequence_at(const Sequences &sq, int t) {
+  int n = 0;
+  for (int i = 0; i <= sq.seqs; i += blockDim.x) {
+    const int at = i + threadIdx.x;
+    n += __syncthreads_count(at <= sq.seqs && sq.first(at) <= t);
+  }
+  return n - 1;
+}
+
+}  // namespace lq

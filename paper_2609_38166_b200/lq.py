@@ -23,6 +23,7 @@ EXPORTS = ["lq_decode_step", "lq_decode_step_profiled", "lq_decode_step_host", "
            "lq_window_flush",
            "lq_quantize_state", "lq_dequantize_state", "lq_ref_decode_step_f32", "lq_ref_decode_step_bf16",
            "lq_decode_launches", "lq_step_launches", "lq_check_device", "lq_clear_device_flags", "lq_selftest_bounded_wait",
+           "lq_conv_prompt", "lq_conv_step", "lq_norm_rotate", "lq_scan_prompt", "lq_scan_prompt_bytes", "lq_scan_step",
            "lq_static_stage_bytes", "lq_import_state", "lq_export_state", "lq_status_string", "lq_version"]
 
 
@@ -80,6 +81,16 @@ def lib() -> C.CDLL:
         L.lq_quantize_state.argtypes = L.lq_dequantize_state.argtypes = [vp] * 4
         L.lq_ref_decode_step_f32.argtypes = L.lq_ref_decode_step_bf16.argtypes = [vp] * 9
         L.lq_import_state.argtypes = L.lq_export_state.argtypes = [vp] * 4
+        i64 = C.c_int64
+        L.lq_conv_prompt.argtypes = [vp, vp, i64, vp, vp, vp, vp, i64, vp, vp, vp, vp]
+        L.lq_conv_step.argtypes = [vp, vp, i64, vp, vp, vp, vp, i64, vp, vp]
+        L.lq_norm_rotate.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp]
+        L.lq_scan_prompt.argtypes = [vp, vp, vp, i64, vp, vp]
+        L.lq_scan_step.argtypes = [vp, vp, vp, i64, vp]
+        for name in ("lq_conv_prompt", "lq_conv_step", "lq_norm_rotate", "lq_scan_prompt", "lq_scan_step"):
+            getattr(L, name).restype = C.c_int
+        L.lq_scan_prompt_bytes.restype = C.c_uint64
+        L.lq_scan_prompt_bytes.argtypes = [vp]
         _lib = L
     return _lib
 
@@ -87,6 +98,26 @@ def lib() -> C.CDLL:
 class _Kept:
     """A place for the C struct of a shape outside of the instance's dict, which holds the fields and nothing else."""
     __slots__ = ("_kept",)
+
+    def ref(self):
+        """A reference to the shape as the C struct, for a call of the library.  The struct is built once and kept until a
+        field changes, however it is changed: a decode step is one call per token and layer, and at small batches its
+        marshalling took longer than its kernels (10.1 us of host time a call, 2.7 us with the struct kept; comparing the
+        fields is 0.2 us of it)."""
+        fields = self.__dict__
+        try:
+            of, ref = self._kept
+            if of == fields:
+                return ref
+        except AttributeError:
+            pass
+        of, ref = dict(fields), C.byref(self.c())
+        if of == fields:                     # (another thread may be changing a field)
+            self._kept = (of, ref)
+        return ref
+
+    def __getstate__(self):                  # (copies and pickles carry the fields only)
+        return self.__dict__
 
 
 @dataclass
@@ -108,26 +139,6 @@ class Shape(_Kept):
     def c(self, batch: Optional[int] = None) -> _Shape:
         return _Shape(self.batch if batch is None else batch, self.heads_v, self.heads_qk, self.d_k, self.d_v, self.W, self.r,
                       self.n_iter, self.gate, self.smooth, self.delta, self.rec16, self.state_bf16)
-
-    def ref(self):
-        """A reference to the shape as the C struct, for a call of the library.  The struct is built once and kept until a
-        field changes, however it is changed: a decode step is one call per token and layer, and at small batches its
-        marshalling took longer than its kernels (10.1 us of host time a call, 2.7 us with the struct kept; comparing the
-        fields is 0.2 us of it)."""
-        fields = self.__dict__
-        try:
-            of, ref = self._kept
-            if of == fields:
-                return ref
-        except AttributeError:
-            pass
-        of, ref = dict(fields), C.byref(self.c())
-        if of == fields:                     # (another thread may be changing a field)
-            self._kept = (of, ref)
-        return ref
-
-    def __getstate__(self):                  # (copies and pickles carry the fields only)
-        return self.__dict__
 
 
 def head_bytes(sh: Shape) -> int:
@@ -375,6 +386,196 @@ def export_state(sh: Shape, st: State, arrays: StateArrays, stream=None) -> None
     """lq_export_state: write the packed state out as separate arrays."""
     s, a, cs = sh.ref(), C.byref(arrays.c()), C.byref(st.c())
     _check(lib().lq_export_state(s, cs, a, _stream(stream)), "lq_export_state")
+
+
+# ---- what surrounds the decode step in a layer: the operators on packed rows ----
+
+BF16, F16, F32 = 0, 1, 2                     # lq_type
+TYPES = {torch.bfloat16: BF16, torch.float16: F16, torch.float32: F32}
+_DTYPES = {v: k for k, v in TYPES.items()}
+NORM_NONE, NORM_L2, NORM_RMS = 0, 1, 2
+
+
+class _Conv(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("tokens", "seqs", "channels", "width", "n_slots", "silu", "type")]
+
+
+class _Norm(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("tokens", "heads_q", "heads_k", "dim", "rot", "pairs", "norm", "type")] + \
+               [(n, C.c_float) for n in ("eps", "scale_q", "scale_k")]
+
+
+class _Scan(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("tokens", "seqs", "max_len", "heads_v", "heads_qk", "d_k", "d_v", "n_slots", "select", "gate_type")]
+
+
+class _ScanIo(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "k", "v")] + [(n, C.c_int64) for n in ("q_stride", "k_stride", "v_stride")] + \
+               [(n, C.c_void_p) for n in ("beta", "alpha")] + [(n, C.c_int64) for n in ("beta_stride", "alpha_stride")] + \
+               [(n, C.c_void_p) for n in ("A", "dt_bias", "skip", "S", "seq_start", "slots", "resume")]
+
+
+@dataclass
+class ConvShape(_Kept):
+    """``lq_conv``: ``tokens`` packed rows of ``seqs`` sequences (``conv_step``: one row each), states in ``n_slots`` slots."""
+    tokens: int
+    seqs: int
+    channels: int
+    width: int = 4
+    n_slots: int = 0
+    silu: int = 1
+    type: int = BF16
+
+    def c(self) -> _Conv:
+        return _Conv(self.tokens, self.seqs, self.channels, self.width, self.n_slots, self.silu, self.type)
+
+
+@dataclass
+class NormShape(_Kept):
+    """``lq_norm``: heads of ``dim`` channels, of which the first ``rot`` are rotated."""
+    tokens: int
+    heads_q: int
+    heads_k: int
+    dim: int = 128
+    rot: int = 0
+    pairs: int = 0
+    norm: int = NORM_L2
+    type: int = BF16
+    eps: float = 1e-6
+    scale_q: float = 1.0
+    scale_k: float = 1.0
+
+    def c(self) -> _Norm:
+        return _Norm(self.tokens, self.heads_q, self.heads_k, self.dim, self.rot, self.pairs, self.norm, self.type, self.eps, self.scale_q,
+                     self.scale_k)
+
+
+@dataclass
+class ScanShape(_Kept):
+    """``lq_scan``: ``max_len`` is at least the length of the longest sequence (``scan_step`` does not look at it)."""
+    tokens: int
+    seqs: int
+    heads_v: int
+    heads_qk: int
+    max_len: int = 1
+    d_k: int = 128
+    d_v: int = 128
+    n_slots: int = 0
+    select: int = 0
+    gate_type: int = BF16
+
+    def c(self) -> _Scan:
+        return _Scan(self.tokens, self.seqs, self.max_len, self.heads_v, self.heads_qk, self.d_k, self.d_v, self.n_slots, self.select, self.gate_type)
+
+
+def _need(ok: bool, what: str, t) -> None:
+    if not ok:
+        raise LqError(f"{what}: " + ("missing" if t is None else f"{t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}"))
+
+
+def _rows(t, what: str, dtype, rows: int, *cols: int):
+    """(address, row stride) of [rows, *cols] of ``dtype`` whose rows are contiguous, on the current device."""
+    if t is None or t.dtype is not dtype or t.get_device() != torch.cuda.current_device() or t.shape != (rows, *cols):
+        _need(False, what, t)
+    stride, run = t.stride(), 1
+    for n, s in zip(reversed(cols), reversed(stride)):
+        _need(n == 1 or s == run, what, t)
+        run *= n
+    return t.data_ptr(), stride[0] if rows > 1 else max(stride[0], run)
+
+
+def _dense(t, what: str, dtype, *shape: int):
+    """Address of a contiguous tensor of that shape on the current device; None stays None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.get_device() != torch.cuda.current_device() or t.shape != shape or not t.is_contiguous():
+        _need(False, what, t)
+    return t.data_ptr()
+
+
+def conv_prompt(sh: ConvShape, x, w, bias, state, out, seq_start, slots=None, resume=None, stream=None) -> None:
+    """lq_conv_prompt: ``x``, ``out`` [tokens, channels] (rows may be strided), ``w`` [channels, width], ``bias`` [channels] or None,
+    ``state`` [n_slots, width-1, channels] or None, ``seq_start`` int32 [seqs+1], ``slots``, ``resume`` int32 [seqs] or None."""
+    dt, i32 = _DTYPES.get(sh.type), torch.int32
+    px, sx = _rows(x, "x", dt, sh.tokens, sh.channels)
+    po, so = _rows(out, "out", dt, sh.tokens, sh.channels)
+    rc = lib().lq_conv_prompt(sh.ref(), px, sx, _dense(w, "w", dt, sh.channels, sh.width), _dense(bias, "bias", dt, sh.channels),
+                              _dense(state, "state", dt, sh.n_slots, sh.width - 1, sh.channels), po, so,
+                              _dense(seq_start, "seq_start", i32, sh.seqs + 1), _dense(slots, "slots", i32, sh.seqs),
+                              _dense(resume, "resume", i32, sh.seqs), _stream(stream))
+    if rc:
+        _check(rc, "lq_conv_prompt")
+
+
+def conv_step(sh: ConvShape, x, w, bias, state, out, slots=None, stream=None) -> None:
+    """lq_conv_step: one row per sequence; ``out`` may be ``x``."""
+    dt = _DTYPES.get(sh.type)
+    px, sx = _rows(x, "x", dt, sh.tokens, sh.channels)
+    po, so = _rows(out, "out", dt, sh.tokens, sh.channels)
+    rc = lib().lq_conv_step(sh.ref(), px, sx, _dense(w, "w", dt, sh.channels, sh.width), _dense(bias, "bias", dt, sh.channels),
+                            _dense(state, "state", dt, sh.n_slots, sh.width - 1, sh.channels), po, so,
+                            _dense(slots, "slots", torch.int32, sh.seqs), _stream(stream))
+    if rc:
+        _check(rc, "lq_conv_step")
+
+
+def norm_rotate(sh: NormShape, q, k, out_q, out_k, w_q=None, w_k=None, positions=None, inv_freq=None, stream=None) -> None:
+    """lq_norm_rotate: ``q``, ``out_q`` [tokens, heads_q, dim], ``k``, ``out_k`` [tokens, heads_k, dim] (rows may be strided; an output
+    may be its input), ``w_q``, ``w_k`` fp32 [dim] or None, ``positions`` int32 [tokens], ``inv_freq`` fp32 [rot/2]."""
+    dt, f32 = _DTYPES.get(sh.type), torch.float32
+    pq, sq = _rows(q, "q", dt, sh.tokens, sh.heads_q, sh.dim) if sh.heads_q else (None, 0)
+    pk, sk = _rows(k, "k", dt, sh.tokens, sh.heads_k, sh.dim) if sh.heads_k else (None, 0)
+    poq, soq = _rows(out_q, "out_q", dt, sh.tokens, sh.heads_q, sh.dim) if sh.heads_q else (None, 0)
+    pok, sok = _rows(out_k, "out_k", dt, sh.tokens, sh.heads_k, sh.dim) if sh.heads_k else (None, 0)
+    rc = lib().lq_norm_rotate(sh.ref(), pq, sq, pk, sk, poq, soq, pok, sok, _dense(w_q, "w_q", f32, sh.dim), _dense(w_k, "w_k", f32, sh.dim),
+                              _dense(positions, "positions", torch.int32, sh.tokens), _dense(inv_freq, "inv_freq", f32, sh.rot // 2),
+                              _stream(stream))
+    if rc:
+        _check(rc, "lq_norm_rotate")
+
+
+def _scan_io(sh: ScanShape, q, k, v, beta, alpha, S, seq_start, slots, resume, A, dt_bias, skip) -> _ScanIo:
+    bf, f32, i32, gate, H = torch.bfloat16, torch.float32, torch.int32, _DTYPES.get(sh.gate_type), sh.heads_v
+    pq, sq = _rows(q, "q", bf, sh.tokens, sh.heads_qk, sh.d_k)
+    pk, sk = _rows(k, "k", bf, sh.tokens, sh.heads_qk, sh.d_k)
+    pv, sv = _rows(v, "v", bf, sh.tokens, H, sh.d_v)
+    pb, sb = _rows(beta, "beta", gate, sh.tokens, H)
+    pa, sa = (None, 0) if alpha is None else _rows(alpha, "alpha", gate, sh.tokens, H)
+    return _ScanIo(pq, pk, pv, sq, sk, sv, pb, pa, sb, sa, _dense(A, "A", f32, H), _dense(dt_bias, "dt_bias", f32, H), _dense(skip, "skip", f32, H),
+                   _dense(S, "S", f32, sh.n_slots, H, sh.d_k, sh.d_v), _dense(seq_start, "seq_start", i32, sh.seqs + 1),
+                   _dense(slots, "slots", i32, sh.seqs), _dense(resume, "resume", i32, sh.seqs))
+
+
+def scan_prompt_bytes(sh: ScanShape) -> int:
+    """lq_scan_prompt_bytes: the size of the workspace of ``scan_prompt``."""
+    return int(lib().lq_scan_prompt_bytes(sh.ref()))
+
+
+def scan_prompt(sh: ScanShape, q, k, v, beta, alpha, o, S, seq_start, slots=None, resume=None, A=None, dt_bias=None, skip=None, work=None,
+                stream=None) -> None:
+    """lq_scan_prompt: ``q``, ``k`` bf16 [tokens, heads_qk, d_k], ``v``, ``o`` bf16 [tokens, heads_v, d_v], ``beta``, ``alpha``
+    [tokens, heads_v] (rows of all of them may be strided; with ``sh.select`` beta is dt and alpha None), ``S`` fp32 [n_slots, heads_v,
+    d_k, d_v], ``A``, ``dt_bias``, ``skip`` fp32 [heads_v], ``work`` uint8 [scan_prompt_bytes] (None where that is 0)."""
+    io = _scan_io(sh, q, k, v, beta, alpha, S, seq_start, slots, resume, A, dt_bias, skip)
+    po, so = _rows(o, "o", torch.bfloat16, sh.tokens, sh.heads_v, sh.d_v)
+    if work is not None and work.numel():
+        need = scan_prompt_bytes(sh)
+        _need(work.dtype is torch.uint8 and work.is_contiguous() and work.numel() >= need and work.get_device() == torch.cuda.current_device(),
+              f"work of {need} bytes", work)
+    else:
+        work = None
+    rc = lib().lq_scan_prompt(sh.ref(), C.byref(io), po, so, None if work is None else work.data_ptr(), _stream(stream))
+    if rc:
+        _check(rc, "lq_scan_prompt")
+
+
+def scan_step(sh: ScanShape, q, k, v, beta, alpha, o, S, slots=None, A=None, dt_bias=None, skip=None, stream=None) -> None:
+    """lq_scan_step: one row per sequence, as in ``scan_prompt``; ``o`` is fp32 [seqs, heads_v, d_v]."""
+    io = _scan_io(sh, q, k, v, beta, alpha, S, None, slots, None, A, dt_bias, skip)
+    po, so = _rows(o, "o", torch.float32, sh.tokens, sh.heads_v, sh.d_v)
+    rc = lib().lq_scan_step(sh.ref(), C.byref(io), po, so, _stream(stream))
+    if rc:
+        _check(rc, "lq_scan_step")
 
 
 def clear_device_flags() -> None:
