@@ -317,7 +317,7 @@ lq_status lq_ref_decode_step_bf16(const lq_shape *shape, uint16_t *S, const uint
  *    per sequence, row n.
  *  - A row's channels are contiguous, `..._stride` is the distance between rows in elements, at least a row long:
  *    slices of a wider projection are taken as they are.  Such arrays need the alignment of their element type only,
- *    except for q, k, v of the scan: 16 bytes, and strides that are multiples of 8.  All other arrays are dense.
+ *    except for q, k, v and o of the scan: 16 bytes, and strides that are multiples of 8.  All other arrays are dense.
  *  - States are kept in SLOTS: sequence n has slot slots[n] (int32 [seqs] in device memory; null: slot n).  Where slots[n] is
  *    negative or not below n_slots, the sequence is padding: none of its rows is written and no state is touched.  No two
  *    sequences of a call may share a slot.
@@ -391,7 +391,7 @@ lq_status lq_norm_rotate(const lq_norm *shape, const void *q, int64_t q_stride, 
  *     S_t = alpha_t S_{t-1} + beta_t k_t v_t^T,      o_t = S_t^T q_t + skip v_t
  * Value head h reads q/k head h/(Hv/Hqk), as in lq_decode_step.  With `select`, beta holds the raw step dt and
  *     dt' = log(1 + exp(dt + dt_bias_h)),   beta_t = dt',   alpha_t = exp(dt' A_h)      (alpha is not looked at).
- *   q, k : bf16 [tokens][Hqk][d_k]    v : bf16 [tokens][Hv][d_v]      strided rows, 16-byte aligned, strides multiples of 8
+ *   q, k : bf16 [tokens][Hqk][d_k]    v : bf16 [tokens][Hv][d_v]      strided rows, 16-byte aligned, strides multiples of 8 (o too)
  *   beta, alpha : [tokens][Hv] of gate_type, strided rows; alpha in [0, 1]
  *   A, dt_bias, skip : fp32 [Hv]; dt_bias and skip may be null (0); A is needed with `select` only, and is not positive
  *   S : fp32 [n_slots][Hv][d_k][d_v], in and out - what lq_quantize_state takes

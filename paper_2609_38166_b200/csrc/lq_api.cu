@@ -14,6 +14,10 @@
 
 namespace lq {
 
+// The error flag of the operators on packed rows (lq_ops.cu)
+bool ops_flags(int *flags);
+bool clear_ops_flags();
+
 // ---------------------------------------------------------------------------------------------
 // Baseline: Eq. 1 on a dense state that is read and written in full every token.
 // ---------------------------------------------------------------------------------------------
@@ -1048,18 +1052,18 @@ lq_status lq_export_state(const lq_shape *shape, const lq_state *src, const lq_s
 
 lq_status lq_check_device(int *flags) {
   if (!flags) return LQ_ERR_NULL;
-  int v = 0;
-  if (cudaMemcpyFromSymbol(&v, g_device_error, sizeof(int)) != cudaSuccess) {
+  int v = 0, ops = 0;
+  if (cudaMemcpyFromSymbol(&v, g_device_error, sizeof(int)) != cudaSuccess || !ops_flags(&ops)) {
     cudaGetLastError();
     return LQ_ERR_CUDA;
   }
-  *flags = v;
+  *flags = v | ops;
   return LQ_OK;
 }
 
 lq_status lq_clear_device_flags(void) {
   const int zero = 0;
-  if (cudaMemcpyToSymbol(g_device_error, &zero, sizeof(int)) != cudaSuccess) {
+  if (cudaMemcpyToSymbol(g_device_error, &zero, sizeof(int)) != cudaSuccess || !clear_ops_flags()) {
     cudaGetLastError();
     return LQ_ERR_CUDA;
   }

@@ -1,4 +1,5 @@
 // C boundary of the operators around the decode step: argument checks and launches.  Declarations and contracts: include/lq.h.
+#include <atomic>
 #include <initializer_list>
 
 #include "lq_conv.cuh"
@@ -142,14 +143,13 @@ static lq_status check_scan_io(const lq_scan *s, const lq_scan_io *io, const voi
   if (!step && !io->seq_start) return LQ_ERR_NULL;
   if ((rc = check_arrays(4, {}, {io->A, io->dt_bias, io->skip, io->seq_start, io->slots, io->resume})) != LQ_OK) return rc;
   if (s->tokens == 0) return LQ_OK;
-  if ((rc = check_arrays(16, {io->q, io->k, io->v})) != LQ_OK) return rc;
-  if ((rc = check_arrays(step ? 4 : 2, {o})) != LQ_OK) return rc;
+  if ((rc = check_arrays(16, {io->q, io->k, io->v, o})) != LQ_OK) return rc;
   if ((rc = check_arrays(type_size(s->gate_type), {io->beta}, {io->alpha})) != LQ_OK) return rc;
   if (s->select ? !io->A : !io->alpha) return LQ_ERR_NULL;
   const int64_t wq = (int64_t)s->heads_qk * SD, wv = (int64_t)s->heads_v * SD;
   if (io->q_stride < wq || io->k_stride < wq || io->v_stride < wv || o_stride < wv) return LQ_ERR_SHAPE;
   if (io->beta_stride < s->heads_v || (!s->select && io->alpha_stride < s->heads_v)) return LQ_ERR_SHAPE;
-  if (io->q_stride % 8 || io->k_stride % 8 || io->v_stride % 8) return LQ_ERR_ALIGN;
+  if (io->q_stride % 8 || io->k_stride % 8 || io->v_stride % 8 || o_stride % 8) return LQ_ERR_ALIGN;
   return LQ_OK;
 }
 
@@ -157,12 +157,90 @@ static ScanArgs scan_args(const lq_scan *s, const lq_scan_io *io, void *o, int64
   auto bf = [](const uint16_t *p) { return reinterpret_cast<const __nv_bfloat16 *>(p); };
   return {bf(io->q), bf(io->k), bf(io->v), io->q_stride, io->k_stride, io->v_stride, io->beta_stride, io->alpha_stride, o_stride, io->beta, io->alpha,
           io->A, io->dt_bias, io->skip, io->S, o, {io->seq_start, io->slots, io->resume, s->tokens, s->seqs, s->n_slots}, s->heads_v,
-          s->heads_qk, s->max_len, s->select, s->gate_type == LQ_F32};
+          s->heads_qk, s->max_len < s->tokens ? s->max_len : s->tokens, s->select, s->gate_type == LQ_F32};
+}
+
+// How a call's prompts are cut.  Uncut, a CTA has all blocks of a head, and `heads` of them keep at most that many SMs busy; in p pieces
+// the blocks are gone through twice (the first time for the state alone).
+static ScanPlan scan_plan(const lq_scan *s, void *work) {
+  constexpr int SMS = 148;
+  const long max_len = s->max_len < s->tokens ? s->max_len : s->tokens;
+  const long heads = (long)s->seqs * s->heads_v, blocks = ceil_div(max_len, SB);
+  long best = 1;
+  double least = (double)ceil_div(heads, SMS) * blocks;
+  for (long p = 2; p <= 64 && 2 * p <= blocks; p++) {
+    const double t = (double)ceil_div(heads * p, SMS) * ceil_div(blocks, p) * 1.65 + 4.0;
+    if (t < least) least = t, best = p;
+  }
+  ScanPlan plan{};
+  plan.piece = (int)ceil_div(blocks > 0 ? blocks : 1, best) * SB;
+  plan.pieces = max_len > 0 ? (int)ceil_div(max_len, plan.piece) : 1;
+  plan.items = (int)(heads * plan.pieces);
+  plan.heads.set(s->heads_v);
+  plan.cuts.set(plan.pieces);
+  plan.group.set(s->heads_v / s->heads_qk);
+  plan.states = static_cast<float *>(work);
+  plan.decays = plan.states + (size_t)plan.items * (SD * SD);
+  return plan;
+}
+
+static uint64_t scan_bytes(const ScanPlan &plan) {
+  return plan.pieces > 1 ? (uint64_t)plan.items * (SD * SD + 1) * sizeof(float) : 0;
+}
+
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                 const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+static EncodeTiled encode_tiled() {
+  static const EncodeTiled f = [] {
+    void *p = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) p = nullptr;
+    cudaGetLastError();
+    return reinterpret_cast<EncodeTiled>(p);
+  }();
+  return f;
+}
+
+// [rows][heads][128] bf16 with strided rows, copied in boxes of SB rows of 64 channels of one head
+static bool row_map(CUtensorMap *map, const void *base, long rows, int heads, int64_t stride) {
+  const cuuint64_t size[3] = {SD, (cuuint64_t)heads, (cuuint64_t)rows}, strides[2] = {SD * 2, (cuuint64_t)stride * 2};
+  const cuuint32_t box[3] = {SD / 2, 1, SB}, one[3] = {1, 1, 1};
+  const EncodeTiled f = encode_tiled();
+  return f && f(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), size, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool OUT>
+static lq_status launch_scan(const ScanMaps &maps, const ScanArgs &a, const ScanPlan &plan, cudaStream_t stream) {
+  constexpr size_t smem = sizeof(ScanShared);
+  static std::atomic<uint64_t> ready{0};        // devices on which the kernel has been given its shared memory
+  int device = 0;
+  if (cudaGetDevice(&device) != cudaSuccess) return LQ_ERR_CUDA;
+  const uint64_t bit = uint64_t(1) << (device & 63);
+  if (!(ready.load(std::memory_order_relaxed) & bit)) {
+    if (cudaFuncSetAttribute(scan_blocks_kernel<OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
+      cudaGetLastError();
+      return LQ_ERR_CUDA;
+    }
+    ready.fetch_or(bit, std::memory_order_relaxed);
+  }
+  scan_blocks_kernel<OUT><<<plan.items < 148 ? plan.items : 148, SCAN_THREADS, smem, stream>>>(maps, a, plan);
+  return launched();
 }
 
 }  // namespace lq
 
 using namespace lq;
+
+// lq_check_device / lq_clear_device_flags: the flag of the kernels in this file (each source file has device variables of its own)
+namespace lq {
+bool ops_flags(int *flags) { return cudaMemcpyFromSymbol(flags, g_ops_error, sizeof(int)) == cudaSuccess; }
+bool clear_ops_flags() {
+  const int zero = 0;
+  return cudaMemcpyToSymbol(g_ops_error, &zero, sizeof(int)) == cudaSuccess;
+}
+}  // namespace lq
 
 extern "C" {
 
@@ -216,16 +294,26 @@ lq_status lq_norm_rotate(const lq_norm *s, const void *q, int64_t q_stride, cons
   return launch_norm<__nv_bfloat16>(s, a, cuda_stream(stream));
 }
 
-uint64_t lq_scan_prompt_bytes(const lq_scan *) { return 0; }
+uint64_t lq_scan_prompt_bytes(const lq_scan *s) { return check_scan(s, false) == LQ_OK ? scan_bytes(scan_plan(s, nullptr)) : 0; }
 
 lq_status lq_scan_prompt(const lq_scan *s, const lq_scan_io *io, uint16_t *o, int64_t o_stride, void *work, lq_stream stream) {
   lq_status rc = check_scan(s, false);
   if (rc != LQ_OK) return rc;
   if (s->seqs == 0) return LQ_OK;
   if ((rc = check_scan_io(s, io, o, o_stride, false)) != LQ_OK) return rc;
-  (void)work;
-  scan_tokens_kernel<<<s->seqs * s->heads_v, 256, 0, cuda_stream(stream)>>>(scan_args(s, io, o, o_stride));
-  return launched();
+  const ScanPlan plan = scan_plan(s, work);
+  if (plan.pieces > 1 && (rc = check_arrays(16, {work})) != LQ_OK) return rc;
+  ScanMaps maps{};
+  if (s->tokens > 0 && !(row_map(&maps.q, io->q, s->tokens, s->heads_qk, io->q_stride) && row_map(&maps.k, io->k, s->tokens, s->heads_qk, io->k_stride) &&
+                         row_map(&maps.v, io->v, s->tokens, s->heads_v, io->v_stride)))
+    return LQ_ERR_CUDA;
+  const ScanArgs a = scan_args(s, io, o, o_stride);
+  if (plan.pieces > 1) {
+    if ((rc = launch_scan<false>(maps, a, plan, cuda_stream(stream))) != LQ_OK) return rc;
+    scan_join_kernel<<<s->seqs * s->heads_v * 16, 256, 0, cuda_stream(stream)>>>(a, plan);
+    if ((rc = launched()) != LQ_OK) return rc;
+  }
+  return launch_scan<true>(maps, a, plan, cuda_stream(stream));
 }
 
 lq_status lq_scan_step(const lq_scan *s, const lq_scan_io *io, float *o, int64_t o_stride, lq_stream stream) {

@@ -1,6 +1,7 @@
 // Selective state space scan with a scalar decay per head: S <- alpha S + beta k v^T, o = S^T q + skip v.
 #pragma once
 #include "lq_rows.cuh"
+#include "lq_tensor.cuh"
 
 namespace lq {
 
@@ -109,30 +110,777 @@ __global__ void __launch_bounds__(256) scan_step_kernel(const ScanArgs a) {
   scan_emit<float>(a, t, o, n, h);
 }
 
-// The prompt, token by token: a CTA has one head of one sequence.
-__global__ void __launch_bounds__(256) scan_tokens_kernel(const ScanArgs a) {
-  __shared__ __align__(16) ScanToken t;
-  const int n = blockIdx.x / a.heads_v, h = blockIdx.x - n * a.heads_v;
-  const int slot = a.sq.slot(n), warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const int first = a.sq.first(n), end = min(a.sq.first(n + 1), first + min(a.max_len, a.sq.tokens - first));
-  if (slot < 0) return;
-  float *S = a.S + ((size_t)slot * a.heads_v + h) * (SD * SD);
-  ScanState st;
-  if (a.sq.resumed(n)) {
-    st.load(S, warp, lane);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 16; i++) st.s[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+// ---------------------------------------------------------------------------------------------
+// Prompts, by blocks of C = 128 rows.  With G_i the sum of the block's log decays up to row i, P = Q K^T and S the state in front:
+//     o_i = exp(G_i) S^T q_i + sum_{j <= i} exp(G_i - G_j) beta_j P_ij v_j + skip v_i
+//     S   = exp(G_C) S + sum_j k_j (w_j v_j)^T,      w_j = exp(G_C - G_j) beta_j
+// Four products of 128 x 128 x 128 on the tensor cores: P, S^T q, the weighted P times V, and the state's, whose weighted values are
+// split into three bf16 pieces that add up to all 24 bits - the state stays binary32, at the price of three products for one.  P's
+// weights and S are rounded to bf16 where they enter a product with an output that is itself rounded to bf16.
+//
+// Six products of 2 * 128^3 operations a block and head are 0.26 us each at what one SM has of the measured peak; the 64 KB of v and o (q and
+// k are shared by the heads of a group and come from L2) take 1.5 us at its share of the bandwidth.  Both bounds are
+// close, so everything runs side by side in one CTA per SM:
+//   warp 0       tensor copies of the tiles of 32 KB, two slots each for K, Q and V
+//   warp 1       the products for the outputs: P, S^T q, weighted P times V
+//   warp 2       the block's gates: log decays, their sums, weights
+//   warp 3       the product for the state, dS^T = (weighted V)^T K
+//   warps 4-7    a row of P per thread: weights on P (to tensor memory, as the next product's operand)
+//   warps 8-15   half a row of o per thread: the factor that both of its parts have, the skip, outputs
+//   warps 16-23  weighted values (to tensor memory, 16 rows at a time, the operand of the state's product)
+//   warps 24-27  a value channel of S per thread (128 registers): S <- gamma S + dS, S as bf16 to shared memory
+// dS does not depend on S, so the only chain from block to block is S's update between two products.
+//
+// Both parts of o_i add up in one accumulator, S^T q_i + sum_j exp(-G_j) beta_j P_ij v_j, and exp(G_i) comes on in the end; where G_i is below
+// -100 (of log2), the accumulator is held at 2^100 o_i instead: S^T q_i then enters with 2^-100 rather than with less, which is nothing next to it.
+//
+// A sum G of log2 decays is held as a whole number and a fraction, added up apart: differences of sums lose nothing however far the
+// sums have come (a decay of 0 counts as 2^-200).
+//
+// Long prompts of few heads are cut into pieces of `piece` rows: a first pass (OUT false: dS only) leaves every piece's own sum and decay in the
+// workspace, scan_join_kernel turns them into the states in front of the pieces, and the second pass runs all pieces side by side.
+// ---------------------------------------------------------------------------------------------
+struct ScanMaps {
+  CUtensorMap q, k, v;
+};
+// Division of numbers below 2^31 by a constant of the call: a multiplication and a shift.
+struct Divisor {
+  uint32_t d, m, shift;
+  void set(uint32_t by) {
+    d = by;
+    shift = 0;
+    while (((uint64_t)1 << shift) < by) shift++;
+    m = (uint32_t)((((uint64_t)1 << (31 + shift)) + by - 1) / by);   // below 2^32
   }
+  __device__ __forceinline__ uint32_t quotient(uint32_t x) const { return (uint32_t)(((uint64_t)x * m) >> 31) >> shift; }
+};
+struct ScanPlan {
+  int piece, pieces;            // rows of a piece, pieces of the longest prompt (1: not cut)
+  int items;                    // seqs * pieces * heads_v
+  Divisor heads, cuts, group;   // division by heads_v, by pieces, by the value heads of a q/k head
+  float *states, *decays;       // [seqs][pieces][heads_v][128][128]: the state in front of a piece; [seqs][pieces][heads_v]
+};
+
+constexpr int SB = 128;                        // rows of a block
+constexpr int SCAN_THREADS = 896;
+constexpr uint32_t TILE = SB * SD * 2;         // a tile of Q, K or V: two halves of 64 channels, rows of 128 bytes, swizzled
+constexpr uint32_t HALF = TILE / 2;
+// Columns of tensor memory: P, o and dS^T (binary32), weighted P (bf16), and two buffers of weighted values (16 rows in three pieces of bf16)
+constexpr int TM_P = 0, TM_O = 128, TM_DS = 256, TM_PW = 384, TM_W = 448;
+
+constexpr float LEAST = -100.0f;               // of G in the factor of an output
+
+struct ScanSums {
+  float minus_whole[SB], minus_frac[SB];       // -G of every row
+  float beta[SB];
+};
+struct ScanWeights {
+  float e[SB];                                 // beta_j exp(G at the end of j's 32 rows - G_j)
+  float end_whole[4], end_frac[4];             // G at the end of every 32 rows
+  float rest[4];                               // exp(G_C - G at the end of every 32 rows)
+  float total, pad[3];                         // exp(G_C)
+};
+struct ScanShared {                            // (all but 96 bytes of what a CTA can have)
+  uint8_t k[2][TILE], q[2][TILE], v[2][TILE];
+  uint8_t s16[TILE];                           // S as bf16: rows of value channels, two halves of 64 key channels
+  ScanSums sums;
+  ScanWeights weights[2];
+  uint64_t k_full[2], k_empty[2], q_full[2], q_empty[2], v_full[2], v_empty[2], sums_full, sums_empty, weights_full[2], weights_empty[2];
+  uint64_t w_full[2], w_empty[2], p_full, p_free, pw_full, o1_full, o_full, o_free, ds_full, ds_free, s_full, clean[2], drained[2];
+  uint32_t tmem;
+};
+static_assert(sizeof(ScanShared) <= 232448, "");
+
+__device__ int g_ops_error = 0;
+constexpr int WAIT_LIMIT = 1 << 15;            // tries of a wait, each of which may last 20 us
+
+// Bounded wait; false: it ran out, leave (everybody else's next wait will too).  (Short, for there are dozens of them: the kernel's speed hangs on
+// how much of its code the instruction caches hold.)
+__device__ __forceinline__ bool wait_one(const uint64_t &bar, uint32_t parity) {
+  const uint32_t at = shared_addr(&bar);
+  int left = WAIT_LIMIT;
 #pragma unroll 1
-  for (int row = first; row < end; row++) {
-    const float alpha = scan_fetch(a, t, row, h);
-    __syncthreads();
-    const float4 o = st.token(alpha, t.bk + 16 * warp, t.q + 16 * warp, *reinterpret_cast<const float4 *>(t.v + 4 * lane));
-    scan_emit<__nv_bfloat16>(a, t, o, row, h);
-    __syncthreads();
+  while (!bar_try(at, parity))
+    if (--left == 0) return false;
+  return true;
+}
+// The same of a warp, with one answer for all of its lanes.
+__device__ __forceinline__ bool wait_for(const uint64_t &bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_one(bar, parity)); }
+
+// What a CTA does in one turn of its loop: rows [row, row + rows) of sequence n, head h.
+struct ScanItem {
+  int n, h, part, slot, row, rows, blocks;
+  bool first, last, state;                     // the prompt's first / last piece; a state in front of it that is not zero
+  template <bool OUT>
+  __device__ __forceinline__ bool get(const ScanArgs &a, const ScanPlan &plan, int item) {
+    const int r = plan.heads.quotient(item);
+    h = item - r * a.heads_v;
+    n = plan.cuts.quotient(r);
+    part = r - n * plan.pieces;
+    slot = a.sq.slot(n);
+    const int start = a.sq.first(n), len = min(max(a.sq.first(n + 1) - start, 0), a.max_len);
+    const int from = part * plan.piece;        // (pieces * piece is less than max_len + piece)
+    rows = max(min(len - from, plan.piece), 0);
+    row = start + from;
+    blocks = (rows + SB - 1) / SB;
+    first = part == 0;
+    last = from + rows >= len;
+    state = OUT && (!first || a.sq.resumed(n));
+    if (slot < 0) return false;
+    return OUT ? rows > 0 || first : rows > 0 && !last;
   }
-  st.store(S, warp, lane);
+};
+
+// A thread's value channel of S (binary32) from or to global memory [128][128]: the lanes of a warp have neighbouring value channels, so
+// every access is a whole line.
+__device__ __forceinline__ void load_state(float (&S)[SD], const float *mem) {
+#pragma unroll
+  for (int j = 0; j < SD; j++) S[j] = mem[j * SD];
+}
+__device__ __forceinline__ void store_state(const float (&S)[SD], float *mem) {
+#pragma unroll
+  for (int j = 0; j < SD; j++) mem[j * SD] = S[j];
+}
+
+// A thread's value channel of S as bf16 to shared memory, where the product with q reads it.  `at`: the thread's row.
+__device__ __forceinline__ void publish_state(const float (&S)[SD], uint8_t *at, int lane) {
+#pragma unroll
+  for (int c = 0; c < 16; c++) {
+    uint4 x;
+    x.x = pack_bf16(S[8 * c], S[8 * c + 1]);
+    x.y = pack_bf16(S[8 * c + 2], S[8 * c + 3]);
+    x.z = pack_bf16(S[8 * c + 4], S[8 * c + 5]);
+    x.w = pack_bf16(S[8 * c + 6], S[8 * c + 7]);
+    *reinterpret_cast<uint4 *>(at + (c / 8) * HALF + (((c % 8) ^ (lane & 7)) << 4)) = x;
+  }
+}
+
+// What a lane has of a block's gates before they are worked out: four consecutive rows of beta (or dt) and alpha.
+struct RawGates {
+  float beta[4], alpha[4];
+  int rows;                                    // rows of the block
+  int h;
+  __device__ __forceinline__ void load(const ScanArgs &a, int row, int rows_, int h_, int lane) {
+    rows = rows_, h = h_;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const int64_t r = row + min(4 * lane + i, rows - 1);   // (rows that are not there: loaded from the last one that is)
+      beta[i] = a.gate(a.beta, r * a.beta_stride + h);
+      alpha[i] = a.select ? 0.0f : a.gate(a.alpha, r * a.alpha_stride + h);
+    }
+  }
+};
+
+// A lane's part of the block's gates, four consecutive rows: worked out, then written when there is room.
+struct LaneGates {
+  float4 minus_whole, minus_frac, beta, e;
+  float end_whole, end_frac, rest, total;
+};
+__device__ __forceinline__ LaneGates scan_gates(const ScanArgs &a, const RawGates &raw, int lane) {
+  float whole[4], frac[4], beta[4];
+  float sw = 0.0f, sf = 0.0f;
+  const float bias = a.select && a.dt_bias ? a.dt_bias[raw.h] : 0.0f, rate = a.select ? a.A[raw.h] * 1.44269504088896340736f : 0.0f;
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    const bool there = 4 * lane + i < raw.rows;
+    float b = raw.beta[i], l;
+    if (a.select) {
+      b = softplus(b + bias);
+      l = b * rate;
+    } else {
+      l = log2f(raw.alpha[i]);
+    }
+    if (l < -200.0f) l = -200.0f;              // (2^-200 is 0 in binary32; a NaN stays)
+    b = there ? b : 0.0f;
+    l = there ? l : 0.0f;
+    beta[i] = b;
+    const float r = rintf(l);
+    sw += r;
+    sf += l - r;
+    whole[i] = sw;
+    frac[i] = sf;
+  }
+  float uw = sw, uf = sf;                      // sums over the lanes up to this one
+#pragma unroll
+  for (int m = 1; m < 32; m *= 2) {
+    const float w = __shfl_up_sync(0xffffffffu, uw, m), f = __shfl_up_sync(0xffffffffu, uf, m);
+    if (lane >= m) uw += w, uf += f;
+  }
+  const int ender = lane | 7;                  // the lane that ends these 32 rows
+  const float rw = __shfl_sync(0xffffffffu, uw, ender), rf = __shfl_sync(0xffffffffu, uf, ender);
+  const float tw = __shfl_sync(0xffffffffu, uw, 31), tf = __shfl_sync(0xffffffffu, uf, 31);
+  uw -= sw;
+  float before = __shfl_up_sync(0xffffffffu, uf, 1);
+  if (lane == 0) before = 0.0f;
+  LaneGates g;
+  g.end_whole = rw, g.end_frac = rf, g.rest = exp2_fast((tw - rw) + (tf - rf)), g.total = exp2_fast(tw + tf);
+  g.beta = make_float4(beta[0], beta[1], beta[2], beta[3]);
+  float *pw = &g.minus_whole.x, *pf = &g.minus_frac.x, *pe = &g.e.x;
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    const float w = uw + whole[i], f = before + frac[i];
+    pw[i] = -w;
+    pf[i] = -f;
+    pe[i] = beta[i] * exp2_fast((rw - w) + (rf - f));
+  }
+  return g;
+}
+
+// Values of 16 rows and 16 channels times the rows' weights, in three bf16 pieces: the leading 8 bits, the next 8, the rest - together all 24.
+// `at`: this lane's address for four transposed 8 x 8 matrices; afterwards the lane has two rows (weights w[m / 2]) of one channel in each.
+__device__ __forceinline__ void weigh_values(uint32_t at, const float2 (&w)[2], uint32_t (&hi)[4], uint32_t (&mid)[4], uint32_t (&low)[4]) {
+  uint32_t v[4];
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(at) : "memory");
+  const float2 minus = make_float2(-1.0f, -1.0f);
+  auto top = [](float2 x) { return make_float2(__uint_as_float(__float_as_uint(x.x) & 0xFFFF0000u), __uint_as_float(__float_as_uint(x.y) & 0xFFFF0000u)); };
+  auto tops = [](float2 x) { return __byte_perm(__float_as_uint(x.x), __float_as_uint(x.y), 0x7632); };
+#pragma unroll
+  for (int m = 0; m < 4; m++) {
+    float2 x = __fmul2_rn(w[m / 2], make_float2(__uint_as_float(v[m] << 16), __uint_as_float(v[m] & 0xFFFF0000u)));
+    hi[m] = tops(x);
+    x = __ffma2_rn(top(x), minus, x);
+    mid[m] = tops(x);
+    x = __ffma2_rn(top(x), minus, x);
+    low[m] = tops(x);
+  }
+}
+
+// One arrival for a warp whose lanes have all come this far; what they wrote is visible to who waits.
+__device__ __forceinline__ void warp_arrive(uint64_t &bar, int lane) {
+  __syncwarp();
+  if (lane == 0) bar_arrive(shared_addr(&bar));
+}
+
+// ---- warp 0 (one thread): tensor copies ----
+template <bool OUT>
+__device__ __forceinline__ void scan_copies(ScanShared &sm, const ScanMaps &maps, const ScanArgs &a, const ScanPlan &plan) {
+  ScanItem it;
+  int c = 0, asked[3] = {0, 0, 0};             // blocks; tiles of K, Q, V that have been asked for
+  bool ok = true;
+  tensor_map_prefetch(&maps.k);
+  tensor_map_prefetch(&maps.v);
+  if (OUT) tensor_map_prefetch(&maps.q);
+  auto copy = [&](const CUtensorMap *map, uint8_t (&to)[2][TILE], int head, int row, uint64_t (&full)[2], uint64_t (&empty)[2], int &count) {
+    const int r = c & 1;
+    if (c >= 2 && !(ok = wait_one(empty[r], ((c >> 1) + 1) & 1))) return false;
+    const uint32_t bar = shared_addr(&full[r]), dst = shared_addr(to[r]);
+    bar_expect(bar, TILE);
+    tensor_g2s(dst, map, 0, head, row, bar);
+    tensor_g2s(dst + HALF, map, 64, head, row, bar);
+    count++;
+    return true;
+  };
+  for (int item = blockIdx.x; ok && item < plan.items; item += gridDim.x) {
+    if (!it.get<OUT>(a, plan, item)) continue;
+    const int hq = plan.group.quotient(it.h);
+    for (int b = 0; b < it.blocks; b++, c++) {
+      const int row = it.row + b * SB;
+      if (OUT && !copy(&maps.q, sm.q, hq, row, sm.q_full, sm.q_empty, asked[1])) break;   // (Q is through first)
+      if (!copy(&maps.k, sm.k, hq, row, sm.k_full, sm.k_empty, asked[0])) break;
+      if (!copy(&maps.v, sm.v, it.h, row, sm.v_full, sm.v_empty, asked[2])) break;
+    }
+  }
+  if (!ok) {                                   // the copies that nobody waited for: the last two of each kind
+    atomicOr(&g_ops_error, 1);
+    auto landed = [](uint64_t (&full)[2], int n) {
+      for (int i = max(n - 2, 0); i < n; i++)
+        for (int spin = 0; spin < WAIT_LIMIT && !bar_try(shared_addr(&full[i & 1]), (i >> 1) & 1); spin++) {
+        }
+    };
+    landed(sm.k_full, asked[0]);
+    landed(sm.q_full, asked[1]);
+    landed(sm.v_full, asked[2]);
+  }
+}
+
+__device__ __forceinline__ void gave_up(bool yes) {
+  if (yes) atomicOr(&g_ops_error, 1);
+}
+
+// What a warp of matrix instructions does in the end where somebody gave up: what it has under way ends before tensor memory is freed.
+__device__ __forceinline__ void drain(uint64_t &bar) {
+  if (elect_one()) {
+    mma_commit(shared_addr(&bar));
+    for (int spin = 0; spin < WAIT_LIMIT && !bar_try(shared_addr(&bar), 0); spin++) {
+    }
+  }
+  __syncwarp();
+}
+
+// ---- warp 1: the products for the outputs ----
+__device__ __forceinline__ void scan_products(ScanShared &sm, const ScanArgs &a, const ScanPlan &plan, uint32_t tmem) {
+  constexpr uint32_t KK = mma_bf16(128, 128, false, false), KN = mma_bf16(128, 128, false, true);
+  const Operand S = operand(shared_addr(sm.s16), 16, 1024);
+  ScanItem it;
+  int c = 0, ns = 0;                           // blocks, states published so far
+  bool ok = true;
+  for (int item = blockIdx.x; ok && item < plan.items; item += gridDim.x) {
+    if (!it.get<true>(a, plan, item)) continue;
+    for (int b = 0; b < it.blocks; b++, c++) {
+      const int r = c & 1;
+      if (!(ok = wait_for(sm.k_full[r], (c >> 1) & 1))) break;
+      if (!(ok = wait_for(sm.q_full[r], (c >> 1) & 1))) break;
+      if (c > 0 && !(ok = wait_for(sm.p_free, (c + 1) & 1))) break;
+      tmem_fence_after();
+      const Operand K = operand(shared_addr(sm.k[0]) + r * TILE, 16, 1024), Q = operand(shared_addr(sm.q[0]) + r * TILE, 16, 1024), V = operand(shared_addr(sm.v[0]) + r * TILE, HALF, 1024);
+      if (elect_one()) {                       // P = Q K^T
+        mma_ss<false>(tmem + TM_P, Q, K, KK);
+#pragma unroll
+        for (int s = 1; s < 8; s++) mma_ss<true>(tmem + TM_P, Q + ((s / 4) * HALF + (s % 4) * 32), K + ((s / 4) * HALF + (s % 4) * 32), KK);
+        mma_commit(shared_addr(&sm.p_full));
+        mma_commit(shared_addr(&sm.k_empty[r]));
+      }
+      __syncwarp();
+      const bool state = it.state || b > 0;
+      if (c > 0 && !(ok = wait_for(sm.o_free, (c + 1) & 1))) break;
+      if (state) {                             // O = Q S
+        if (!(ok = wait_for(sm.s_full, ns++ & 1))) break;
+        tmem_fence_after();
+        if (elect_one()) {
+          mma_ss<false>(tmem + TM_O, Q, S, KK);
+#pragma unroll
+          for (int s = 1; s < 8; s++) mma_ss<true>(tmem + TM_O, Q + ((s / 4) * HALF + (s % 4) * 32), S + ((s / 4) * HALF + (s % 4) * 32), KK);
+        }
+        __syncwarp();
+      }
+      if (elect_one()) {
+        mma_commit(shared_addr(&sm.q_empty[r]));
+        mma_commit(shared_addr(&sm.o1_full));
+      }
+      __syncwarp();
+      if (!(ok = wait_for(sm.v_full[r], (c >> 1) & 1))) break;
+      if (!(ok = wait_for(sm.clean[r], (c >> 1) & 1))) break;
+      if (!(ok = wait_for(sm.pw_full, c & 1))) break;
+      tmem_fence_after();
+      if (elect_one()) {                       // O += (weighted P) V
+        mma_ts(tmem + TM_O, tmem + TM_PW, V, KN, state);
+#pragma unroll
+        for (int s = 1; s < 8; s++) mma_ts<true>(tmem + TM_O, tmem + TM_PW + 8 * s, V + s * 2048, KN);
+        mma_commit(shared_addr(&sm.o_full));
+        mma_commit(shared_addr(&sm.v_empty[r]));
+      }
+      __syncwarp();
+    }
+  }
+  if (!ok) drain(sm.drained[0]);
+  gave_up(!ok);
+}
+
+// ---- warp 3: the product for the state, dS^T = (weighted V)^T K, the small pieces first ----
+template <bool OUT>
+__device__ __forceinline__ void scan_state_product(ScanShared &sm, const ScanArgs &a, const ScanPlan &plan, uint32_t tmem) {
+  constexpr uint32_t KN = mma_bf16(128, 128, false, true);
+  ScanItem it;
+  int c = 0;
+  bool ok = true;
+  for (int item = blockIdx.x; ok && item < plan.items; item += gridDim.x) {
+    if (!it.get<OUT>(a, plan, item)) continue;
+    for (int b = 0; b < it.blocks; b++, c++) {
+      const int r = c & 1;
+      if (!(ok = wait_for(sm.k_full[r], (c >> 1) & 1))) break;
+      if (c > 0 && !(ok = wait_for(sm.ds_free, (c + 1) & 1))) break;
+      const Operand K = operand(shared_addr(sm.k[0]) + r * TILE, HALF, 1024);
+#pragma unroll 1
+      for (int q = 0; q < SB / 16; q++) {
+        const int r = q & 1;
+        if (!(ok = wait_for(sm.w_full[r], (q >> 1) & 1))) break;   // (four uses of a buffer in a block)
+        tmem_fence_after();
+        const uint32_t W = tmem + TM_W + 24 * r;
+        const Operand y = K + q * 2048;
+        if (elect_one()) {
+          mma_ts(tmem + TM_DS, W + 16, y, KN, q > 0);
+          mma_ts<true>(tmem + TM_DS, W + 8, y, KN);
+          mma_ts<true>(tmem + TM_DS, W, y, KN);
+          mma_commit(shared_addr(&sm.w_empty[r]));
+        }
+        __syncwarp();
+      }
+      if (!ok) break;
+      if (elect_one()) {
+        mma_commit(shared_addr(&sm.ds_full));
+        mma_commit(shared_addr(&sm.k_empty[r]));
+        mma_commit(shared_addr(&sm.v_empty[r]));
+      }
+      __syncwarp();
+    }
+  }
+  if (!ok) drain(sm.drained[1]);
+  gave_up(!ok);
+}
+
+// ---- warps 4 - 7: weights on P.  A thread has row i = 32 w + lane ----
+__device__ __forceinline__ void scan_weights(ScanShared &sm, const ScanArgs &a, const ScanPlan &plan, uint32_t tmem, int w, int lane) {
+  const int i = 32 * w + lane;
+  const uint32_t mine = tmem + ((uint32_t)(32 * w) << 16);
+  {                                            // above the diagonal there is nothing, in every block
+    uint32_t zero[16];
+#pragma unroll
+    for (int j = 0; j < 16; j++) zero[j] = 0;
+    for (int col = w + 1; col < 4; col++) tmem_store16(mine + TM_PW + 16 * col, zero);
+  }
+  ScanItem it;
+  int c = 0;
+  bool ok = true;
+  for (int item = blockIdx.x; ok && item < plan.items; item += gridDim.x) {
+    if (!it.get<true>(a, plan, item)) continue;
+    for (int b = 0; b < it.blocks; b++, c++) {
+      const ScanWeights &g = sm.weights[c & 1];
+      const int rows = min(it.rows - b * SB, SB);
+      if (!(ok = wait_for(sm.weights_full[c & 1], (c >> 1) & 1))) break;
+      if (!(ok = wait_for(sm.sums_full, c & 1))) break;
+      const bool far = -sm.sums.minus_whole[i] < LEAST;      // (of G_i, what is not in the output's factor)
+      const float whole = far ? -sm.sums.minus_whole[i] - LEAST : 0.0f, frac = far ? -sm.sums.minus_frac[i] : 0.0f;
+      if (!(ok = wait_for(sm.p_full, c & 1))) break;
+      if (c > 0 && !(ok = wait_for(sm.o_full, (c + 1) & 1))) break;   // (the product that reads the weighted P of the block before)
+      tmem_fence_after();
+#pragma unroll 1
+      for (int col = 0; col <= w; col++) {
+        uint32_t p[32], packed[16];
+        tmem_load32(mine + TM_P + 32 * col, p);
+        tmem_wait_loads(p);
+        if (col < w) {                         // all rows below these columns: exp(G_i - G_end) exp(G_end - G_j), the second at most 1
+          const float f = exp2_fast((whole - g.end_whole[col]) + (frac - g.end_frac[col]));
+          const float2 ff = make_float2(f, f);
+          const float4 *e = reinterpret_cast<const float4 *>(g.e + 32 * col);
+#pragma unroll
+          for (int j = 0; j < 8; j++) {
+            const float4 x = e[j];
+            const float2 y = __fmul2_rn(ff, __fmul2_rn(make_float2(x.x, x.y), make_float2(__uint_as_float(p[4 * j]), __uint_as_float(p[4 * j + 1]))));
+            const float2 z = __fmul2_rn(ff, __fmul2_rn(make_float2(x.z, x.w), make_float2(__uint_as_float(p[4 * j + 2]), __uint_as_float(p[4 * j + 3]))));
+            packed[2 * j] = pack_bf16(y.x, y.y);
+            packed[2 * j + 1] = pack_bf16(z.x, z.y);
+          }
+        } else {
+          const int last = min(lane, rows - 1 - 32 * col);   // (columns of rows that are not there: nothing, whatever P holds)
+          const float2 whole2 = make_float2(whole, whole), frac2 = make_float2(frac, frac);
+          const float4 *gw = reinterpret_cast<const float4 *>(sm.sums.minus_whole + 32 * col),
+                       *gf = reinterpret_cast<const float4 *>(sm.sums.minus_frac + 32 * col), *gb = reinterpret_cast<const float4 *>(sm.sums.beta + 32 * col);
+#pragma unroll
+          for (int j = 0; j < 8; j++) {
+            const float4 x = gw[j], y = gf[j], z = gb[j];
+            auto weighted = [&](float2 xw, float2 xf, float2 beta, int k) {
+              const float2 d = __fadd2_rn(__fadd2_rn(whole2, xw), __fadd2_rn(frac2, xf));
+              const float2 e = __fmul2_rn(__fmul2_rn(beta, make_float2(exp2_fast(d.x), exp2_fast(d.y))),
+                                          make_float2(__uint_as_float(p[4 * j + k]), __uint_as_float(p[4 * j + k + 1])));
+              return pack_bf16(4 * j + k <= last ? e.x : 0.0f, 4 * j + k + 1 <= last ? e.y : 0.0f);
+            };
+            packed[2 * j] = weighted(make_float2(x.x, x.y), make_float2(y.x, y.y), make_float2(z.x, z.y), 0);
+            packed[2 * j + 1] = weighted(make_float2(x.z, x.w), make_float2(y.z, y.w), make_float2(z.z, z.w), 2);
+          }
+        }
+        tmem_store16(mine + TM_PW + 16 * col, packed);
+      }
+      tmem_wait_stores();
+      tmem_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        bar_arrive(shared_addr(&sm.p_free));
+        bar_arrive(shared_addr(&sm.pw_full));
+        bar_arrive(shared_addr(&sm.sums_empty));
+        bar_arrive(shared_addr(&sm.weights_empty[c & 1]));
+      }
+    }
+  }
+  gave_up(!ok);
+}
+
+__device__ __forceinline__ void store_sector(void *to, const uint32_t (&x)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]),
+               "r"(x[6]), "r"(x[7])
+               : "memory");
+}
+
+// ---- warps 8 - 15: outputs.  A thread has row i = 32 w + lane and columns 64 * half .. 64 * half + 63 ----
+__device__ __forceinline__ void scan_outputs(ScanShared &sm, const ScanArgs &a, const ScanPlan &plan, uint32_t tmem, int warp, int lane) {
+  const int half = warp / 4, w = warp % 4, i = 32 * w + lane;
+  const uint32_t mine = tmem + ((uint32_t)(32 * w) << 16) + TM_O + 64 * half;
+  const bool sectors = reinterpret_cast<uintptr_t>(a.o) % 32 == 0 && a.o_stride % 16 == 0;   // a row's pieces are whole 32-byte sectors
+  ScanItem it;
+  int c = 0;
+  bool ok = true;
+  for (int item = blockIdx.x; ok && item < plan.items; item += gridDim.x) {
+    if (!it.get<true>(a, plan, item)) continue;
+    const float skip = a.skip ? a.skip[it.h] : 0.0f;
+    __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(a.o) + (int64_t)(it.row + i) * a.o_stride + it.h * SD + 64 * half;
+    for (int b = 0; b < it.blocks; b++, c++) {
+      if (!(ok = wait_for(sm.sums_full, c & 1))) break;
+      const float whole = -sm.sums.minus_whole[i], g = exp2_fast(whole >= LEAST ? whole - sm.sums.minus_frac[i] : LEAST);
+      const float2 gamma = make_float2(g, g);
+      warp_arrive(sm.sums_empty, lane);
+      if (!(ok = wait_for(sm.v_full[c & 1], (c >> 1) & 1))) break;
+      if (!(ok = wait_for(sm.o_full, c & 1))) break;
+      tmem_fence_after();
+      const bool there = it.row + b * SB + i < it.row + it.rows;
+      const uint8_t *V = sm.v[c & 1] + half * HALF + i * 128;
+#pragma unroll 1
+      for (int col = 0; col < 4; col++) {
+        uint32_t o[16], y[8];
+        tmem_load16(mine + 16 * col, o);
+        uint4 x[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+        if (a.skip) {
+          x[0] = *reinterpret_cast<const uint4 *>(V + (((2 * col) ^ (i & 7)) << 4));
+          x[1] = *reinterpret_cast<const uint4 *>(V + (((2 * col + 1) ^ (i & 7)) << 4));
+        }
+        const uint32_t in[8] = {x[0].x, x[0].y, x[0].z, x[0].w, x[1].x, x[1].y, x[1].z, x[1].w};
+        tmem_wait_loads(o);
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+          const float2 v = __fmul2_rn(make_float2(skip, skip), make_float2(__uint_as_float(in[j] << 16), __uint_as_float(in[j] & 0xFFFF0000u)));
+          const float2 z = __ffma2_rn(gamma, make_float2(__uint_as_float(o[2 * j]), __uint_as_float(o[2 * j + 1])), v);
+          y[j] = pack_bf16(z.x, z.y);
+        }
+        if (there) {                           // a thread's 32 bytes of a row: one sector where the rows allow it
+          if (sectors) {
+            store_sector(out + 16 * col, y);
+          } else {
+            reinterpret_cast<uint4 *>(out + 16 * col)[0] = make_uint4(y[0], y[1], y[2], y[3]);
+            reinterpret_cast<uint4 *>(out + 16 * col)[1] = make_uint4(y[4], y[5], y[6], y[7]);
+          }
+        }
+      }
+      tmem_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        bar_arrive(shared_addr(&sm.o_free));
+        bar_arrive(shared_addr(&sm.v_empty[c & 1]));
+      }
+      out += SB * a.o_stride;
+    }
+  }
+  gave_up(!ok);
+}
+
+// ---- warps 16 - 23: weighted values.  A warp has value channels 32 w .. 32 w + 31, the warps of a half have every other 16 rows ----
+template <bool OUT>
+__device__ __forceinline__ void scan_values(ScanShared &sm, const ScanArgs &a, const ScanPlan &plan, uint32_t tmem, int warp, int lane) {
+  const int half = warp / 4, w = warp % 4, thread = 32 * warp + lane;
+  const uint32_t to = tmem + ((uint32_t)(32 * w) << 16) + TM_W + 24 * half;
+  // matrix lane / 8: channels 8 (lane / 8 % 2) of 16, rows 8 (lane / 16) of 16
+  const int mrow = 8 * (lane / 16) + lane % 8, chunk = 4 * (w & 1) + (lane / 8) % 2;
+  const uint32_t first = (w >> 1) * HALF + half * 2048 + mrow * 128, pick[2] = {(uint32_t)((chunk ^ (lane % 8)) << 4), (uint32_t)(((chunk + 2) ^ (lane % 8)) << 4)};
+  ScanItem it;
+  int c = 0;
+  bool ok = true;
+  for (int item = blockIdx.x; ok && item < plan.items; item += gridDim.x) {
+    if (!it.get<OUT>(a, plan, item)) continue;
+    for (int b = 0; b < it.blocks; b++, c++) {
+      const int rows = min(it.rows - b * SB, SB);
+      uint8_t *V = sm.v[c & 1];
+      if (!(ok = wait_for(sm.weights_full[c & 1], (c >> 1) & 1))) break;
+      if (!(ok = wait_for(sm.v_full[c & 1], (c >> 1) & 1))) break;
+      if (rows < SB) {                         // rows of another sequence, or of none: what they hold must not meet the weights 0
+        if (!(ok = wait_for(sm.k_full[c & 1], (c >> 1) & 1))) break;
+        uint8_t *K = sm.k[c & 1];
+        for (int u = thread; u < (SB - rows) * 16; u += 256) {
+          const uint32_t off = (u & 1) * HALF + rows * 128 + (u >> 1) * 16;
+          *reinterpret_cast<uint4 *>(K + off) = make_uint4(0, 0, 0, 0);
+          *reinterpret_cast<uint4 *>(V + off) = make_uint4(0, 0, 0, 0);
+        }
+        fence_async_shared();
+      }
+      warp_arrive(sm.clean[c & 1], lane);
+      if (rows < SB && !(ok = wait_for(sm.clean[c & 1], (c >> 1) & 1))) break;
+      const uint32_t v = shared_addr(V) + first;
+      const ScanWeights &g = sm.weights[c & 1];
+      const float *weights = g.e + 16 * half + 2 * (lane % 4);
+#pragma unroll 1
+      for (int q = 0; q < SB / 32; q++) {
+        uint32_t hi[2][4], mid[2][4], low[2][4];
+        const float2 rest = make_float2(g.rest[q], g.rest[q]);
+        const float2 x[2] = {__fmul2_rn(rest, *reinterpret_cast<const float2 *>(weights + 32 * q)),
+                             __fmul2_rn(rest, *reinterpret_cast<const float2 *>(weights + 32 * q + 8))};
+#pragma unroll
+        for (int i = 0; i < 2; i++) weigh_values(v + q * 4096 + pick[i], x, hi[i], mid[i], low[i]);
+        if ((c > 0 || q > 0) && !(ok = wait_for(sm.w_empty[half], (q + 1) & 1))) break;
+        tmem_fence_after();
+#pragma unroll
+        for (int i = 0; i < 2; i++) {
+          const uint32_t lanes = to + ((uint32_t)(16 * i) << 16);
+          tmem_store_16x8(lanes, hi[i]);
+          tmem_store_16x8(lanes + 8, mid[i]);
+          tmem_store_16x8(lanes + 16, low[i]);
+        }
+        tmem_wait_stores();
+        tmem_fence_before();
+        warp_arrive(sm.w_full[half], lane);
+      }
+      if (!ok) break;
+      warp_arrive(sm.weights_empty[c & 1], lane);
+    }
+  }
+  gave_up(!ok);
+}
+
+// ---- warps 24 - 27: the state.  A thread has value channel 32 w + lane ----
+template <bool OUT>
+__device__ __forceinline__ void scan_state(ScanShared &sm, const ScanArgs &a, const ScanPlan &plan, uint32_t tmem, int w, int lane) {
+  const uint32_t mine = tmem + ((uint32_t)(32 * w) << 16) + TM_DS;
+  const int channel = 32 * w + lane;
+  uint8_t *s16 = sm.s16 + channel * 128;
+  ScanItem it;
+  int c = 0;
+  bool ok = true;
+  for (int item = blockIdx.x; ok && item < plan.items; item += gridDim.x) {
+    if (!it.get<OUT>(a, plan, item)) continue;
+    const size_t at = ((size_t)it.n * plan.pieces + it.part) * a.heads_v + it.h;
+    float *slot = a.S + ((size_t)it.slot * a.heads_v + it.h) * (SD * SD) + channel;
+    float S[SD];
+#pragma unroll
+    for (int j = 0; j < SD; j++) S[j] = 0.0f;
+    if (it.state && it.blocks > 0) load_state(S, plan.pieces > 1 ? plan.states + at * (SD * SD) + channel : slot);
+    float decay = 1.0f;
+    for (int b = 0; b < it.blocks; b++, c++) {
+      if (OUT && (it.state || b > 0)) {
+        // The product that reads the state in front of the last block.  (Waited for only where a state is published: until then the product
+        // behind does not run, so this phase cannot be passed twice.)
+        if (c > 0 && !(ok = wait_for(sm.o1_full, (c + 1) & 1))) break;
+        publish_state(S, s16, lane);
+        fence_async_shared();
+        warp_arrive(sm.s_full, lane);
+      }
+      if (!(ok = wait_for(sm.weights_full[c & 1], (c >> 1) & 1))) break;
+      const float gamma = sm.weights[c & 1].total;
+      warp_arrive(sm.weights_empty[c & 1], lane);
+      decay *= gamma;
+      if (!(ok = wait_for(sm.ds_full, c & 1))) break;
+      tmem_fence_after();
+#pragma unroll
+      for (int col = 0; col < 8; col++) {
+        uint32_t d[16];
+        tmem_load16(mine + 16 * col, d);
+        tmem_wait_loads(d);
+#pragma unroll
+        for (int j = 0; j < 16; j++) S[16 * col + j] = fmaf(gamma, S[16 * col + j], __uint_as_float(d[j]));
+      }
+      tmem_fence_before();
+      warp_arrive(sm.ds_free, lane);
+    }
+    if (!ok) break;
+    if (OUT) {
+      if (it.last && (it.blocks > 0 || !it.state)) store_state(S, slot);
+    } else {
+      store_state(S, plan.states + (at + a.heads_v) * (SD * SD) + channel);
+      if (channel == 0) plan.decays[at] = decay;
+    }
+  }
+  gave_up(!ok);
+}
+
+// ---- warp 2: gates.  The next block's are loaded before this block's are worked out ----
+template <bool OUT>
+__device__ __forceinline__ void scan_gate_warp(ScanShared &sm, const ScanArgs &a, const ScanPlan &plan, int lane) {
+  ScanItem it;
+  RawGates next;
+  int item = blockIdx.x, b = 0, c = 0;
+  auto load = [&] {                            // the block that b and item point to, or the first one behind; false: there is none
+    while (item < plan.items) {
+      if ((b > 0 || it.get<OUT>(a, plan, item)) && b < it.blocks) {
+        next.load(a, it.row + b * SB, min(it.rows - b * SB, SB), it.h, lane);
+        b++;
+        return true;
+      }
+      item += gridDim.x, b = 0;
+    }
+    return false;
+  };
+  bool more = load(), ok = true;
+  for (; more; c++) {
+    const RawGates now = next;
+    more = load();
+    const LaneGates g = scan_gates(a, now, lane);
+    if (c >= 2 && !(ok = wait_for(sm.weights_empty[c & 1], ((c >> 1) + 1) & 1))) break;
+    ScanWeights &w = sm.weights[c & 1];
+    reinterpret_cast<float4 *>(w.e)[lane] = g.e;
+    if (lane % 8 == 7) w.end_whole[lane / 8] = g.end_whole, w.end_frac[lane / 8] = g.end_frac, w.rest[lane / 8] = g.rest;
+    if (lane == 0) w.total = g.total;
+    warp_arrive(sm.weights_full[c & 1], lane);
+    if (OUT) {
+      if (c >= 1 && !(ok = wait_for(sm.sums_empty, (c + 1) & 1))) break;
+      reinterpret_cast<float4 *>(sm.sums.minus_whole)[lane] = g.minus_whole;
+      reinterpret_cast<float4 *>(sm.sums.minus_frac)[lane] = g.minus_frac;
+      reinterpret_cast<float4 *>(sm.sums.beta)[lane] = g.beta;
+      warp_arrive(sm.sums_full, lane);
+    }
+  }
+  gave_up(!ok);
+}
+
+template <bool OUT>
+__global__ void __launch_bounds__(SCAN_THREADS, 1) scan_blocks_kernel(const __grid_constant__ ScanMaps maps, const ScanArgs a, const ScanPlan plan) {
+  extern __shared__ __align__(1024) uint8_t raw[];
+  ScanShared &sm = *reinterpret_cast<ScanShared *>(raw);
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  if (shared_addr(raw) % 1024 != 0) {          // (the swizzled tiles count on it)
+    if (threadIdx.x == 0) atomicOr(&g_ops_error, 2);
+    return;
+  }
+  if (threadIdx.x == 0) {
+    auto init = [](uint64_t &bar, int count) { bar_init(shared_addr(&bar), count); };
+    for (int i = 0; i < 2; i++) {              // K is left by two products, V by two products and the eight warps that add the skip
+      init(sm.k_full[i], 1), init(sm.k_empty[i], OUT ? 2 : 1), init(sm.q_full[i], 1), init(sm.q_empty[i], 1);
+      init(sm.v_full[i], 1), init(sm.v_empty[i], OUT ? 10 : 1);
+      init(sm.weights_full[i], 1), init(sm.weights_empty[i], OUT ? 16 : 12);
+      init(sm.w_full[i], 4), init(sm.w_empty[i], 1);
+      init(sm.clean[i], 8), init(sm.drained[i], 1);
+    }
+    for (uint64_t *b : {&sm.sums_full, &sm.p_full, &sm.o1_full, &sm.o_full, &sm.ds_full}) init(*b, 1);
+    for (uint64_t *b : {&sm.p_free, &sm.pw_full, &sm.ds_free, &sm.s_full}) init(*b, 4);
+    init(sm.o_free, 8);
+    init(sm.sums_empty, 12);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 3) tmem_alloc(shared_addr(&sm.tmem), 512);
+  tmem_fence_before();
+  __syncthreads();
+  tmem_fence_after();
+  const uint32_t tmem = sm.tmem;
+  // 896 threads start with 72 registers each, 64512 in all: dealt out anew, 128 * (56 + 72 + 168) + 256 * (64 + 40)
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    if (warp == 0) {
+      if (lane == 0) scan_copies<OUT>(sm, maps, a, plan);
+    } else if (warp == 1) {
+      if (OUT) scan_products(sm, a, plan, tmem);
+    } else if (warp == 2) {
+      scan_gate_warp<OUT>(sm, a, plan, lane);
+    } else {
+      scan_state_product<OUT>(sm, a, plan, tmem);
+    }
+  } else if (warp < 8) {
+    if (OUT) scan_weights(sm, a, plan, tmem, warp - 4, lane);
+  } else if (warp < 16) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    if (OUT) scan_outputs(sm, a, plan, tmem, warp - 8, lane);
+  } else if (warp < 24) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    scan_values<OUT>(sm, a, plan, tmem, warp - 16, lane);
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+    scan_state<OUT>(sm, a, plan, tmem, warp - 24, lane);
+  }
+  __syncwarp();
+  tmem_fence_before();
+  __syncthreads();
+  tmem_fence_after();
+  if (warp == 3) tmem_free(tmem, 512);
+}
+
+// From every piece's own sum (in the place of the state in front of the next piece) to the states in front of the pieces.
+__global__ void __launch_bounds__(256) scan_join_kernel(const ScanArgs a, const ScanPlan plan) {
+  const int r = blockIdx.x / 16, n = r / a.heads_v, h = r - n * a.heads_v;
+  const int slot = a.sq.slot(n), start = a.sq.first(n), len = min(max(a.sq.first(n + 1) - start, 0), a.max_len);
+  if (slot < 0) return;
+  const size_t e = (size_t)(blockIdx.x % 16) * 1024 + threadIdx.x * 4;
+  float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  if (a.sq.resumed(n)) x = *reinterpret_cast<const float4 *>(a.S + ((size_t)slot * a.heads_v + h) * (SD * SD) + e);
+  for (int p = 0;; p++) {
+    const size_t at = ((size_t)n * plan.pieces + p) * a.heads_v + h;
+    *reinterpret_cast<float4 *>(plan.states + at * (SD * SD) + e) = x;
+    if ((p + 1) * plan.piece >= len) break;
+    const float d = plan.decays[at];
+    const float4 y = *reinterpret_cast<const float4 *>(plan.states + (at + a.heads_v) * (SD * SD) + e);
+    x = make_float4(fmaf(d, x.x, y.x), fmaf(d, x.y, y.y), fmaf(d, x.z, y.z), fmaf(d, x.w, y.w));
+  }
 }
 
 }  // namespace lq

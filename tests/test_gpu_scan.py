@@ -113,6 +113,13 @@ def test_single_tokens_packed():
     Case([1] * 40, 2, 2, resume=[i % 2 for i in range(40)]).check()
 
 
+@pytest.mark.parametrize("resume", ["none", "all", "some"])
+@pytest.mark.parametrize("lens", [[128] * 60, [3, 128, 64, 200, 0, 1] * 10, [256, 130] * 30])
+def test_many_heads_to_a_multiprocessor(lens, resume):
+    """Several heads one after the other in a CTA, with and without a state in front of them."""
+    Case(lens, 8, 2, resume=[{"none": 0, "all": 1, "some": i % 3 % 2}[resume] for i in range(len(lens))], skip=True).check()
+
+
 def test_decays_of_zero_and_one():
     """alpha 0 empties the state in the middle of a prompt, also many times in a block; alpha 1 keeps all."""
     c = Case([300, 260], 2, 1, gates=torch.float32, resume=[1, 1])
