@@ -211,22 +211,30 @@ static bool row_map(CUtensorMap *map, const void *base, long rows, int heads, in
                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool OUT>
-static lq_status launch_scan(const ScanMaps &maps, const ScanArgs &a, const ScanPlan &plan, cudaStream_t stream) {
+template <bool OUT, typename G, bool SELECT>
+static lq_status launch_scan_t(const ScanMaps &maps, const ScanArgs &a, const ScanPlan &plan, cudaStream_t stream) {
   constexpr size_t smem = sizeof(ScanShared);
   static std::atomic<uint64_t> ready{0};        // devices on which the kernel has been given its shared memory
   int device = 0;
   if (cudaGetDevice(&device) != cudaSuccess) return LQ_ERR_CUDA;
   const uint64_t bit = uint64_t(1) << (device & 63);
   if (!(ready.load(std::memory_order_relaxed) & bit)) {
-    if (cudaFuncSetAttribute(scan_blocks_kernel<OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
+    if (cudaFuncSetAttribute(scan_blocks_kernel<OUT, G, SELECT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
       cudaGetLastError();
       return LQ_ERR_CUDA;
     }
     ready.fetch_or(bit, std::memory_order_relaxed);
   }
-  scan_blocks_kernel<OUT><<<plan.items < 148 ? plan.items : 148, SCAN_THREADS, smem, stream>>>(maps, a, plan);
+  scan_blocks_kernel<OUT, G, SELECT><<<plan.items < 148 ? plan.items : 148, SCAN_THREADS, smem, stream>>>(maps, a, plan);
   return launched();
+}
+
+template <bool OUT>
+static lq_status launch_scan(const ScanMaps &maps, const ScanArgs &a, const ScanPlan &plan, cudaStream_t stream) {
+  if (a.select) {
+    return a.gates_f32 ? launch_scan_t<OUT, float, true>(maps, a, plan, stream) : launch_scan_t<OUT, __nv_bfloat16, true>(maps, a, plan, stream);
+  }
+  return a.gates_f32 ? launch_scan_t<OUT, float, false>(maps, a, plan, stream) : launch_scan_t<OUT, __nv_bfloat16, false>(maps, a, plan, stream);
 }
 
 }  // namespace lq

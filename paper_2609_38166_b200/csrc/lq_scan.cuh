@@ -192,7 +192,7 @@ struct ScanShared {                            // (all but 96 bytes of what a CT
 static_assert(sizeof(ScanShared) <= 232448, "");
 
 __device__ int g_ops_error = 0;
-constexpr int WAIT_LIMIT = 1 << 15;            // tries of a wait, each of which may last 20 us
+constexpr int WAIT_LIMIT = 1 << 20;            // tries of a wait
 
 // Bounded wait; false: it ran out, leave (everybody else's next wait will too).  (Short, for there are dozens of them: the kernel's speed hangs on
 // how much of its code the instruction caches hold.)
@@ -256,17 +256,19 @@ __device__ __forceinline__ void publish_state(const float (&S)[SD], uint8_t *at,
 }
 
 // What a lane has of a block's gates before they are worked out: four consecutive rows of beta (or dt) and alpha.
+template <typename G, bool SELECT>
 struct RawGates {
-  float beta[4], alpha[4];
+  G beta[4], alpha[4];
   int rows;                                    // rows of the block
   int h;
   __device__ __forceinline__ void load(const ScanArgs &a, int row, int rows_, int h_, int lane) {
     rows = rows_, h = h_;
+    const G *b = static_cast<const G *>(a.beta) + h, *al = static_cast<const G *>(a.alpha) + h;
 #pragma unroll
     for (int i = 0; i < 4; i++) {
-      const int64_t r = row + min(4 * lane + i, rows - 1);   // (rows that are not there: loaded from the last one that is)
-      beta[i] = a.gate(a.beta, r * a.beta_stride + h);
-      alpha[i] = a.select ? 0.0f : a.gate(a.alpha, r * a.alpha_stride + h);
+      const int r = row + min(4 * lane + i, rows - 1);       // (rows that are not there: loaded from the last one that is)
+      beta[i] = b[r * a.beta_stride];
+      if (!SELECT) alpha[i] = al[r * a.alpha_stride];
     }
   }
 };
@@ -276,19 +278,20 @@ struct LaneGates {
   float4 minus_whole, minus_frac, beta, e;
   float end_whole, end_frac, rest, total;
 };
-__device__ __forceinline__ LaneGates scan_gates(const ScanArgs &a, const RawGates &raw, int lane) {
+template <typename G, bool SELECT>
+__device__ __forceinline__ LaneGates scan_gates(const ScanArgs &a, const RawGates<G, SELECT> &raw, int lane) {
   float whole[4], frac[4], beta[4];
   float sw = 0.0f, sf = 0.0f;
-  const float bias = a.select && a.dt_bias ? a.dt_bias[raw.h] : 0.0f, rate = a.select ? a.A[raw.h] * 1.44269504088896340736f : 0.0f;
+  const float bias = SELECT && a.dt_bias ? a.dt_bias[raw.h] : 0.0f, rate = SELECT ? a.A[raw.h] * 1.44269504088896340736f : 0.0f;
 #pragma unroll
   for (int i = 0; i < 4; i++) {
     const bool there = 4 * lane + i < raw.rows;
-    float b = raw.beta[i], l;
-    if (a.select) {
+    float b = to_float(raw.beta[i]), l;
+    if (SELECT) {
       b = softplus(b + bias);
       l = b * rate;
     } else {
-      l = log2f(raw.alpha[i]);
+      l = log2f(to_float(raw.alpha[i]));
     }
     if (l < -200.0f) l = -200.0f;              // (2^-200 is 0 in binary32; a NaN stays)
     b = there ? b : 0.0f;
@@ -407,6 +410,16 @@ __device__ __forceinline__ void drain(uint64_t &bar) {
   __syncwarp();
 }
 
+// A product over 128 channels, two halves of 64 that lie HALF apart, anew.
+__device__ __forceinline__ void multiply_halves(uint32_t d, Operand a, Operand b, uint32_t what) {
+#pragma unroll 1
+  for (int half = 0; half < 2; half++) {
+    mma_ss(d, a + half * HALF, b + half * HALF, what, half > 0);
+#pragma unroll
+    for (int s = 1; s < 4; s++) mma_ss<true>(d, a + (half * HALF + s * 32), b + (half * HALF + s * 32), what);
+  }
+}
+
 // ---- warp 1: the products for the outputs ----
 __device__ __forceinline__ void scan_products(ScanShared &sm, const ScanArgs &a, const ScanPlan &plan, uint32_t tmem) {
   constexpr uint32_t KK = mma_bf16(128, 128, false, false), KN = mma_bf16(128, 128, false, true);
@@ -424,9 +437,7 @@ __device__ __forceinline__ void scan_products(ScanShared &sm, const ScanArgs &a,
       tmem_fence_after();
       const Operand K = operand(shared_addr(sm.k[0]) + r * TILE, 16, 1024), Q = operand(shared_addr(sm.q[0]) + r * TILE, 16, 1024), V = operand(shared_addr(sm.v[0]) + r * TILE, HALF, 1024);
       if (elect_one()) {                       // P = Q K^T
-        mma_ss<false>(tmem + TM_P, Q, K, KK);
-#pragma unroll
-        for (int s = 1; s < 8; s++) mma_ss<true>(tmem + TM_P, Q + ((s / 4) * HALF + (s % 4) * 32), K + ((s / 4) * HALF + (s % 4) * 32), KK);
+        multiply_halves(tmem + TM_P, Q, K, KK);
         mma_commit(shared_addr(&sm.p_full));
         mma_commit(shared_addr(&sm.k_empty[r]));
       }
@@ -437,9 +448,7 @@ __device__ __forceinline__ void scan_products(ScanShared &sm, const ScanArgs &a,
         if (!(ok = wait_for(sm.s_full, ns++ & 1))) break;
         tmem_fence_after();
         if (elect_one()) {
-          mma_ss<false>(tmem + TM_O, Q, S, KK);
-#pragma unroll
-          for (int s = 1; s < 8; s++) mma_ss<true>(tmem + TM_O, Q + ((s / 4) * HALF + (s % 4) * 32), S + ((s / 4) * HALF + (s % 4) * 32), KK);
+          multiply_halves(tmem + TM_O, Q, S, KK);
         }
         __syncwarp();
       }
@@ -453,9 +462,8 @@ __device__ __forceinline__ void scan_products(ScanShared &sm, const ScanArgs &a,
       if (!(ok = wait_for(sm.pw_full, c & 1))) break;
       tmem_fence_after();
       if (elect_one()) {                       // O += (weighted P) V
-        mma_ts(tmem + TM_O, tmem + TM_PW, V, KN, state);
-#pragma unroll
-        for (int s = 1; s < 8; s++) mma_ts<true>(tmem + TM_O, tmem + TM_PW + 8 * s, V + s * 2048, KN);
+#pragma unroll 2
+        for (int s = 0; s < 8; s++) mma_ts(tmem + TM_O, tmem + TM_PW + 8 * s, V + s * 2048, KN, state || s > 0);
         mma_commit(shared_addr(&sm.o_full));
         mma_commit(shared_addr(&sm.v_empty[r]));
       }
@@ -750,7 +758,12 @@ __device__ __forceinline__ void scan_state(ScanShared &sm, const ScanArgs &a, co
         tmem_load16(mine + 16 * col, d);
         tmem_wait_loads(d);
 #pragma unroll
-        for (int j = 0; j < 16; j++) S[16 * col + j] = fmaf(gamma, S[16 * col + j], __uint_as_float(d[j]));
+        for (int j = 0; j < 16; j += 2) {
+          const float2 x = __ffma2_rn(make_float2(gamma, gamma), make_float2(S[16 * col + j], S[16 * col + j + 1]),
+                                      make_float2(__uint_as_float(d[j]), __uint_as_float(d[j + 1])));
+          S[16 * col + j] = x.x;
+          S[16 * col + j + 1] = x.y;
+        }
       }
       tmem_fence_before();
       warp_arrive(sm.ds_free, lane);
@@ -767,26 +780,29 @@ __device__ __forceinline__ void scan_state(ScanShared &sm, const ScanArgs &a, co
 }
 
 // ---- warp 2: gates.  The next block's are loaded before this block's are worked out ----
-template <bool OUT>
+template <bool OUT, typename G, bool SELECT>
 __device__ __forceinline__ void scan_gate_warp(ScanShared &sm, const ScanArgs &a, const ScanPlan &plan, int lane) {
   ScanItem it;
-  RawGates next;
-  int item = blockIdx.x, b = 0, c = 0;
-  auto load = [&] {                            // the block that b and item point to, or the first one behind; false: there is none
-    while (item < plan.items) {
+  RawGates<G, SELECT> next;
+  int item = blockIdx.x, b = 0, c = -1;
+  bool more = false, ok = true;
+  for (;; c++) {
+    const RawGates<G, SELECT> now = next;
+    const bool none = !more;
+    more = false;
+    while (item < plan.items) {                // the block that b and item point to, or the first one behind
       if ((b > 0 || it.get<OUT>(a, plan, item)) && b < it.blocks) {
         next.load(a, it.row + b * SB, min(it.rows - b * SB, SB), it.h, lane);
         b++;
-        return true;
+        more = true;
+        break;
       }
       item += gridDim.x, b = 0;
     }
-    return false;
-  };
-  bool more = load(), ok = true;
-  for (; more; c++) {
-    const RawGates now = next;
-    more = load();
+    if (none) {
+      if (more) continue;                      // (the first one)
+      break;
+    }
     const LaneGates g = scan_gates(a, now, lane);
     if (c >= 2 && !(ok = wait_for(sm.weights_empty[c & 1], ((c >> 1) + 1) & 1))) break;
     ScanWeights &w = sm.weights[c & 1];
@@ -805,7 +821,7 @@ __device__ __forceinline__ void scan_gate_warp(ScanShared &sm, const ScanArgs &a
   gave_up(!ok);
 }
 
-template <bool OUT>
+template <bool OUT, typename G, bool SELECT>
 __global__ void __launch_bounds__(SCAN_THREADS, 1) scan_blocks_kernel(const __grid_constant__ ScanMaps maps, const ScanArgs a, const ScanPlan plan) {
   extern __shared__ __align__(1024) uint8_t raw[];
   ScanShared &sm = *reinterpret_cast<ScanShared *>(raw);
@@ -842,7 +858,7 @@ __global__ void __launch_bounds__(SCAN_THREADS, 1) scan_blocks_kernel(const __gr
     } else if (warp == 1) {
       if (OUT) scan_products(sm, a, plan, tmem);
     } else if (warp == 2) {
-      scan_gate_warp<OUT>(sm, a, plan, lane);
+      scan_gate_warp<OUT, G, SELECT>(sm, a, plan, lane);
     } else {
       scan_state_product<OUT>(sm, a, plan, tmem);
     }

@@ -22,10 +22,10 @@ __device__ __forceinline__ void bar_arrive(uint32_t bar) { asm volatile("mbarrie
 __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-// One try, for which the warp may be suspended for up to 20 us.
+// One try, for which the warp may be suspended (for a time of the hardware's choosing).
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
   uint32_t done;
-  asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 20000;\n selp.u32 %0, 1, 0, p;\n}\n"
+  asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
                : "=r"(done) : "r"(bar), "r"(parity) : "memory");
   return done;
 }
@@ -130,6 +130,13 @@ __device__ __forceinline__ void mma_ss(uint32_t d, Operand a, Operand b, uint32_
   asm volatile(
       "{\n .reg .pred p;\n .reg .b64 a, b;\n setp.ne.u32 p, %6, 0;\n mov.b64 a, {%1, %2};\n mov.b64 b, {%3, %4};\n"
       " tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %5, p;\n}\n" ::"r"(d), "r"(a.low), "r"(a.high), "r"(b.low), "r"(b.high), "r"(what), "n"(ADD)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, Operand a, Operand b, uint32_t what, bool add) {
+  asm volatile(
+      "{\n .reg .pred p;\n .reg .b64 a, b;\n setp.ne.u32 p, %6, 0;\n mov.b64 a, {%1, %2};\n mov.b64 b, {%3, %4};\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %5, p;\n}\n" ::"r"(d), "r"(a.low), "r"(a.high), "r"(b.low), "r"(b.high), "r"(what),
+      "r"((uint32_t)add)
       : "memory");
 }
 template <bool ADD>
