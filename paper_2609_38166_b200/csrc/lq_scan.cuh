@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(256) scan_step_kernel(const ScanArgs a) {
 //   warp 3       the product for the state, dS^T = (weighted V)^T K
 //   warps 4-7    a row of P per thread: weights on P (to tensor memory, as the next product's operand)
 //   warps 8-15   half a row of o per thread: the factor that both of its parts have, the skip, outputs
-//   warps 16-23  weighted values (to tensor memory, 16 rows at a time, the operand of the state's product)
+//   warps 16-23  weighted values (to tensor memory, 32 rows at a time, the operand of the state's product)
 //   warps 24-27  a value channel of S per thread (128 registers): S <- gamma S + dS, S as bf16 to shared memory
 // dS does not depend on S, so the only chain from block to block is S's update between two products.
 //
@@ -165,8 +165,9 @@ constexpr int SB = 128;                        // rows of a block
 constexpr int SCAN_THREADS = 896;
 constexpr uint32_t TILE = SB * SD * 2;         // a tile of Q, K or V: two halves of 64 channels, rows of 128 bytes, swizzled
 constexpr uint32_t HALF = TILE / 2;
-// Columns of tensor memory: P, o and dS^T (binary32), weighted P (bf16), and two buffers of weighted values (16 rows in three pieces of bf16)
-constexpr int TM_P = 0, TM_O = 128, TM_DS = 256, TM_PW = 384, TM_W = 448;
+// Columns of tensor memory: P, o and dS^T (binary32), and two buffers of weighted values (twice 16 rows in three pieces of bf16, 24 columns).  The weighted P,
+// as bf16, takes the place of the first half of P: a thread has all of a row and has read what it overwrites.
+constexpr int TM_P = 0, TM_O = 128, TM_DS = 256, TM_W = 384;
 
 constexpr float LEAST = -100.0f;               // of G in the factor of an output
 
@@ -186,7 +187,7 @@ struct ScanShared {                            // (all but 96 bytes of what a CT
   ScanSums sums;
   ScanWeights weights[2];
   uint64_t k_full[2], k_empty[2], q_full[2], q_empty[2], v_full[2], v_empty[2], sums_full, sums_empty, weights_full[2], weights_empty[2];
-  uint64_t w_full[2], w_empty[2], p_full, p_free, pw_full, o1_full, o_full, o_free, ds_full, ds_free, s_full, clean[2], drained[2];
+  uint64_t w_full[2], w_empty[2], p_full, pw_full, o1_full, o_full, o_free, ds_full, ds_free, s_full, clean[2], drained[2];
   uint32_t tmem;
 };
 static_assert(sizeof(ScanShared) <= 232448, "");
@@ -421,7 +422,7 @@ __device__ __forceinline__ void multiply_halves(uint32_t d, Operand a, Operand b
 }
 
 // ---- warp 1: the products for the outputs ----
-__device__ __forceinline__ void scan_products(ScanShared &sm, const ScanArgs &a, const ScanPlan &plan, uint32_t tmem) {
+__device__ __forceinline__ void scan_products(ScanShared &sm, const ScanArgs &a, const ScanPlan &plan) {
   constexpr uint32_t KK = mma_bf16(128, 128, false, false), KN = mma_bf16(128, 128, false, true);
   const Operand S = operand(shared_addr(sm.s16), 16, 1024);
   ScanItem it;
@@ -433,11 +434,11 @@ __device__ __forceinline__ void scan_products(ScanShared &sm, const ScanArgs &a,
       const int r = c & 1;
       if (!(ok = wait_for(sm.k_full[r], (c >> 1) & 1))) break;
       if (!(ok = wait_for(sm.q_full[r], (c >> 1) & 1))) break;
-      if (c > 0 && !(ok = wait_for(sm.p_free, (c + 1) & 1))) break;
+      if (c > 0 && !(ok = wait_for(sm.o_full, (c + 1) & 1))) break;   // (the product that reads the weighted P of the block before)
       tmem_fence_after();
       const Operand K = operand(shared_addr(sm.k[0]) + r * TILE, 16, 1024), Q = operand(shared_addr(sm.q[0]) + r * TILE, 16, 1024), V = operand(shared_addr(sm.v[0]) + r * TILE, HALF, 1024);
       if (elect_one()) {                       // P = Q K^T
-        multiply_halves(tmem + TM_P, Q, K, KK);
+        multiply_halves(TM_P, Q, K, KK);
         mma_commit(shared_addr(&sm.p_full));
         mma_commit(shared_addr(&sm.k_empty[r]));
       }
@@ -448,7 +449,7 @@ __device__ __forceinline__ void scan_products(ScanShared &sm, const ScanArgs &a,
         if (!(ok = wait_for(sm.s_full, ns++ & 1))) break;
         tmem_fence_after();
         if (elect_one()) {
-          multiply_halves(tmem + TM_O, Q, S, KK);
+          multiply_halves(TM_O, Q, S, KK);
         }
         __syncwarp();
       }
@@ -463,7 +464,7 @@ __device__ __forceinline__ void scan_products(ScanShared &sm, const ScanArgs &a,
       tmem_fence_after();
       if (elect_one()) {                       // O += (weighted P) V
 #pragma unroll 2
-        for (int s = 0; s < 8; s++) mma_ts(tmem + TM_O, tmem + TM_PW + 8 * s, V + s * 2048, KN, state || s > 0);
+        for (int s = 0; s < 8; s++) mma_ts(TM_O, TM_P + 8 * s, V + s * 2048, KN, state || s > 0);
         mma_commit(shared_addr(&sm.o_full));
         mma_commit(shared_addr(&sm.v_empty[r]));
       }
@@ -476,7 +477,7 @@ __device__ __forceinline__ void scan_products(ScanShared &sm, const ScanArgs &a,
 
 // ---- warp 3: the product for the state, dS^T = (weighted V)^T K, the small pieces first ----
 template <bool OUT>
-__device__ __forceinline__ void scan_state_product(ScanShared &sm, const ScanArgs &a, const ScanPlan &plan, uint32_t tmem) {
+__device__ __forceinline__ void scan_state_product(ScanShared &sm, const ScanArgs &a, const ScanPlan &plan) {
   constexpr uint32_t KN = mma_bf16(128, 128, false, true);
   ScanItem it;
   int c = 0;
@@ -489,17 +490,20 @@ __device__ __forceinline__ void scan_state_product(ScanShared &sm, const ScanArg
       if (c > 0 && !(ok = wait_for(sm.ds_free, (c + 1) & 1))) break;
       const Operand K = operand(shared_addr(sm.k[0]) + r * TILE, HALF, 1024);
 #pragma unroll 1
-      for (int q = 0; q < SB / 16; q++) {
-        const int r = q & 1;
-        if (!(ok = wait_for(sm.w_full[r], (q >> 1) & 1))) break;   // (four uses of a buffer in a block)
+      for (int q = 0; q < SB / 32; q++) {
+        const int u = q & 1;
+        if (!(ok = wait_for(sm.w_full[u], q >> 1))) break;   // (two uses of a buffer in a block)
         tmem_fence_after();
-        const uint32_t W = tmem + TM_W + 24 * r;
-        const Operand y = K + q * 2048;
+        const uint32_t W = TM_W + 48 * u;
+        const Operand y = K + q * 4096;
         if (elect_one()) {
-          mma_ts(tmem + TM_DS, W + 16, y, KN, q > 0);
-          mma_ts<true>(tmem + TM_DS, W + 8, y, KN);
-          mma_ts<true>(tmem + TM_DS, W, y, KN);
-          mma_commit(shared_addr(&sm.w_empty[r]));
+          mma_ts(TM_DS, W + 16, y, KN, q > 0);
+          mma_ts<true>(TM_DS, W + 8, y, KN);
+          mma_ts<true>(TM_DS, W, y, KN);
+          mma_ts<true>(TM_DS, W + 40, y + 2048, KN);
+          mma_ts<true>(TM_DS, W + 32, y + 2048, KN);
+          mma_ts<true>(TM_DS, W + 24, y + 2048, KN);
+          mma_commit(shared_addr(&sm.w_empty[u]));
         }
         __syncwarp();
       }
@@ -517,15 +521,9 @@ __device__ __forceinline__ void scan_state_product(ScanShared &sm, const ScanArg
 }
 
 // ---- warps 4 - 7: weights on P.  A thread has row i = 32 w + lane ----
-__device__ __forceinline__ void scan_weights(ScanShared &sm, const ScanArgs &a, const ScanPlan &plan, uint32_t tmem, int w, int lane) {
+__device__ __forceinline__ void scan_weights(ScanShared &sm, const ScanArgs &a, const ScanPlan &plan, int w, int lane) {
   const int i = 32 * w + lane;
-  const uint32_t mine = tmem + ((uint32_t)(32 * w) << 16);
-  {                                            // above the diagonal there is nothing, in every block
-    uint32_t zero[16];
-#pragma unroll
-    for (int j = 0; j < 16; j++) zero[j] = 0;
-    for (int col = w + 1; col < 4; col++) tmem_store16(mine + TM_PW + 16 * col, zero);
-  }
+  const uint32_t mine = ((uint32_t)(32 * w) << 16);
   ScanItem it;
   int c = 0;
   bool ok = true;
@@ -534,12 +532,10 @@ __device__ __forceinline__ void scan_weights(ScanShared &sm, const ScanArgs &a, 
     for (int b = 0; b < it.blocks; b++, c++) {
       const ScanWeights &g = sm.weights[c & 1];
       const int rows = min(it.rows - b * SB, SB);
-      if (!(ok = wait_for(sm.weights_full[c & 1], (c >> 1) & 1))) break;
-      if (!(ok = wait_for(sm.sums_full, c & 1))) break;
+      if (!(ok = wait_for(sm.sums_full, c & 1))) break;      // (the weights are there before the sums)
       const bool far = -sm.sums.minus_whole[i] < LEAST;      // (of G_i, what is not in the output's factor)
       const float whole = far ? -sm.sums.minus_whole[i] - LEAST : 0.0f, frac = far ? -sm.sums.minus_frac[i] : 0.0f;
       if (!(ok = wait_for(sm.p_full, c & 1))) break;
-      if (c > 0 && !(ok = wait_for(sm.o_full, (c + 1) & 1))) break;   // (the product that reads the weighted P of the block before)
       tmem_fence_after();
 #pragma unroll 1
       for (int col = 0; col <= w; col++) {
@@ -576,13 +572,19 @@ __device__ __forceinline__ void scan_weights(ScanShared &sm, const ScanArgs &a, 
             packed[2 * j + 1] = weighted(make_float2(x.z, x.w), make_float2(y.z, y.w), make_float2(z.z, z.w), 2);
           }
         }
-        tmem_store16(mine + TM_PW + 16 * col, packed);
+        tmem_store16(mine + TM_P + 16 * col, packed);
+      }
+#pragma unroll 1
+      for (int col = w + 1; col < 4; col++) {  // above the diagonal there is nothing
+        uint32_t zero[16];
+#pragma unroll
+        for (int j = 0; j < 16; j++) zero[j] = 0;
+        tmem_store16(mine + TM_P + 16 * col, zero);
       }
       tmem_wait_stores();
       tmem_fence_before();
       __syncwarp();
       if (lane == 0) {
-        bar_arrive(shared_addr(&sm.p_free));
         bar_arrive(shared_addr(&sm.pw_full));
         bar_arrive(shared_addr(&sm.sums_empty));
         bar_arrive(shared_addr(&sm.weights_empty[c & 1]));
@@ -599,9 +601,9 @@ __device__ __forceinline__ void store_sector(void *to, const uint32_t (&x)[8]) {
 }
 
 // ---- warps 8 - 15: outputs.  A thread has row i = 32 w + lane and columns 64 * half .. 64 * half + 63 ----
-__device__ __forceinline__ void scan_outputs(ScanShared &sm, const ScanArgs &a, const ScanPlan &plan, uint32_t tmem, int warp, int lane) {
+__device__ __forceinline__ void scan_outputs(ScanShared &sm, const ScanArgs &a, const ScanPlan &plan, int warp, int lane) {
   const int half = warp / 4, w = warp % 4, i = 32 * w + lane;
-  const uint32_t mine = tmem + ((uint32_t)(32 * w) << 16) + TM_O + 64 * half;
+  const uint32_t mine = ((uint32_t)(32 * w) << 16) + TM_O + 64 * half;
   const bool sectors = reinterpret_cast<uintptr_t>(a.o) % 32 == 0 && a.o_stride % 16 == 0;   // a row's pieces are whole 32-byte sectors
   ScanItem it;
   int c = 0;
@@ -660,9 +662,9 @@ __device__ __forceinline__ void scan_outputs(ScanShared &sm, const ScanArgs &a, 
 
 // ---- warps 16 - 23: weighted values.  A warp has value channels 32 w .. 32 w + 31, the warps of a half have every other 16 rows ----
 template <bool OUT>
-__device__ __forceinline__ void scan_values(ScanShared &sm, const ScanArgs &a, const ScanPlan &plan, uint32_t tmem, int warp, int lane) {
+__device__ __forceinline__ void scan_values(ScanShared &sm, const ScanArgs &a, const ScanPlan &plan, int warp, int lane) {
   const int half = warp / 4, w = warp % 4, thread = 32 * warp + lane;
-  const uint32_t to = tmem + ((uint32_t)(32 * w) << 16) + TM_W + 24 * half;
+  const uint32_t mine = ((uint32_t)(32 * w) << 16) + TM_W + 24 * half;
   // matrix lane / 8: channels 8 (lane / 8 % 2) of 16, rows 8 (lane / 16) of 16
   const int mrow = 8 * (lane / 16) + lane % 8, chunk = 4 * (w & 1) + (lane / 8) % 2;
   const uint32_t first = (w >> 1) * HALF + half * 2048 + mrow * 128, pick[2] = {(uint32_t)((chunk ^ (lane % 8)) << 4), (uint32_t)(((chunk + 2) ^ (lane % 8)) << 4)};
@@ -699,18 +701,19 @@ __device__ __forceinline__ void scan_values(ScanShared &sm, const ScanArgs &a, c
                              __fmul2_rn(rest, *reinterpret_cast<const float2 *>(weights + 32 * q + 8))};
 #pragma unroll
         for (int i = 0; i < 2; i++) weigh_values(v + q * 4096 + pick[i], x, hi[i], mid[i], low[i]);
-        if ((c > 0 || q > 0) && !(ok = wait_for(sm.w_empty[half], (q + 1) & 1))) break;
+        const int u = q & 1;                   // two uses of a buffer in a block
+        if ((c > 0 || q > 1) && !(ok = wait_for(sm.w_empty[u], (q >> 1) ^ 1))) break;
         tmem_fence_after();
 #pragma unroll
         for (int i = 0; i < 2; i++) {
-          const uint32_t lanes = to + ((uint32_t)(16 * i) << 16);
+          const uint32_t lanes = mine + 48 * u + ((uint32_t)(16 * i) << 16);
           tmem_store_16x8(lanes, hi[i]);
           tmem_store_16x8(lanes + 8, mid[i]);
           tmem_store_16x8(lanes + 16, low[i]);
         }
         tmem_wait_stores();
         tmem_fence_before();
-        warp_arrive(sm.w_full[half], lane);
+        warp_arrive(sm.w_full[u], lane);
       }
       if (!ok) break;
       warp_arrive(sm.weights_empty[c & 1], lane);
@@ -721,8 +724,8 @@ __device__ __forceinline__ void scan_values(ScanShared &sm, const ScanArgs &a, c
 
 // ---- warps 24 - 27: the state.  A thread has value channel 32 w + lane ----
 template <bool OUT>
-__device__ __forceinline__ void scan_state(ScanShared &sm, const ScanArgs &a, const ScanPlan &plan, uint32_t tmem, int w, int lane) {
-  const uint32_t mine = tmem + ((uint32_t)(32 * w) << 16) + TM_DS;
+__device__ __forceinline__ void scan_state(ScanShared &sm, const ScanArgs &a, const ScanPlan &plan, int w, int lane) {
+  const uint32_t mine = ((uint32_t)(32 * w) << 16) + TM_DS;
   const int channel = 32 * w + lane;
   uint8_t *s16 = sm.s16 + channel * 128;
   ScanItem it;
@@ -836,11 +839,11 @@ __global__ void __launch_bounds__(SCAN_THREADS, 1) scan_blocks_kernel(const __gr
       init(sm.k_full[i], 1), init(sm.k_empty[i], OUT ? 2 : 1), init(sm.q_full[i], 1), init(sm.q_empty[i], 1);
       init(sm.v_full[i], 1), init(sm.v_empty[i], OUT ? 10 : 1);
       init(sm.weights_full[i], 1), init(sm.weights_empty[i], OUT ? 16 : 12);
-      init(sm.w_full[i], 4), init(sm.w_empty[i], 1);
+      init(sm.w_full[i], 8), init(sm.w_empty[i], 1);
       init(sm.clean[i], 8), init(sm.drained[i], 1);
     }
     for (uint64_t *b : {&sm.sums_full, &sm.p_full, &sm.o1_full, &sm.o_full, &sm.ds_full}) init(*b, 1);
-    for (uint64_t *b : {&sm.p_free, &sm.pw_full, &sm.ds_free, &sm.s_full}) init(*b, 4);
+    for (uint64_t *b : {&sm.pw_full, &sm.ds_free, &sm.s_full}) init(*b, 4);
     init(sm.o_free, 8);
     init(sm.sums_empty, 12);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -849,36 +852,41 @@ __global__ void __launch_bounds__(SCAN_THREADS, 1) scan_blocks_kernel(const __gr
   tmem_fence_before();
   __syncthreads();
   tmem_fence_after();
-  const uint32_t tmem = sm.tmem;
-  // 896 threads start with 72 registers each, 64512 in all: dealt out anew, 128 * (56 + 72 + 168) + 256 * (64 + 40)
+  if (sm.tmem != 0) {                          // (all of tensor memory is this CTA's, so its columns start at 0: the addresses are constants)
+    if (threadIdx.x == 0) atomicOr(&g_ops_error, 2);
+    __syncthreads();
+    if (warp == 3) tmem_free(sm.tmem, 512);
+    return;
+  }
+  // 896 threads start with 72 registers each, 64512 in all: dealt out anew, 128 * (56 + 72 + 168) + 256 * (48 + 56)
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     if (warp == 0) {
       if (lane == 0) scan_copies<OUT>(sm, maps, a, plan);
     } else if (warp == 1) {
-      if (OUT) scan_products(sm, a, plan, tmem);
+      if (OUT) scan_products(sm, a, plan);
     } else if (warp == 2) {
       scan_gate_warp<OUT, G, SELECT>(sm, a, plan, lane);
     } else {
-      scan_state_product<OUT>(sm, a, plan, tmem);
+      scan_state_product<OUT>(sm, a, plan);
     }
   } else if (warp < 8) {
-    if (OUT) scan_weights(sm, a, plan, tmem, warp - 4, lane);
+    if (OUT) scan_weights(sm, a, plan, warp - 4, lane);
   } else if (warp < 16) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-    if (OUT) scan_outputs(sm, a, plan, tmem, warp - 8, lane);
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+    if (OUT) scan_outputs(sm, a, plan, warp - 8, lane);
   } else if (warp < 24) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
-    scan_values<OUT>(sm, a, plan, tmem, warp - 16, lane);
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    scan_values<OUT>(sm, a, plan, warp - 16, lane);
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
-    scan_state<OUT>(sm, a, plan, tmem, warp - 24, lane);
+    scan_state<OUT>(sm, a, plan, warp - 24, lane);
   }
   __syncwarp();
   tmem_fence_before();
   __syncthreads();
   tmem_fence_after();
-  if (warp == 3) tmem_free(tmem, 512);
+  if (warp == 3) tmem_free(0, 512);
 }
 
 // From every piece's own sum (in the place of the state in front of the next piece) to the states in front of the pieces.
