@@ -394,13 +394,15 @@ lq_status lq_norm_rotate(const lq_norm *shape, const void *q, int64_t q_stride, 
  *   q, k : bf16 [tokens][Hqk][d_k]    v : bf16 [tokens][Hv][d_v]      strided rows, 16-byte aligned, strides multiples of 8 (o too)
  *   beta, alpha : [tokens][Hv] of gate_type, strided rows; alpha in [0, 1]
  *   A, dt_bias, skip : fp32 [Hv]; dt_bias and skip may be null (0); A is needed with `select` only, and is not positive
- *   S : fp32 [n_slots][Hv][d_k][d_v], in and out - what lq_quantize_state takes
+ *   S : fp32 [n_slots][Hv][d_k][d_v], written - what lq_quantize_state takes - and, where S0 is null, what resumed sequences start from
+ *   S0 : fp32, as S, read only: resumed sequences start from here and S0 stays as it is (a kept prefix that several continuations share);
+ *       null: from S.  S itself, or without an element in common with it.
  * lq_scan_prompt: o is bf16.  The outputs are rounded to bf16 once; in front of that the state and the weighted scores of a
  * block of tokens are rounded to bf16 where they enter a product, as the inputs are; S is held and updated in binary32.
  * A NaN or an infinity in a row makes o undefined from the first row of its block (128 rows from the sequence's first on) to
  * the end of its sequence, and S of that sequence; other sequences never see it.
- * lq_scan_step: one row per sequence (tokens = seqs), every slot is resumed, o is fp32 [seqs][Hv][d_v] in strided rows.
- * A sequence without rows leaves its slot as it is if it is resumed, and empties it (zeros) if it is not.
+ * lq_scan_step: one row per sequence (tokens = seqs), every sequence is resumed, o is fp32 [seqs][Hv][d_v] in strided rows.
+ * A sequence without rows has the state it starts from in its slot afterwards: what it is resumed from, or zeros.
  * Neither may have S, o and the inputs overlap.
  *
  * `work`: lq_scan_prompt_bytes(shape) bytes of device memory, 16-byte aligned, for the states between the pieces that long prompts are
@@ -422,6 +424,7 @@ typedef struct {
   const void *beta, *alpha;
   int64_t beta_stride, alpha_stride;
   const float *A, *dt_bias, *skip;
+  const float *S0;
   float *S;
   const int32_t *seq_start, *slots, *resume;   /* lq_scan_step: seq_start and resume are not looked at */
 } lq_scan_io;

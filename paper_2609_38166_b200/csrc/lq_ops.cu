@@ -139,7 +139,7 @@ static lq_status check_scan(const lq_scan *s, bool step) {
 static lq_status check_scan_io(const lq_scan *s, const lq_scan_io *io, const void *o, int64_t o_stride, bool step) {
   lq_status rc;
   if (!io) return LQ_ERR_NULL;
-  if ((rc = check_arrays(16, {io->S})) != LQ_OK) return rc;
+  if ((rc = check_arrays(16, {io->S}, {io->S0})) != LQ_OK) return rc;
   if (!step && !io->seq_start) return LQ_ERR_NULL;
   if ((rc = check_arrays(4, {}, {io->A, io->dt_bias, io->skip, io->seq_start, io->slots, io->resume})) != LQ_OK) return rc;
   if (s->tokens == 0) return LQ_OK;
@@ -156,7 +156,7 @@ static lq_status check_scan_io(const lq_scan *s, const lq_scan_io *io, const voi
 static ScanArgs scan_args(const lq_scan *s, const lq_scan_io *io, void *o, int64_t o_stride) {
   auto bf = [](const uint16_t *p) { return reinterpret_cast<const __nv_bfloat16 *>(p); };
   return {bf(io->q), bf(io->k), bf(io->v), io->q_stride, io->k_stride, io->v_stride, io->beta_stride, io->alpha_stride, o_stride, io->beta, io->alpha,
-          io->A, io->dt_bias, io->skip, io->S, o, {io->seq_start, io->slots, io->resume, s->tokens, s->seqs, s->n_slots}, s->heads_v,
+          io->A, io->dt_bias, io->skip, io->S0 ? io->S0 : io->S, io->S, o, {io->seq_start, io->slots, io->resume, s->tokens, s->seqs, s->n_slots}, s->heads_v,
           s->heads_qk, s->max_len < s->tokens ? s->max_len : s->tokens, s->select, s->gate_type == LQ_F32};
 }
 

@@ -12,6 +12,7 @@ struct ScanArgs {
   int64_t q_stride, k_stride, v_stride, beta_stride, alpha_stride, o_stride;
   const void *beta, *alpha;
   const float *A, *dt_bias, *skip;
+  const float *S0;                             // where resumed sequences start from; S, or another array of the same slots
   float *S;
   void *o;
   Sequences sq;
@@ -100,13 +101,13 @@ __global__ void __launch_bounds__(256) scan_step_kernel(const ScanArgs a) {
   const int n = blockIdx.x / a.heads_v, h = blockIdx.x - n * a.heads_v;
   const int slot = a.sq.slot(n), warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   if (slot < 0) return;
-  float *S = a.S + ((size_t)slot * a.heads_v + h) * (SD * SD);
+  const size_t at = ((size_t)slot * a.heads_v + h) * (SD * SD);
   ScanState st;
-  st.load(S, warp, lane);
+  st.load(a.S0 + at, warp, lane);
   const float alpha = scan_fetch(a, t, n, h);
   __syncthreads();
   const float4 o = st.token(alpha, t.bk + 16 * warp, t.q + 16 * warp, *reinterpret_cast<const float4 *>(t.v + 4 * lane));
-  st.store(S, warp, lane);
+  st.store(a.S + at, warp, lane);
   scan_emit<float>(a, t, o, n, h);
 }
 
@@ -734,11 +735,12 @@ __device__ __forceinline__ void scan_state(ScanShared &sm, const ScanArgs &a, co
   for (int item = blockIdx.x; ok && item < plan.items; item += gridDim.x) {
     if (!it.get<OUT>(a, plan, item)) continue;
     const size_t at = ((size_t)it.n * plan.pieces + it.part) * a.heads_v + it.h;
-    float *slot = a.S + ((size_t)it.slot * a.heads_v + it.h) * (SD * SD) + channel;
+    const size_t slot = ((size_t)it.slot * a.heads_v + it.h) * (SD * SD) + channel;
+    const bool keep = it.state && it.blocks == 0 && a.S0 == a.S;   // no rows: the state is where it belongs
     float S[SD];
 #pragma unroll
     for (int j = 0; j < SD; j++) S[j] = 0.0f;
-    if (it.state && it.blocks > 0) load_state(S, plan.pieces > 1 ? plan.states + at * (SD * SD) + channel : slot);
+    if (it.state && !keep) load_state(S, plan.pieces > 1 ? plan.states + at * (SD * SD) + channel : a.S0 + slot);
     float decay = 1.0f;
     for (int b = 0; b < it.blocks; b++, c++) {
       if (OUT && (it.state || b > 0)) {
@@ -773,7 +775,7 @@ __device__ __forceinline__ void scan_state(ScanShared &sm, const ScanArgs &a, co
     }
     if (!ok) break;
     if (OUT) {
-      if (it.last && (it.blocks > 0 || !it.state)) store_state(S, slot);
+      if (it.last && !keep) store_state(S, a.S + slot);
     } else {
       store_state(S, plan.states + (at + a.heads_v) * (SD * SD) + channel);
       if (channel == 0) plan.decays[at] = decay;
@@ -896,7 +898,7 @@ __global__ void __launch_bounds__(256) scan_join_kernel(const ScanArgs a, const 
   if (slot < 0) return;
   const size_t e = (size_t)(blockIdx.x % 16) * 1024 + threadIdx.x * 4;
   float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  if (a.sq.resumed(n)) x = *reinterpret_cast<const float4 *>(a.S + ((size_t)slot * a.heads_v + h) * (SD * SD) + e);
+  if (a.sq.resumed(n)) x = *reinterpret_cast<const float4 *>(a.S0 + ((size_t)slot * a.heads_v + h) * (SD * SD) + e);
   for (int p = 0;; p++) {
     const size_t at = ((size_t)n * plan.pieces + p) * a.heads_v + h;
     *reinterpret_cast<float4 *>(plan.states + at * (SD * SD) + e) = x;

@@ -412,7 +412,7 @@ class _Scan(C.Structure):
 class _ScanIo(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("q", "k", "v")] + [(n, C.c_int64) for n in ("q_stride", "k_stride", "v_stride")] + \
                [(n, C.c_void_p) for n in ("beta", "alpha")] + [(n, C.c_int64) for n in ("beta_stride", "alpha_stride")] + \
-               [(n, C.c_void_p) for n in ("A", "dt_bias", "skip", "S", "seq_start", "slots", "resume")]
+               [(n, C.c_void_p) for n in ("A", "dt_bias", "skip", "S0", "S", "seq_start", "slots", "resume")]
 
 
 @dataclass
@@ -534,7 +534,7 @@ def norm_rotate(sh: NormShape, q, k, out_q, out_k, w_q=None, w_k=None, positions
         _check(rc, "lq_norm_rotate")
 
 
-def _scan_io(sh: ScanShape, q, k, v, beta, alpha, S, seq_start, slots, resume, A, dt_bias, skip) -> _ScanIo:
+def _scan_io(sh: ScanShape, q, k, v, beta, alpha, S0, S, seq_start, slots, resume, A, dt_bias, skip) -> _ScanIo:
     bf, f32, i32, gate, H = torch.bfloat16, torch.float32, torch.int32, _DTYPES.get(sh.gate_type), sh.heads_v
     pq, sq = _rows(q, "q", bf, sh.tokens, sh.heads_qk, sh.d_k)
     pk, sk = _rows(k, "k", bf, sh.tokens, sh.heads_qk, sh.d_k)
@@ -542,7 +542,7 @@ def _scan_io(sh: ScanShape, q, k, v, beta, alpha, S, seq_start, slots, resume, A
     pb, sb = _rows(beta, "beta", gate, sh.tokens, H)
     pa, sa = (None, 0) if alpha is None else _rows(alpha, "alpha", gate, sh.tokens, H)
     return _ScanIo(pq, pk, pv, sq, sk, sv, pb, pa, sb, sa, _dense(A, "A", f32, H), _dense(dt_bias, "dt_bias", f32, H), _dense(skip, "skip", f32, H),
-                   _dense(S, "S", f32, sh.n_slots, H, sh.d_k, sh.d_v), _dense(seq_start, "seq_start", i32, sh.seqs + 1),
+                   _dense(S0, "S0", f32, sh.n_slots, H, sh.d_k, sh.d_v), _dense(S, "S", f32, sh.n_slots, H, sh.d_k, sh.d_v), _dense(seq_start, "seq_start", i32, sh.seqs + 1),
                    _dense(slots, "slots", i32, sh.seqs), _dense(resume, "resume", i32, sh.seqs))
 
 
@@ -551,12 +551,12 @@ def scan_prompt_bytes(sh: ScanShape) -> int:
     return int(lib().lq_scan_prompt_bytes(sh.ref()))
 
 
-def scan_prompt(sh: ScanShape, q, k, v, beta, alpha, o, S, seq_start, slots=None, resume=None, A=None, dt_bias=None, skip=None, work=None,
-                stream=None) -> None:
+def scan_prompt(sh: ScanShape, q, k, v, beta, alpha, o, S, seq_start, slots=None, resume=None, A=None, dt_bias=None, skip=None, S0=None,
+                work=None, stream=None) -> None:
     """lq_scan_prompt: ``q``, ``k`` bf16 [tokens, heads_qk, d_k], ``v``, ``o`` bf16 [tokens, heads_v, d_v], ``beta``, ``alpha``
     [tokens, heads_v] (rows of all of them may be strided; with ``sh.select`` beta is dt and alpha None), ``S`` fp32 [n_slots, heads_v,
-    d_k, d_v], ``A``, ``dt_bias``, ``skip`` fp32 [heads_v], ``work`` uint8 [scan_prompt_bytes] (None where that is 0)."""
-    io = _scan_io(sh, q, k, v, beta, alpha, S, seq_start, slots, resume, A, dt_bias, skip)
+    d_k, d_v], ``S0`` the same or None (resumed from S), ``A``, ``dt_bias``, ``skip`` fp32 [heads_v], ``work`` uint8 [scan_prompt_bytes] (None where that is 0)."""
+    io = _scan_io(sh, q, k, v, beta, alpha, S0, S, seq_start, slots, resume, A, dt_bias, skip)
     po, so = _rows(o, "o", torch.bfloat16, sh.tokens, sh.heads_v, sh.d_v)
     if work is not None and work.numel():
         need = scan_prompt_bytes(sh)
@@ -569,9 +569,9 @@ def scan_prompt(sh: ScanShape, q, k, v, beta, alpha, o, S, seq_start, slots=None
         _check(rc, "lq_scan_prompt")
 
 
-def scan_step(sh: ScanShape, q, k, v, beta, alpha, o, S, slots=None, A=None, dt_bias=None, skip=None, stream=None) -> None:
+def scan_step(sh: ScanShape, q, k, v, beta, alpha, o, S, slots=None, A=None, dt_bias=None, skip=None, S0=None, stream=None) -> None:
     """lq_scan_step: one row per sequence, as in ``scan_prompt``; ``o`` is fp32 [seqs, heads_v, d_v]."""
-    io = _scan_io(sh, q, k, v, beta, alpha, S, None, slots, None, A, dt_bias, skip)
+    io = _scan_io(sh, q, k, v, beta, alpha, S0, S, None, slots, None, A, dt_bias, skip)
     po, so = _rows(o, "o", torch.float32, sh.tokens, sh.heads_v, sh.d_v)
     rc = lib().lq_scan_step(sh.ref(), C.byref(io), po, so, _stream(stream))
     if rc:

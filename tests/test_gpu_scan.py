@@ -57,18 +57,20 @@ class Case:
         return lq.ScanShape(self.T, len(self.lens), self.hv, self.hq, max_len=max(self.lens, default=0), n_slots=self.n_slots, select=int(self.select),
                             gate_type=lq.TYPES[self.gates], **kw)
 
-    def prompt(self, sh=None, work=None, stream=None):
+    def prompt(self, sh=None, work=None, stream=None, apart=False):
         sh = sh or self.shape()
         o = torch.full((self.T, self.hv * D + self.pad), FILL, dtype=torch.bfloat16, device="cuda")
         S = self.S.cuda()
+        S0, S = (S, torch.full_like(S, float("nan"))) if apart else (None, S)
         n = lq.scan_prompt_bytes(sh)
         work = torch.full((n,), 255, dtype=torch.uint8, device="cuda") if work is None else work
         i32 = torch.int32
         lq.scan_prompt(sh, self.wide(self.q), self.wide(self.k), self.wide(self.v), self.dev(self.beta), self.dev(self.alpha),
                        o[:, :self.hv * D].unflatten(-1, (self.hv, D)), S, self.dev(self.starts, i32), slots=self.dev(self.slots, i32),
-                       resume=self.dev(self.resume, i32), A=self.dev(self.A), dt_bias=self.dev(self.dt_bias), skip=self.dev(self.skip), work=work, stream=stream)
+                       resume=self.dev(self.resume, i32), A=self.dev(self.A), dt_bias=self.dev(self.dt_bias), skip=self.dev(self.skip), S0=S0, work=work, stream=stream)
         torch.cuda.synchronize()
         assert lq.check_device() == 0
+        assert S0 is None or torch.equal(S0.cpu(), self.S)
         assert bool((o[:, self.hv * D:] == FILL).all())
         return o[:, :self.hv * D].unflatten(-1, (self.hv, D)).cpu(), S.cpu()
 
@@ -191,6 +193,14 @@ def test_longer_than_max_len_is_cut():
     want, _ = b.prompt()
     assert torch.equal(o[:60], want[:60]) and torch.equal(o[100:], want[100:])
     assert bool((o[60:100] == FILL).all())
+
+
+@pytest.mark.parametrize("lens", [[100, 0, 300, 0], [1500, 0, 2]])
+def test_resumed_from_a_state_that_stays(lens):
+    a = Case(lens, 2, 1, resume=[1, 1, 0, 0][:len(lens)])
+    o, S = a.prompt()
+    o2, S2 = a.prompt(apart=True)
+    assert torch.equal(o, o2) and torch.equal(S, S2)
 
 
 def test_no_rows_at_all():

@@ -80,7 +80,7 @@ def test_norm_refusals(L):
 def scan(L, sh, o=P << 4, os=None, work=None, step=False, no_io=False, **kw):
     H, G = (sh.heads_v, sh.heads_qk) if sh else (1, 1)
     io = dict(q=P, k=P, v=P, q_stride=G * 128, k_stride=G * 128, v_stride=H * 128, beta=P, alpha=P, beta_stride=H, alpha_stride=H, A=None, dt_bias=None,
-              skip=None, S=P, seq_start=P, slots=None, resume=None)
+              skip=None, S0=None, S=P, seq_start=P, slots=None, resume=None)
     io.update(kw)
     f = L.lq_scan_step if step else L.lq_scan_prompt
     args = [C.byref(sh.c()) if sh else None, None if no_io else C.byref(lq._ScanIo(**io)), o, H * 128 if os is None else os]
@@ -101,7 +101,7 @@ def test_scan_refusals(L, step):
     for kw in (dict(q=None), dict(k=None), dict(v=None), dict(beta=None), dict(alpha=None), dict(S=None), dict(o=None)):
         assert go(sh, **kw) == NULL, kw
     assert go(rep(select=1)) == NULL                                              # A is missing
-    for kw in (dict(q=P + 2), dict(k=P + 8), dict(v=P + 4), dict(S=P + 4), dict(beta=P + 1), dict(alpha=P + 1), dict(A=P + 2), dict(dt_bias=P + 1), dict(skip=P + 2),
+    for kw in (dict(q=P + 2), dict(k=P + 8), dict(v=P + 4), dict(S=P + 4), dict(S0=P + 8), dict(beta=P + 1), dict(alpha=P + 1), dict(A=P + 2), dict(dt_bias=P + 1), dict(skip=P + 2),
                dict(slots=P + 2), dict(o=P + 1), dict(q_stride=260), dict(k_stride=257), dict(v_stride=513)):
         assert go(sh, **kw) == ALIGN, kw
     assert go(rep(gate_type=lq.F32), beta=P + 2) == ALIGN
