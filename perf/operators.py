@@ -332,6 +332,7 @@ def _own(s):
         sh = s["shape"] = _own_shape(lq, s)
         if op == "scan_prompt":
             s["work"] = torch.empty((lq.scan_prompt_bytes(sh),), dtype=torch.uint8, device="cuda")
+            s["S_out"] = torch.empty_like(s["S"])
     if op == "conv_prompt":
         lq.conv_prompt(sh, s["x"], s["w"], s["bias"], s["state"], s["out"], s["seq_start"], slots=s["slots"], resume=s["resume"])
         return {"out": s["out"], "state": s["state"]}
@@ -343,10 +344,10 @@ def _own(s):
         return {"q": s["out_q"], "k": s["out_k"]}
     gates = {"A": s["A"], "dt_bias": s["dt_bias"], "skip": s["skip"]}
     if op == "scan_prompt":
-        lq.scan_prompt(sh, s["q"], s["k"], s["v"], s["beta"], s["alpha"], s["o"], s["S"], s["seq_start"], slots=s["slots"], resume=s["resume"], work=s["work"],
-                       **gates)
-    else:
-        lq.scan_step(sh, s["q"], s["k"], s["v"], s["beta"], s["alpha"], s["o"], s["S"], slots=s["slots"], **gates)
+        lq.scan_prompt(sh, s["q"], s["k"], s["v"], s["beta"], s["alpha"], s["o"], s["S_out"], s["seq_start"], slots=s["slots"], resume=s["resume"], S0=s["S"],
+                       work=s["work"], **gates)
+        return {"o": s["o"], "S": s["S_out"]}
+    lq.scan_step(sh, s["q"], s["k"], s["v"], s["beta"], s["alpha"], s["o"], s["S"], slots=s["slots"], **gates)
     return {"o": s["o"], "S": s["S"]}
 
 
