@@ -1,7 +1,8 @@
 // Short causal depthwise convolution with SiLU: packed prompts and single tokens.
 //
 // out[t][c] = f(bias[c] + sum_i w[c][i] x[t-(width-1)+i][c]): two multiply-adds a tap and one exponential per element, against
-// 2 x 2 bytes of traffic - bound by memory.  A thread owns VEC neighbouring channels (16 bytes) and walks down the rows of its
+// 2 x 2 bytes of traffic - bound by memory.  A thread owns VEC neighbouring channels (four; one where
+// their number, strides or addresses do not divide) and walks down the rows of its
 // tile with the last width-1 rows in registers, so a row is read once per tile (and width-1 rows of the tile before it).
 #pragma once
 #include "lq_rows.cuh"
@@ -18,10 +19,56 @@ struct ConvArgs {
 
 constexpr int CONV_THREADS = 128;
 
+__device__ __forceinline__ float exp2_ftz(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float reciprocal(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// VEC values in binary32, as pairs where VEC is even: sums go two channels at a time.
+template <int VEC>
+struct ConvRow {
+  float x[VEC];
+  template <typename T>
+  __device__ __forceinline__ void unpack(const T (&t)[VEC]) {
+#pragma unroll
+    for (int e = 0; e < VEC; e++) x[e] = to_float(t[e]);
+  }
+  // x + a * b, channel by channel
+  __device__ __forceinline__ void add(const ConvRow &a, const ConvRow &b) {
+    if constexpr (VEC % 2 == 0) {
+#pragma unroll
+      for (int e = 0; e < VEC; e += 2) {
+        const float2 s = __ffma2_rn(make_float2(a.x[e], a.x[e + 1]), make_float2(b.x[e], b.x[e + 1]), make_float2(x[e], x[e + 1]));
+        x[e] = s.x;
+        x[e + 1] = s.y;
+      }
+    } else {
+      x[0] = fmaf(a.x[0], b.x[0], x[0]);
+    }
+  }
+};
+
+template <typename T, int VEC>
+__device__ __forceinline__ void pack(const ConvRow<VEC> &s, T (&y)[VEC]) {
+#pragma unroll
+  for (int e = 0; e < VEC; e++) y[e] = from_float<T>(s.x[e]);
+}
+template <>
+__device__ __forceinline__ void pack<__nv_bfloat16, 4>(const ConvRow<4> &s, __nv_bfloat16 (&y)[4]) {
+  reinterpret_cast<__nv_bfloat162 *>(y)[0] = __floats2bfloat162_rn(s.x[0], s.x[1]);
+  reinterpret_cast<__nv_bfloat162 *>(y)[1] = __floats2bfloat162_rn(s.x[2], s.x[3]);
+}
+
 // The taps of a thread's channels and the sum over them, in binary32.
 template <typename T, int W, int VEC>
 struct ConvTaps {
-  float w[W][VEC], bias[VEC];
+  ConvRow<VEC> w[W], bias;
   int silu;
   __device__ __forceinline__ void load(const ConvArgs &a, int c) {
     const T *src = static_cast<const T *>(a.w) + (size_t)c * W;
@@ -30,28 +77,27 @@ struct ConvTaps {
 #pragma unroll
     for (int e = 0; e < VEC; e++)
 #pragma unroll
-      for (int i = 0; i < W; i++) w[i][e] = to_float(t[e * W + i]);
+      for (int i = 0; i < W; i++) w[i].x[e] = to_float(t[e * W + i]);
 #pragma unroll
-    for (int e = 0; e < VEC; e++) bias[e] = a.bias ? to_float(static_cast<const T *>(a.bias)[c + e]) : 0.0f;
+    for (int e = 0; e < VEC; e++) bias.x[e] = a.bias ? to_float(static_cast<const T *>(a.bias)[c + e]) : 0.0f;
     silu = a.silu;
   }
   // rows[i] is the row that tap i meets
-  __device__ __forceinline__ void apply(const T (&r0)[VEC], const T (*hist)[VEC], T (&y)[VEC]) const {
+  __device__ __forceinline__ void apply(const ConvRow<VEC> *rows, T (&y)[VEC]) const {
+    ConvRow<VEC> s = bias;
 #pragma unroll
-    for (int e = 0; e < VEC; e++) {
-      float s = bias[e];
+    for (int i = 0; i < W; i++) s.add(w[i], rows[i]);
+    if (silu) {                               // y / (1 + exp(-y)): a quotient that overflows is a product with 0
 #pragma unroll
-      for (int i = 0; i < W - 1; i++) s = fmaf(w[i][e], to_float(hist[i][e]), s);
-      s = fmaf(w[W - 1][e], to_float(r0[e]), s);
-      if (silu) s = __fdividef(s, 1.0f + __expf(-s));
-      y[e] = from_float<T>(s);
+      for (int e = 0; e < VEC; e++) s.x[e] *= reciprocal(1.0f + exp2_ftz(s.x[e] * -1.44269504088896340736f));
     }
+    pack(s, y);
   }
 };
 
 template <typename T, int W, int VEC>
 __global__ void __launch_bounds__(CONV_THREADS) conv_prompt_kernel(const ConvArgs a) {
-  constexpr int H = W - 1, U = 8;             // rows of history; rows in flight
+  constexpr int H = W - 1, U = 4;             // rows of history; rows that are asked for while as many are worked on
   constexpr bool WIDE = VEC != 1;
   const Sequences &sq = a.sq;
   const int c = (blockIdx.y * CONV_THREADS + threadIdx.x) * VEC;
@@ -63,10 +109,9 @@ __global__ void __launch_bounds__(CONV_THREADS) conv_prompt_kernel(const ConvArg
     return t > s && t < s + H ? max(t, min(s + H, e)) : t;
   };
   const int t0 = blockIdx.x * a.rows_per_tile, t1 = min(t0 + a.rows_per_tile, sq.tokens);
-  int n = sequence_at(sq, t0);
-  const int n1 = t1 < sq.tokens ? sequence_at(sq, t1) : -1;
-  int t = border(t0, n);
-  const int end = border(t1, n1);
+  const int2 at = sequences_at(sq, t0, t1);
+  int n = at.x, t = border(t0, at.x);
+  const int end = t1 < sq.tokens ? border(t1, at.y) : t1;
   if (c >= a.channels) return;
   ConvTaps<T, W, VEC> taps;
   taps.load(a, c);
@@ -110,27 +155,32 @@ __global__ void __launch_bounds__(CONV_THREADS) conv_prompt_kernel(const ConvArg
         store_row<WIDE>(mine + (size_t)j * a.channels, last);
       }
     }
+    ConvRow<VEC> rows[H + U];
+#pragma unroll
+    for (int i = 0; i < H; i++) rows[i].unpack(hist[i]);
+    alignas(16) T next[U][VEC];
+    const T *in = x + from * a.x_stride;
+    T *to_row = out + from * a.out_stride;
+#pragma unroll
+    for (int i = 0; i < U; i++)
+      if (from + i < to) load_row<WIDE>(in + i * a.x_stride, next[i]);
 #pragma unroll 1
     for (int r = from; r < to; r += U) {
-      alignas(16) T rows[H + U][VEC];
 #pragma unroll
-      for (int i = 0; i < H; i++)
-#pragma unroll
-        for (int v = 0; v < VEC; v++) rows[i][v] = hist[i][v];
+      for (int i = 0; i < U; i++) rows[H + i].unpack(next[i]);
+      in += U * a.x_stride;
 #pragma unroll
       for (int i = 0; i < U; i++)
-        if (r + i < to) load_row<WIDE>(x + (int64_t)(r + i) * a.x_stride, rows[H + i]);
+        if (r + U + i < to) load_row<WIDE>(in + i * a.x_stride, next[i]);
 #pragma unroll
-      for (int i = 0; i < U; i++)
+      for (int i = 0; i < U; i++, to_row += a.out_stride)
         if (r + i < to) {
           alignas(16) T y[VEC];
-          taps.apply(rows[H + i], rows + i, y);
-          store_row<WIDE>(out + (int64_t)(r + i) * a.out_stride, y);
+          taps.apply(rows + i, y);
+          store_row<WIDE>(to_row, y);
         }
 #pragma unroll
-      for (int i = 0; i < H; i++)
-#pragma unroll
-        for (int v = 0; v < VEC; v++) hist[i][v] = rows[U + i][v];
+      for (int i = 0; i < H; i++) rows[i] = rows[U + i];
     }
   }
 }
@@ -151,7 +201,10 @@ __global__ void __launch_bounds__(CONV_THREADS) conv_step_kernel(const ConvArgs 
   load_row<WIDE>(static_cast<const T *>(a.x) + n * a.x_stride + c, rows[H]);
   ConvTaps<T, W, VEC> taps;
   taps.load(a, c);
-  taps.apply(rows[H], rows, y);
+  ConvRow<VEC> x[W];
+#pragma unroll
+  for (int i = 0; i < W; i++) x[i].unpack(rows[i]);
+  taps.apply(x, y);
   store_row<WIDE>(static_cast<T *>(a.out) + n * a.out_stride + c, y);
 #pragma unroll
   for (int i = 0; i < H; i++) store_row<WIDE>(state + (size_t)i * a.channels, rows[i + 1]);

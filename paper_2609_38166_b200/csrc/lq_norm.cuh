@@ -1,9 +1,9 @@
 // Queries and keys normalised per head and rotated by position, in one pass.
 //
 // Every row is read and written once; the arithmetic (one sum of squares per head, four multiply-adds per rotated pair) is far below
-// that - bound by memory.  A lane owns eight neighbouring channels, dim/8 neighbouring lanes a head: the sum of
-// squares is a butterfly over them, and the other half of a rotated pair is one exchange away.  A CTA takes the angles of its rows
-// once for all heads: position * inv_freq in binary64, brought to a fraction of a turn there, so that what binary32 gets
+// that - bound by memory.  A lane owns two 16-byte pieces of a head and neighbouring lanes the rest; the sum of squares is a butterfly over them.
+// Where channels i and i + rot/2 are a pair, a lane's pieces are one of either half, so that its pairs are its own.  A CTA takes the angles of its
+// rows once for all heads: position * inv_freq in binary64, brought to a fraction of a turn there, so that what binary32 gets
 // is below one half whatever the position.
 #pragma once
 #include "lq_rows.cuh"
@@ -18,86 +18,121 @@ struct NormArgs {
   const int32_t *positions;
   int tokens, heads_q, heads_k, rot, pairs, norm, rows_per_cta;
   float eps, scale_q, scale_k;
+  Divisor heads, half;
 };
 
 constexpr int NORM_THREADS = 256;
-constexpr int NORM_MAX_ROWS = 4;              // rows of a CTA
+constexpr int NORM_MAX_ROWS = 8;              // rows of a CTA
+constexpr int NORM_TRIPS = 20;                // heads that a lane has in turn
 
 template <typename T, int DIM, bool WIDE>
 __global__ void __launch_bounds__(NORM_THREADS) norm_rotate_kernel(const NormArgs a) {
-  constexpr int LANES = DIM / 8;              // of a head
-  __shared__ float2 turn[NORM_MAX_ROWS][DIM / 2];
+  constexpr int F = 16 / sizeof(T), LANES = DIM / (2 * F);   // channels of a piece, lanes of a head
+  __shared__ __align__(16) float2 turn[NORM_MAX_ROWS][DIM / 2];
+  __shared__ __align__(16) float weight[2][DIM];
+  constexpr int BATCH = 2;                    // heads that a lane works on while it waits for as many: 64 bytes
   const int row0 = blockIdx.x * a.rows_per_cta, rows = min(a.rows_per_cta, a.tokens - row0);
   const int half = a.rot / 2, heads = a.heads_q + a.heads_k;
+  const int lane = threadIdx.x % LANES;
+  const bool turned = 2 * F * lane < a.rot, apart = turned && !a.pairs;
+  const int c0 = apart ? F * lane : 2 * F * lane, c1 = apart ? half + F * lane : c0 + F;   // where the lane's pieces start
+  const int units = rows * heads;             // heads of all rows
+  constexpr int STEP = NORM_THREADS / LANES;  // heads that the CTA has at a time
+  alignas(16) T next[BATCH][2][F];
+  auto load = [&](int u0) {
+#pragma unroll
+    for (int i = 0; i < BATCH; i++) {
+      const int u = u0 + i * STEP;
+      if (u >= units) continue;
+      const int r = a.heads.quotient(u), h = u - r * heads;
+      const int64_t row = row0 + r;
+      const T *src = h < a.heads_q ? static_cast<const T *>(a.q) + row * a.q_stride + h * DIM
+                                   : static_cast<const T *>(a.k) + row * a.k_stride + (h - a.heads_q) * DIM;
+      load_row<WIDE>(src + c0, next[i][0]);
+      load_row<WIDE>(src + c1, next[i][1]);
+    }
+  };
+  const int mine = threadIdx.x / LANES;
+  load(mine);                                 // (on their way while the angles are worked out)
   if (half > 0) {
     for (int i = threadIdx.x; i < rows * half; i += NORM_THREADS) {
-      const int r = i / half, f = i - r * half;
+      const int r = a.half.quotient(i), f = i - r * half;
       const double turns = (double)a.positions[row0 + r] * (double)a.inv_freq[f] * 0.15915494309189533577;   // / (2 pi)
       float sn, cs;
       sincospif(2.0f * (float)(turns - rint(turns)), &sn, &cs);
       turn[r][f] = make_float2(cs, sn);
     }
-    __syncthreads();
   }
-  const int lane = threadIdx.x % LANES, c = 8 * lane;
-  const int units = rows * heads;             // heads of all rows
+  if (a.norm == LQ_NORM_RMS)
+    for (int i = threadIdx.x; i < 2 * DIM; i += NORM_THREADS) {
+      const float *w = i < DIM ? a.w_q : a.w_k;
+      weight[i / DIM][i % DIM] = w ? w[i % DIM] : 1.0f;
+    }
+  __syncthreads();
 #pragma unroll 1
-  for (int u0 = threadIdx.x / 32 * (32 / LANES); u0 < units; u0 += NORM_THREADS / LANES) {   // (the same trips for all lanes of a warp)
-    const int u = u0 + threadIdx.x % 32 / LANES;
-    const bool there = u < units;
-    const int r = there ? u / heads : 0, h = there ? u - r * heads : 0;
-    const bool is_q = h < a.heads_q;
-    const int64_t row = row0 + r;
-    const T *src = is_q ? static_cast<const T *>(a.q) + row * a.q_stride + h * DIM
-                        : static_cast<const T *>(a.k) + row * a.k_stride + (h - a.heads_q) * DIM;
-    alignas(16) T in[8];
+  for (int u0 = mine; u0 - mine < units; u0 += BATCH * STEP) {   // (the same trips for all lanes of a warp)
+    alignas(16) T in[BATCH][2][F];
 #pragma unroll
-    for (int e = 0; e < 8; e++) in[e] = from_float<T>(0.0f);
-    if (there) load_row<WIDE>(src + c, in);
-    float x[8];
+    for (int i = 0; i < BATCH; i++)
 #pragma unroll
-    for (int e = 0; e < 8; e++) x[e] = to_float(in[e]);
-    float scale = is_q ? a.scale_q : a.scale_k;
-    if (a.norm != LQ_NORM_NONE) {
-      float s = 0.0f;
+      for (int e = 0; e < 2 * F; e++) in[i][e / F][e % F] = next[i][e / F][e % F];
+    load(u0 + BATCH * STEP);
 #pragma unroll
-      for (int e = 0; e < 8; e++) s = fmaf(x[e], x[e], s);
+    for (int i = 0; i < BATCH; i++) {
+      const int u = u0 + i * STEP;
+      if (u - mine >= units) break;
+      const bool there = u < units;
+      const int r = there ? a.heads.quotient(u) : 0, h = there ? u - r * heads : 0;
+      const bool is_q = h < a.heads_q;
+      const int64_t row = row0 + r;
+      float x[2][F];
 #pragma unroll
-      for (int m = 1; m < LANES; m *= 2) s += __shfl_xor_sync(0xffffffffu, s, m);
-      scale *= rsqrtf((a.norm == LQ_NORM_RMS ? s * (1.0f / DIM) : s) + a.eps);
-    }
-    const float *w = is_q ? a.w_q : a.w_k;
+      for (int e = 0; e < 2 * F; e++) x[e / F][e % F] = there ? to_float(in[i][e / F][e % F]) : 0.0f;
+      float scale = is_q ? a.scale_q : a.scale_k;
+      if (a.norm != LQ_NORM_NONE) {
+        float s = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 8; e++) x[e] *= scale * (a.norm == LQ_NORM_RMS && w ? w[c + e] : 1.0f);
-    if (a.pairs) {
-      if (c < a.rot) {
+        for (int e = 0; e < 2 * F; e++) s = fmaf(x[e / F][e % F], x[e / F][e % F], s);
 #pragma unroll
-        for (int e = 0; e < 8; e += 2) {
-          const float2 t = turn[r][(c + e) / 2];
-          const float y0 = x[e], y1 = x[e + 1];
-          x[e] = fmaf(y0, t.x, -(y1 * t.y));
-          x[e + 1] = fmaf(y1, t.x, y0 * t.y);
+        for (int m = 1; m < LANES; m *= 2) s += __shfl_xor_sync(0xffffffffu, s, m);
+        scale *= rsqrtf((a.norm == LQ_NORM_RMS ? s * (1.0f / DIM) : s) + a.eps);
+      }
+      if (a.norm == LQ_NORM_RMS) {
+#pragma unroll
+        for (int e = 0; e < 2 * F; e++) x[e / F][e % F] *= scale * weight[is_q ? 0 : 1][(e < F ? c0 : c1 - F) + e];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 2 * F; e++) x[e / F][e % F] *= scale;
+      }
+      if (turned) {                           // pairs: neighbours in either piece, or the pieces element by element
+        float cs[F], sn[F];
+#pragma unroll
+        for (int p = 0; p < F; p += 2) {
+          const float4 t = *reinterpret_cast<const float4 *>(&turn[r][F * lane + p]);
+          cs[p] = t.x, sn[p] = t.y, cs[p + 1] = t.z, sn[p + 1] = t.w;
+        }
+        auto rotate = [](float &p0, float &p1, float cs, float sn) {
+          const float y0 = p0, y1 = p1;
+          p0 = fmaf(y0, cs, -(y1 * sn));
+          p1 = fmaf(y1, cs, y0 * sn);
+        };
+        if (a.pairs) {
+#pragma unroll
+          for (int p = 0; p < F; p++) rotate(x[2 * p / F][2 * p % F], x[2 * p / F][2 * p % F + 1], cs[p], sn[p]);
+        } else {
+#pragma unroll
+          for (int p = 0; p < F; p++) rotate(x[0][p], x[1][p], cs[p], sn[p]);
         }
       }
-    } else if (half > 0) {                    // the other half of a pair sits half/8 lanes further or back
-      const bool low = c < half;
-      const int other = low ? lane + half / 8 : lane - half / 8;
+      if (there && (!a.positions || a.positions[row] >= 0)) {
+        alignas(16) T y[2][F];
 #pragma unroll
-      for (int e = 0; e < 8; e++) {
-        const float y = __shfl_sync(0xffffffffu, x[e], other & (LANES - 1), LANES);
-        if (c < a.rot) {
-          const float2 t = turn[r][(low ? c : c - half) + e];
-          x[e] = low ? fmaf(x[e], t.x, -(y * t.y)) : fmaf(x[e], t.x, y * t.y);
-        }
+        for (int e = 0; e < 2 * F; e++) y[e / F][e % F] = from_float<T>(x[e / F][e % F]);
+        T *dst = is_q ? static_cast<T *>(a.out_q) + row * a.out_q_stride + h * DIM
+                      : static_cast<T *>(a.out_k) + row * a.out_k_stride + (h - a.heads_q) * DIM;
+        store_row<WIDE>(dst + c0, y[0]);
+        store_row<WIDE>(dst + c1, y[1]);
       }
-    }
-    if (there && (!a.positions || a.positions[row] >= 0)) {
-      alignas(16) T y[8];
-#pragma unroll
-      for (int e = 0; e < 8; e++) y[e] = from_float<T>(x[e]);
-      T *dst = is_q ? static_cast<T *>(a.out_q) + row * a.out_q_stride + h * DIM
-                    : static_cast<T *>(a.out_k) + row * a.out_k_stride + (h - a.heads_q) * DIM;
-      store_row<WIDE>(dst + c, y);
     }
   }
 }

@@ -1,4 +1,5 @@
 // C boundary of the operators around the decode step: argument checks and launches.  Declarations and contracts: include/lq.h.
+#include <algorithm>
 #include <atomic>
 #include <initializer_list>
 
@@ -61,7 +62,7 @@ static lq_status launch_conv_t(const lq_conv *s, ConvArgs a, bool step, cudaStre
   if (step) {
     conv_step_kernel<T, W, VEC><<<dim3(s->seqs, blocks_c), CONV_THREADS, 0, stream>>>(a);
   } else {
-    a.rows_per_tile = 32;
+    a.rows_per_tile = s->tokens * blocks_c >= 64l * 148 * 16 ? 64 : 32;
     conv_prompt_kernel<T, W, VEC><<<dim3(ceil_div(s->tokens, a.rows_per_tile), blocks_c), CONV_THREADS, 0, stream>>>(a);
   }
   return launched();
@@ -69,9 +70,9 @@ static lq_status launch_conv_t(const lq_conv *s, ConvArgs a, bool step, cudaStre
 
 template <typename T>
 static lq_status launch_conv(const lq_conv *s, const ConvArgs &a, bool step, cudaStream_t stream) {
-  constexpr int VEC = 16 / sizeof(T);
-  bool wide = s->channels % VEC == 0 && a.x_stride % VEC == 0 && a.out_stride % VEC == 0;
-  for (const void *p : {a.x, a.w, (const void *)a.state, (const void *)a.out}) wide = wide && aligned(p, 16);
+  constexpr int VEC = 4;
+  bool wide = s->channels % VEC == 0 && a.x_stride % VEC == 0 && a.out_stride % VEC == 0 && aligned(a.w, 16);
+  for (const void *p : {a.x, (const void *)a.state, (const void *)a.out}) wide = wide && aligned(p, VEC * sizeof(T));
 #define LQ_CONV(W) return wide ? launch_conv_t<T, W, VEC>(s, a, step, stream) : launch_conv_t<T, W, 1>(s, a, step, stream)
   if (s->width == 2) LQ_CONV(2);
   if (s->width == 3) LQ_CONV(3);
@@ -105,7 +106,9 @@ static lq_status conv(const lq_conv *s, const void *x, int64_t x_stride, const v
 
 template <typename T, int DIM>
 static lq_status launch_norm_t(const lq_norm *s, NormArgs a, bool wide, cudaStream_t stream) {
-  a.rows_per_cta = 1;
+  // as many rows to a CTA as keep its lanes busy for some trips, and not more than leave two CTAs to an SM
+  const long heads = s->heads_q + s->heads_k, lanes = NORM_THREADS / (DIM * (long)sizeof(T) / 32);
+  a.rows_per_cta = (int)std::max(1l, std::min({(long)NORM_MAX_ROWS, std::max(1l, NORM_TRIPS * lanes / heads), s->tokens / (2 * 148l)}));
   const long grid = ceil_div(s->tokens, a.rows_per_cta);
   if (wide) norm_rotate_kernel<T, DIM, true><<<grid, NORM_THREADS, 0, stream>>>(a);
   else norm_rotate_kernel<T, DIM, false><<<grid, NORM_THREADS, 0, stream>>>(a);
@@ -295,8 +298,10 @@ lq_status lq_norm_rotate(const lq_norm *s, const void *q, int64_t q_stride, cons
   if (s->heads_q && s->heads_k &&
       rows_overlap(out_q, out_q_stride, (long)s->heads_q * s->dim, out_k, out_k_stride, (long)s->heads_k * s->dim, s->tokens, bytes))
     return LQ_ERR_UNSUPPORTED;
-  const NormArgs a{side[0].in, side[1].in, side[0].out, side[1].out, side[0].in_stride, side[1].in_stride, side[0].out_stride, side[1].out_stride,
-                   w_q, w_k, inv_freq, positions, s->tokens, s->heads_q, s->heads_k, s->rot, s->pairs, s->norm, 0, s->eps, s->scale_q, s->scale_k};
+  NormArgs a{side[0].in, side[1].in, side[0].out, side[1].out, side[0].in_stride, side[1].in_stride, side[0].out_stride, side[1].out_stride,
+                   w_q, w_k, inv_freq, positions, s->tokens, s->heads_q, s->heads_k, s->rot, s->pairs, s->norm, 0, s->eps, s->scale_q, s->scale_k, {}, {}};
+  a.heads.set(s->heads_q + s->heads_k);
+  a.half.set(s->rot > 0 ? s->rot / 2 : 1);
   if (s->type == LQ_F32) return launch_norm<float>(s, a, cuda_stream(stream));
   if (s->type == LQ_F16) return launch_norm<__half>(s, a, cuda_stream(stream));
   return launch_norm<__nv_bfloat16>(s, a, cuda_stream(stream));

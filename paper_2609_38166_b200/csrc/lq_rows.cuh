@@ -17,14 +17,17 @@ template <> __device__ __forceinline__ float from_float<float>(float x) { return
 template <> __device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
-// N consecutive elements at `src`; with WIDE in 16-byte pieces (N * sizeof(T) a multiple of 16, src 16-byte aligned).
+// N consecutive elements at `src`; with WIDE in pieces of 16 or 8 bytes, to which src and N * sizeof(T) are aligned.
 template <bool WIDE, typename T, int N>
 __device__ __forceinline__ void load_row(const T *src, T (&x)[N]) {
-  if constexpr (WIDE) {
-    static_assert(N * sizeof(T) % 16 == 0, "");
-    uint4 *d = reinterpret_cast<uint4 *>(x);
+  constexpr int BYTES = N * sizeof(T);
+  if constexpr (WIDE && BYTES % 16 == 0) {
 #pragma unroll
-    for (int i = 0; i < (int)(N * sizeof(T) / 16); i++) d[i] = reinterpret_cast<const uint4 *>(src)[i];
+    for (int i = 0; i < BYTES / 16; i++) reinterpret_cast<uint4 *>(x)[i] = reinterpret_cast<const uint4 *>(src)[i];
+  } else if constexpr (WIDE) {
+    static_assert(BYTES % 8 == 0, "");
+#pragma unroll
+    for (int i = 0; i < BYTES / 8; i++) reinterpret_cast<uint2 *>(x)[i] = reinterpret_cast<const uint2 *>(src)[i];
   } else {
 #pragma unroll
     for (int i = 0; i < N; i++) x[i] = src[i];
@@ -32,15 +35,30 @@ __device__ __forceinline__ void load_row(const T *src, T (&x)[N]) {
 }
 template <bool WIDE, typename T, int N>
 __device__ __forceinline__ void store_row(T *dst, const T (&x)[N]) {
-  if constexpr (WIDE) {
-    const uint4 *s = reinterpret_cast<const uint4 *>(x);
+  constexpr int BYTES = N * sizeof(T);
+  if constexpr (WIDE && BYTES % 16 == 0) {
 #pragma unroll
-    for (int i = 0; i < (int)(N * sizeof(T) / 16); i++) reinterpret_cast<uint4 *>(dst)[i] = s[i];
+    for (int i = 0; i < BYTES / 16; i++) reinterpret_cast<uint4 *>(dst)[i] = reinterpret_cast<const uint4 *>(x)[i];
+  } else if constexpr (WIDE) {
+#pragma unroll
+    for (int i = 0; i < BYTES / 8; i++) reinterpret_cast<uint2 *>(dst)[i] = reinterpret_cast<const uint2 *>(x)[i];
   } else {
 #pragma unroll
     for (int i = 0; i < N; i++) dst[i] = x[i];
   }
 }
+
+// Division of numbers below 2^31 by a constant of the call: a multiplication and a shift.
+struct Divisor {
+  uint32_t d, m, shift;
+  void set(uint32_t by) {
+    d = by;
+    shift = 0;
+    while (((uint64_t)1 << shift) < by) shift++;
+    m = (uint32_t)((((uint64_t)1 << (31 + shift)) + by - 1) / by);   // below 2^32
+  }
+  __device__ __forceinline__ uint32_t quotient(uint32_t x) const { return (uint32_t)(((uint64_t)x * m) >> 31) >> shift; }
+};
 
 // The sequences of a packed batch.  What the arrays hold is not checked by the host, so every row number is brought into
 // [0, tokens] and every slot is compared with n_slots here: nothing outside of the arrays is touched whatever they hold.
@@ -57,14 +75,15 @@ struct Sequences {
   __device__ __forceinline__ bool resumed(int n) const { return resume && resume[n] != 0; }
 };
 
-// The last sequence that starts at row t or before it (-1: none), found by all threads of the CTA together.
-__device__ __forceinline__ int sequence_at(const Sequences &sq, int t) {
-  int n = 0;
+// The last sequences that start at row t or before it and at row u or before it (-1: none), found by all threads of the CTA together.
+__device__ __forceinline__ int2 sequences_at(const Sequences &sq, int t, int u) {
+  int2 n = make_int2(-1, -1);
   for (int i = 0; i <= sq.seqs; i += blockDim.x) {
-    const int at = i + threadIdx.x;
-    n += __syncthreads_count(at <= sq.seqs && sq.first(at) <= t);
+    const int at = i + threadIdx.x, first = at <= sq.seqs ? sq.first(at) : INT32_MAX;
+    n.x += __syncthreads_count(first <= t);
+    n.y += __syncthreads_count(first <= u);
   }
-  return n - 1;
+  return n;
 }
 
 }  // namespace lq

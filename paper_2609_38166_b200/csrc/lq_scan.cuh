@@ -144,17 +144,6 @@ __global__ void __launch_bounds__(256) scan_step_kernel(const ScanArgs a) {
 struct ScanMaps {
   CUtensorMap q, k, v;
 };
-// Division of numbers below 2^31 by a constant of the call: a multiplication and a shift.
-struct Divisor {
-  uint32_t d, m, shift;
-  void set(uint32_t by) {
-    d = by;
-    shift = 0;
-    while (((uint64_t)1 << shift) < by) shift++;
-    m = (uint32_t)((((uint64_t)1 << (31 + shift)) + by - 1) / by);   // below 2^32
-  }
-  __device__ __forceinline__ uint32_t quotient(uint32_t x) const { return (uint32_t)(((uint64_t)x * m) >> 31) >> shift; }
-};
 struct ScanPlan {
   int piece, pieces;            // rows of a piece, pieces of the longest prompt (1: not cut)
   int items;                    // seqs * pieces * heads_v
