@@ -97,7 +97,7 @@ struct ConvTaps {
 
 template <typename T, int W, int VEC>
 __global__ void __launch_bounds__(CONV_THREADS) conv_prompt_kernel(const ConvArgs a) {
-  constexpr int H = W - 1, U = 4;             // rows of history; rows that are asked for while as many are worked on
+  constexpr int H = W - 1, U = 8;             // rows of history; rows on their way while as many are worked on
   constexpr bool WIDE = VEC != 1;
   const Sequences &sq = a.sq;
   const int c = (blockIdx.y * CONV_THREADS + threadIdx.x) * VEC;
@@ -155,32 +155,44 @@ __global__ void __launch_bounds__(CONV_THREADS) conv_prompt_kernel(const ConvArg
         store_row<WIDE>(mine + (size_t)j * a.channels, last);
       }
     }
-    ConvRow<VEC> rows[H + U];
+    ConvRow<VEC> rows[W];                     // the rows that the taps meet, in binary32
 #pragma unroll
-    for (int i = 0; i < H; i++) rows[i].unpack(hist[i]);
+    for (int i = 0; i < H; i++) rows[i + 1].unpack(hist[i]);
     alignas(16) T next[U][VEC];
     const T *in = x + from * a.x_stride;
     T *to_row = out + from * a.out_stride;
+    // the next rows from `first` on; where all of them are there, without a question for each
+    auto load = [&](int first) {
+      if (first + U <= to) {
 #pragma unroll
-    for (int i = 0; i < U; i++)
-      if (from + i < to) load_row<WIDE>(in + i * a.x_stride, next[i]);
+        for (int i = 0; i < U; i++) load_row<WIDE>(in + i * a.x_stride, next[i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < U; i++)
+          if (first + i < to) load_row<WIDE>(in + i * a.x_stride, next[i]);
+      }
+      in += U * a.x_stride;
+    };
+    load(from);
 #pragma unroll 1
     for (int r = from; r < to; r += U) {
-#pragma unroll
-      for (int i = 0; i < U; i++) rows[H + i].unpack(next[i]);
-      in += U * a.x_stride;
+      alignas(16) T now[U][VEC];
 #pragma unroll
       for (int i = 0; i < U; i++)
-        if (r + U + i < to) load_row<WIDE>(in + i * a.x_stride, next[i]);
 #pragma unroll
-      for (int i = 0; i < U; i++, to_row += a.out_stride)
-        if (r + i < to) {
-          alignas(16) T y[VEC];
-          taps.apply(rows + i, y);
-          store_row<WIDE>(to_row, y);
-        }
+        for (int v = 0; v < VEC; v++) now[i][v] = next[i][v];
+      load(r + U);
+      const bool all = r + U <= to;
 #pragma unroll
-      for (int i = 0; i < H; i++) rows[i] = rows[U + i];
+      for (int i = 0; i < U; i++) {
+#pragma unroll
+        for (int k = 0; k < H; k++) rows[k] = rows[k + 1];
+        rows[H].unpack(now[i]);
+        alignas(16) T y[VEC];
+        taps.apply(rows, y);
+        if (all || r + i < to) store_row<WIDE>(to_row + i * a.out_stride, y);
+      }
+      to_row += U * a.out_stride;
     }
   }
 }

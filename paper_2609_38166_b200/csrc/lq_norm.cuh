@@ -3,8 +3,8 @@
 // Every row is read and written once; the arithmetic (one sum of squares per head, four multiply-adds per rotated pair) is far below
 // that - bound by memory.  A lane owns two 16-byte pieces of a head and neighbouring lanes the rest; the sum of squares is a butterfly over them.
 // Where channels i and i + rot/2 are a pair, a lane's pieces are one of either half, so that its pairs are its own.  A CTA takes the angles of its
-// rows once for all heads: position * inv_freq in binary64, brought to a fraction of a turn there, so that what binary32 gets
-// is below one half whatever the position.
+// rows once for all heads: a frequency in turns as a fraction of 64 bits (from binary64), times the position modulo one turn - whole
+// turns drop out exactly, and what binary32 gets is at most half a turn whatever the position.
 #pragma once
 #include "lq_rows.cuh"
 
@@ -22,27 +22,29 @@ struct NormArgs {
 };
 
 constexpr int NORM_THREADS = 256;
-constexpr int NORM_MAX_ROWS = 8;              // rows of a CTA
+constexpr int NORM_MAX_ROWS = 16;             // rows of a CTA
 constexpr int NORM_TRIPS = 20;                // heads that a lane has in turn
 
 template <typename T, int DIM, bool WIDE>
-__global__ void __launch_bounds__(NORM_THREADS) norm_rotate_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(NORM_THREADS, 3) norm_rotate_kernel(const NormArgs a) {
   constexpr int F = 16 / sizeof(T), LANES = DIM / (2 * F);   // channels of a piece, lanes of a head
-  __shared__ __align__(16) float2 turn[NORM_MAX_ROWS][DIM / 2];
-  __shared__ __align__(16) float weight[2][DIM];
-  constexpr int BATCH = 2;                    // heads that a lane works on while it waits for as many: 64 bytes
+  // by lane, 16 bytes at a time: neighbouring lanes read neighbouring pieces
+  __shared__ __align__(16) float2 turn[NORM_MAX_ROWS][F / 2][LANES][2];
+  __shared__ __align__(16) float weight[2][2 * F / 4][LANES][4];
+  __shared__ uint64_t step[DIM / 2];
+  constexpr int BATCH = 1;                    // heads that a lane works on while it waits for as many
   const int row0 = blockIdx.x * a.rows_per_cta, rows = min(a.rows_per_cta, a.tokens - row0);
   const int half = a.rot / 2, heads = a.heads_q + a.heads_k;
   const int lane = threadIdx.x % LANES;
   const bool turned = 2 * F * lane < a.rot, apart = turned && !a.pairs;
   const int c0 = apart ? F * lane : 2 * F * lane, c1 = apart ? half + F * lane : c0 + F;   // where the lane's pieces start
   const int units = rows * heads;             // heads of all rows
-  constexpr int STEP = NORM_THREADS / LANES;  // heads that the CTA has at a time
+  constexpr int SIDE = NORM_THREADS / LANES;  // heads that the CTA has at a time
   alignas(16) T next[BATCH][2][F];
   auto load = [&](int u0) {
 #pragma unroll
     for (int i = 0; i < BATCH; i++) {
-      const int u = u0 + i * STEP;
+      const int u = u0 + i * SIDE;
       if (u >= units) continue;
       const int r = a.heads.quotient(u), h = u - r * heads;
       const int64_t row = row0 + r;
@@ -55,31 +57,38 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_rotate_kernel(const NormArg
   const int mine = threadIdx.x / LANES;
   load(mine);                                 // (on their way while the angles are worked out)
   if (half > 0) {
+    for (int f = threadIdx.x; f < half; f += NORM_THREADS) {
+      const double turns = (double)a.inv_freq[f] * 0.15915494309189533577;   // of a turn a position, / (2 pi)
+      step[f] = (uint64_t)(int64_t)((turns - rint(turns)) * 18446744073709551616.0);   // modulo 1, in units of 2^-64
+    }
+    __syncthreads();
     for (int i = threadIdx.x; i < rows * half; i += NORM_THREADS) {
       const int r = a.half.quotient(i), f = i - r * half;
-      const double turns = (double)a.positions[row0 + r] * (double)a.inv_freq[f] * 0.15915494309189533577;   // / (2 pi)
+      const int32_t phase = (int32_t)((step[f] * (uint64_t)(int64_t)a.positions[row0 + r]) >> 32);
       float sn, cs;
-      sincospif(2.0f * (float)(turns - rint(turns)), &sn, &cs);
-      turn[r][f] = make_float2(cs, sn);
+      sincospif((float)phase * 4.656612873077392578125e-10f, &sn, &cs);   // 2^-31: in half turns
+      turn[r][f % F / 2][f / F][f % 2] = make_float2(cs, sn);
     }
   }
   if (a.norm == LQ_NORM_RMS)
     for (int i = threadIdx.x; i < 2 * DIM; i += NORM_THREADS) {
       const float *w = i < DIM ? a.w_q : a.w_k;
-      weight[i / DIM][i % DIM] = w ? w[i % DIM] : 1.0f;
+      const int l = i % DIM / (2 * F), e = i % (2 * F);
+      const int channel = 2 * F * l < a.rot && !a.pairs ? (e < F ? 0 : half - F) + F * l + e : 2 * F * l + e;
+      weight[i / DIM][e / 4][l][e % 4] = w ? w[channel] : 1.0f;
     }
   __syncthreads();
 #pragma unroll 1
-  for (int u0 = mine; u0 - mine < units; u0 += BATCH * STEP) {   // (the same trips for all lanes of a warp)
+  for (int u0 = mine; u0 - mine < units; u0 += BATCH * SIDE) {   // (the same trips for all lanes of a warp)
     alignas(16) T in[BATCH][2][F];
 #pragma unroll
     for (int i = 0; i < BATCH; i++)
 #pragma unroll
       for (int e = 0; e < 2 * F; e++) in[i][e / F][e % F] = next[i][e / F][e % F];
-    load(u0 + BATCH * STEP);
+    load(u0 + BATCH * SIDE);
 #pragma unroll
     for (int i = 0; i < BATCH; i++) {
-      const int u = u0 + i * STEP;
+      const int u = u0 + i * SIDE;
       if (u - mine >= units) break;
       const bool there = u < units;
       const int r = there ? a.heads.quotient(u) : 0, h = there ? u - r * heads : 0;
@@ -99,7 +108,13 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_rotate_kernel(const NormArg
       }
       if (a.norm == LQ_NORM_RMS) {
 #pragma unroll
-        for (int e = 0; e < 2 * F; e++) x[e / F][e % F] *= scale * weight[is_q ? 0 : 1][(e < F ? c0 : c1 - F) + e];
+        for (int e = 0; e < 2 * F; e += 4) {
+          const float4 w = *reinterpret_cast<const float4 *>(weight[is_q ? 0 : 1][e / 4][lane]);
+          x[e / F][e % F] *= scale * w.x;
+          x[e / F][e % F + 1] *= scale * w.y;
+          x[e / F][e % F + 2] *= scale * w.z;
+          x[e / F][e % F + 3] *= scale * w.w;
+        }
       } else {
 #pragma unroll
         for (int e = 0; e < 2 * F; e++) x[e / F][e % F] *= scale;
@@ -108,7 +123,7 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_rotate_kernel(const NormArg
         float cs[F], sn[F];
 #pragma unroll
         for (int p = 0; p < F; p += 2) {
-          const float4 t = *reinterpret_cast<const float4 *>(&turn[r][F * lane + p]);
+          const float4 t = *reinterpret_cast<const float4 *>(turn[r][p / 2][lane]);
           cs[p] = t.x, sn[p] = t.y, cs[p + 1] = t.z, sn[p + 1] = t.w;
         }
         auto rotate = [](float &p0, float &p1, float cs, float sn) {
