@@ -406,7 +406,7 @@ lq_status lq_norm_rotate(const lq_norm *shape, const void *q, int64_t q_stride, 
  * Neither may have S, o and the inputs overlap.
  *
  * `work`: lq_scan_prompt_bytes(shape) bytes of device memory, 16-byte aligned, for the states between the pieces that long prompts are
- * cut into (null if that is 0).  Its contents mean nothing between calls; calls that may run at the same time need one each.
+ * cut into and for handing out the heads (null if that is 0).  Its contents mean nothing between calls; calls that may run at the same time need one each.
  */
 typedef struct {
   int tokens;    /* rows (lq_scan_step: equal to seqs)                                                      */

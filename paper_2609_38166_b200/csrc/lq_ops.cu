@@ -182,13 +182,15 @@ static ScanPlan scan_plan(const lq_scan *s, void *work) {
   plan.heads.set(s->heads_v);
   plan.cuts.set(plan.pieces);
   plan.group.set(s->heads_v / s->heads_qk);
-  plan.states = static_cast<float *>(work);
+  if (plan.items > SMS) plan.next = static_cast<int *>(work);   // more heads than CTAs: whoever is through takes the next
+  plan.states = static_cast<float *>(work) + 4;
   plan.decays = plan.states + (size_t)plan.items * (SD * SD);
   return plan;
 }
 
 static uint64_t scan_bytes(const ScanPlan &plan) {
-  return plan.pieces > 1 ? (uint64_t)plan.items * (SD * SD + 1) * sizeof(float) : 0;
+  if (plan.items <= 148 && plan.pieces == 1) return 0;
+  return 16 + (plan.pieces > 1 ? (uint64_t)plan.items * (SD * SD + 1) * sizeof(float) : 0);
 }
 
 using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
@@ -227,6 +229,10 @@ static lq_status launch_scan_t(const ScanMaps &maps, const ScanArgs &a, const Sc
       return LQ_ERR_CUDA;
     }
     ready.fetch_or(bit, std::memory_order_relaxed);
+  }
+  if (plan.next && cudaMemsetAsync(plan.next, 0, sizeof(int), stream) != cudaSuccess) {
+    cudaGetLastError();
+    return LQ_ERR_CUDA;
   }
   scan_blocks_kernel<OUT, G, SELECT><<<plan.items < 148 ? plan.items : 148, SCAN_THREADS, smem, stream>>>(maps, a, plan);
   return launched();
@@ -315,7 +321,7 @@ lq_status lq_scan_prompt(const lq_scan *s, const lq_scan_io *io, uint16_t *o, in
   if (s->seqs == 0) return LQ_OK;
   if ((rc = check_scan_io(s, io, o, o_stride, false)) != LQ_OK) return rc;
   const ScanPlan plan = scan_plan(s, work);
-  if (plan.pieces > 1 && (rc = check_arrays(16, {work})) != LQ_OK) return rc;
+  if (scan_bytes(plan) > 0 && (rc = check_arrays(16, {work})) != LQ_OK) return rc;
   ScanMaps maps{};
   if (s->tokens > 0 && !(row_map(&maps.q, io->q, s->tokens, s->heads_qk, io->q_stride) && row_map(&maps.k, io->k, s->tokens, s->heads_qk, io->k_stride) &&
                          row_map(&maps.v, io->v, s->tokens, s->heads_v, io->v_stride)))

@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(256) scan_step_kernel(const ScanArgs a) {
 // Six products of 2 * 128^3 operations a block and head are 0.26 us each at what one SM has of the measured peak; the 64 KB of v and o (q and
 // k are shared by the heads of a group and come from L2) take 1.5 us at its share of the bandwidth.  Both bounds are
 // close, so everything runs side by side in one CTA per SM:
-//   warp 0       tensor copies of the tiles of 32 KB, two slots each for K, Q and V
+//   warp 0       takes the next head and tells the others; tensor copies of the tiles of 32 KB, two slots each for K, Q and V
 //   warp 1       the products for the outputs: P, S^T q, weighted P times V
 //   warp 2       the block's gates: log decays, their sums, weights
 //   warp 3       the product for the state, dS^T = (weighted V)^T K
@@ -148,6 +148,7 @@ struct ScanPlan {
   int piece, pieces;            // rows of a piece, pieces of the longest prompt (1: not cut)
   int items;                    // seqs * pieces * heads_v
   Divisor heads, cuts, group;   // division by heads_v, by pieces, by the value heads of a q/k head
+  int *next;                    // how many items have been taken beyond the first of every CTA (null: they are dealt out in turn)
   float *states, *decays;       // [seqs][pieces][heads_v][128][128]: the state in front of a piece; [seqs][pieces][heads_v]
 };
 
@@ -176,7 +177,8 @@ struct ScanShared {                            // (all but 96 bytes of what a CT
   uint8_t s16[TILE];                           // S as bf16: rows of value channels, two halves of 64 key channels
   ScanSums sums;
   ScanWeights weights[2];
-  uint64_t k_full[2], k_empty[2], q_full[2], q_empty[2], v_full[2], v_empty[2], sums_full, sums_empty, weights_full[2], weights_empty[2];
+  int items[2][6];                             // h, slot, row, rows, at, flags
+  uint64_t items_full[2], items_empty[2], k_full[2], k_empty[2], q_full[2], q_empty[2], v_full[2], v_empty[2], sums_full, sums_empty, weights_full[2], weights_empty[2];
   uint64_t w_full[2], w_empty[2], p_full, pw_full, o1_full, o_full, o_free, ds_full, ds_free, s_full, clean[2], drained[2];
   uint32_t tmem;
 };
@@ -198,27 +200,30 @@ __device__ __forceinline__ bool wait_one(const uint64_t &bar, uint32_t parity) {
 // The same of a warp, with one answer for all of its lanes.
 __device__ __forceinline__ bool wait_for(const uint64_t &bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_one(bar, parity)); }
 
-// What a CTA does in one turn of its loop: rows [row, row + rows) of sequence n, head h.
+// What a CTA does in one turn of its loop: rows [row, row + rows) of a sequence, head h.
 struct ScanItem {
-  int n, h, part, slot, row, rows, blocks;
-  bool first, last, state;                     // the prompt's first / last piece; a state in front of it that is not zero
+  int h, slot, row, rows;                      // rows: -1 when there is nothing more to do
+  int at;                                      // in the workspace: (sequence * pieces + piece) * heads_v + h
+  int flags;                                   // 1: a state in front of it that is not zero; 2: the prompt's last piece
+  int blocks;                                  // (of 128 rows)
+
+  __device__ __forceinline__ bool state() const { return flags & 1; }
+  __device__ __forceinline__ bool last() const { return flags & 2; }
+  // false: there is nothing to do
   template <bool OUT>
-  __device__ __forceinline__ bool get(const ScanArgs &a, const ScanPlan &plan, int item) {
-    const int r = plan.heads.quotient(item);
+  __device__ __forceinline__ bool find(const ScanArgs &a, const ScanPlan &plan, int item) {
+    const int r = plan.heads.quotient(item), n = plan.cuts.quotient(r), part = r - n * plan.pieces;
     h = item - r * a.heads_v;
-    n = plan.cuts.quotient(r);
-    part = r - n * plan.pieces;
+    at = item;
     slot = a.sq.slot(n);
     const int start = a.sq.first(n), len = min(max(a.sq.first(n + 1) - start, 0), a.max_len);
     const int from = part * plan.piece;        // (pieces * piece is less than max_len + piece)
     rows = max(min(len - from, plan.piece), 0);
     row = start + from;
-    blocks = (rows + SB - 1) / SB;
-    first = part == 0;
-    last = from + rows >= len;
-    state = OUT && (!first || a.sq.resumed(n));
+    const bool end = from + rows >= len;
+    flags = (OUT && (part > 0 || a.sq.resumed(n)) ? 1 : 0) | (end ? 2 : 0);
     if (slot < 0) return false;
-    return OUT ? rows > 0 || first : rows > 0 && !last;
+    return OUT ? rows > 0 || part == 0 : rows > 0 && !end;
   }
 };
 
@@ -345,7 +350,18 @@ __device__ __forceinline__ void warp_arrive(uint64_t &bar, int lane) {
   if (lane == 0) bar_arrive(shared_addr(&bar));
 }
 
-// ---- warp 0 (one thread): tensor copies ----
+// The CTA's next item; false: a wait ran out.
+__device__ __forceinline__ bool take(ScanShared &sm, ScanItem &it, int &t, int lane) {
+  if (!wait_for(sm.items_full[t & 1], (t >> 1) & 1)) return false;
+  const int *x = sm.items[t & 1];
+  it.h = x[0], it.slot = x[1], it.row = x[2], it.rows = x[3], it.at = x[4], it.flags = x[5];
+  it.blocks = (it.rows + SB - 1) / SB;
+  warp_arrive(sm.items_empty[t & 1], lane);
+  t++;
+  return true;
+}
+
+// ---- warp 0 (one thread): items, tensor copies ----
 template <bool OUT>
 __device__ __forceinline__ void scan_copies(ScanShared &sm, const ScanMaps &maps, const ScanArgs &a, const ScanPlan &plan) {
   ScanItem it;
@@ -364,11 +380,20 @@ __device__ __forceinline__ void scan_copies(ScanShared &sm, const ScanMaps &maps
     count++;
     return true;
   };
-  for (int item = blockIdx.x; ok && item < plan.items; item += gridDim.x) {
-    if (!it.get<OUT>(a, plan, item)) continue;
+  int item = blockIdx.x, behind = 0;
+  for (int t = 0; ok; t++) {
+    bool found = false;
+    for (; item < plan.items && !found; item = behind) {
+      behind = plan.next ? (int)gridDim.x + atomicAdd(plan.next, 1) : item + (int)gridDim.x;   // (needed at the end of this item)
+      found = it.find<OUT>(a, plan, item);
+    }
+    if (t >= 2 && !(ok = wait_one(sm.items_empty[t & 1], ((t >> 1) + 1) & 1))) break;
+    int *x = sm.items[t & 1];
+    x[0] = it.h, x[1] = it.slot, x[2] = it.row, x[3] = found ? it.rows : -1, x[4] = it.at, x[5] = it.flags;
+    bar_arrive(shared_addr(&sm.items_full[t & 1]));
+    if (!found) break;
     const int hq = plan.group.quotient(it.h);
-    for (int b = 0; b < it.blocks; b++, c++) {
-      const int row = it.row + b * SB;
+    for (int row = it.row; row < it.row + it.rows; row += SB, c++) {
       if (OUT && !copy(&maps.q, sm.q, hq, row, sm.q_full, sm.q_empty, asked[1])) break;   // (Q is through first)
       if (!copy(&maps.k, sm.k, hq, row, sm.k_full, sm.k_empty, asked[0])) break;
       if (!copy(&maps.v, sm.v, it.h, row, sm.v_full, sm.v_empty, asked[2])) break;
@@ -412,14 +437,13 @@ __device__ __forceinline__ void multiply_halves(uint32_t d, Operand a, Operand b
 }
 
 // ---- warp 1: the products for the outputs ----
-__device__ __forceinline__ void scan_products(ScanShared &sm, const ScanArgs &a, const ScanPlan &plan) {
+__device__ __forceinline__ void scan_products(ScanShared &sm, int lane) {
   constexpr uint32_t KK = mma_bf16(128, 128, false, false), KN = mma_bf16(128, 128, false, true);
   const Operand S = operand(shared_addr(sm.s16), 16, 1024);
   ScanItem it;
-  int c = 0, ns = 0;                           // blocks, states published so far
+  int t = 0, c = 0, ns = 0;                    // items, blocks, states published so far
   bool ok = true;
-  for (int item = blockIdx.x; ok && item < plan.items; item += gridDim.x) {
-    if (!it.get<true>(a, plan, item)) continue;
+  while (ok && (ok = take(sm, it, t, lane)) && it.rows >= 0) {
     for (int b = 0; b < it.blocks; b++, c++) {
       const int r = c & 1;
       if (!(ok = wait_for(sm.k_full[r], (c >> 1) & 1))) break;
@@ -433,7 +457,7 @@ __device__ __forceinline__ void scan_products(ScanShared &sm, const ScanArgs &a,
         mma_commit(shared_addr(&sm.k_empty[r]));
       }
       __syncwarp();
-      const bool state = it.state || b > 0;
+      const bool state = it.state() || b > 0;
       if (c > 0 && !(ok = wait_for(sm.o_free, (c + 1) & 1))) break;
       if (state) {                             // O = Q S
         if (!(ok = wait_for(sm.s_full, ns++ & 1))) break;
@@ -466,14 +490,12 @@ __device__ __forceinline__ void scan_products(ScanShared &sm, const ScanArgs &a,
 }
 
 // ---- warp 3: the product for the state, dS^T = (weighted V)^T K, the small pieces first ----
-template <bool OUT>
-__device__ __forceinline__ void scan_state_product(ScanShared &sm, const ScanArgs &a, const ScanPlan &plan) {
+__device__ __forceinline__ void scan_state_product(ScanShared &sm, int lane) {
   constexpr uint32_t KN = mma_bf16(128, 128, false, true);
   ScanItem it;
-  int c = 0;
+  int t = 0, c = 0;
   bool ok = true;
-  for (int item = blockIdx.x; ok && item < plan.items; item += gridDim.x) {
-    if (!it.get<OUT>(a, plan, item)) continue;
+  while (ok && (ok = take(sm, it, t, lane)) && it.rows >= 0) {
     for (int b = 0; b < it.blocks; b++, c++) {
       const int r = c & 1;
       if (!(ok = wait_for(sm.k_full[r], (c >> 1) & 1))) break;
@@ -511,14 +533,13 @@ __device__ __forceinline__ void scan_state_product(ScanShared &sm, const ScanArg
 }
 
 // ---- warps 4 - 7: weights on P.  A thread has row i = 32 w + lane ----
-__device__ __forceinline__ void scan_weights(ScanShared &sm, const ScanArgs &a, const ScanPlan &plan, int w, int lane) {
+__device__ __forceinline__ void scan_weights(ScanShared &sm, int w, int lane) {
   const int i = 32 * w + lane;
   const uint32_t mine = ((uint32_t)(32 * w) << 16);
   ScanItem it;
-  int c = 0;
+  int t = 0, c = 0;
   bool ok = true;
-  for (int item = blockIdx.x; ok && item < plan.items; item += gridDim.x) {
-    if (!it.get<true>(a, plan, item)) continue;
+  while (ok && (ok = take(sm, it, t, lane)) && it.rows >= 0) {
     for (int b = 0; b < it.blocks; b++, c++) {
       const ScanWeights &g = sm.weights[c & 1];
       const int rows = min(it.rows - b * SB, SB);
@@ -591,15 +612,14 @@ __device__ __forceinline__ void store_sector(void *to, const uint32_t (&x)[8]) {
 }
 
 // ---- warps 8 - 15: outputs.  A thread has row i = 32 w + lane and columns 64 * half .. 64 * half + 63 ----
-__device__ __forceinline__ void scan_outputs(ScanShared &sm, const ScanArgs &a, const ScanPlan &plan, int warp, int lane) {
+__device__ __forceinline__ void scan_outputs(ScanShared &sm, const ScanArgs &a, int warp, int lane) {
   const int half = warp / 4, w = warp % 4, i = 32 * w + lane;
   const uint32_t mine = ((uint32_t)(32 * w) << 16) + TM_O + 64 * half;
   const bool sectors = reinterpret_cast<uintptr_t>(a.o) % 32 == 0 && a.o_stride % 16 == 0;   // a row's pieces are whole 32-byte sectors
   ScanItem it;
-  int c = 0;
+  int t = 0, c = 0;
   bool ok = true;
-  for (int item = blockIdx.x; ok && item < plan.items; item += gridDim.x) {
-    if (!it.get<true>(a, plan, item)) continue;
+  while (ok && (ok = take(sm, it, t, lane)) && it.rows >= 0) {
     const float skip = a.skip ? a.skip[it.h] : 0.0f;
     __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(a.o) + (int64_t)(it.row + i) * a.o_stride + it.h * SD + 64 * half;
     for (int b = 0; b < it.blocks; b++, c++) {
@@ -651,18 +671,16 @@ __device__ __forceinline__ void scan_outputs(ScanShared &sm, const ScanArgs &a, 
 }
 
 // ---- warps 16 - 23: weighted values.  A warp has value channels 32 w .. 32 w + 31, the warps of a half have every other 16 rows ----
-template <bool OUT>
-__device__ __forceinline__ void scan_values(ScanShared &sm, const ScanArgs &a, const ScanPlan &plan, int warp, int lane) {
+__device__ __forceinline__ void scan_values(ScanShared &sm, int warp, int lane) {
   const int half = warp / 4, w = warp % 4, thread = 32 * warp + lane;
   const uint32_t mine = ((uint32_t)(32 * w) << 16) + TM_W + 24 * half;
   // matrix lane / 8: channels 8 (lane / 8 % 2) of 16, rows 8 (lane / 16) of 16
   const int mrow = 8 * (lane / 16) + lane % 8, chunk = 4 * (w & 1) + (lane / 8) % 2;
   const uint32_t first = (w >> 1) * HALF + half * 2048 + mrow * 128, pick[2] = {(uint32_t)((chunk ^ (lane % 8)) << 4), (uint32_t)(((chunk + 2) ^ (lane % 8)) << 4)};
   ScanItem it;
-  int c = 0;
+  int t = 0, c = 0;
   bool ok = true;
-  for (int item = blockIdx.x; ok && item < plan.items; item += gridDim.x) {
-    if (!it.get<OUT>(a, plan, item)) continue;
+  while (ok && (ok = take(sm, it, t, lane)) && it.rows >= 0) {
     for (int b = 0; b < it.blocks; b++, c++) {
       const int rows = min(it.rows - b * SB, SB);
       uint8_t *V = sm.v[c & 1];
@@ -719,20 +737,19 @@ __device__ __forceinline__ void scan_state(ScanShared &sm, const ScanArgs &a, co
   const int channel = 32 * w + lane;
   uint8_t *s16 = sm.s16 + channel * 128;
   ScanItem it;
-  int c = 0;
+  int t = 0, c = 0;
   bool ok = true;
-  for (int item = blockIdx.x; ok && item < plan.items; item += gridDim.x) {
-    if (!it.get<OUT>(a, plan, item)) continue;
-    const size_t at = ((size_t)it.n * plan.pieces + it.part) * a.heads_v + it.h;
+  while (ok && (ok = take(sm, it, t, lane)) && it.rows >= 0) {
+    const size_t at = it.at;
     const size_t slot = ((size_t)it.slot * a.heads_v + it.h) * (SD * SD) + channel;
-    const bool keep = it.state && it.blocks == 0 && a.S0 == a.S;   // no rows: the state is where it belongs
+    const bool keep = it.state() && it.blocks == 0 && a.S0 == a.S;   // no rows: the state is where it belongs
     float S[SD];
 #pragma unroll
     for (int j = 0; j < SD; j++) S[j] = 0.0f;
-    if (it.state && !keep) load_state(S, plan.pieces > 1 ? plan.states + at * (SD * SD) + channel : a.S0 + slot);
+    if (it.state() && !keep) load_state(S, plan.pieces > 1 ? plan.states + at * (SD * SD) + channel : a.S0 + slot);
     float decay = 1.0f;
     for (int b = 0; b < it.blocks; b++, c++) {
-      if (OUT && (it.state || b > 0)) {
+      if (OUT && (it.state() || b > 0)) {
         // The product that reads the state in front of the last block.  (Waited for only where a state is published: until then the product
         // behind does not run, so this phase cannot be passed twice.)
         if (c > 0 && !(ok = wait_for(sm.o1_full, (c + 1) & 1))) break;
@@ -764,7 +781,7 @@ __device__ __forceinline__ void scan_state(ScanShared &sm, const ScanArgs &a, co
     }
     if (!ok) break;
     if (OUT) {
-      if (it.last && !keep) store_state(S, a.S + slot);
+      if (it.last() && !keep) store_state(S, a.S + slot);
     } else {
       store_state(S, plan.states + (at + a.heads_v) * (SD * SD) + channel);
       if (channel == 0) plan.decays[at] = decay;
@@ -775,28 +792,27 @@ __device__ __forceinline__ void scan_state(ScanShared &sm, const ScanArgs &a, co
 
 // ---- warp 2: gates.  The next block's are loaded before this block's are worked out ----
 template <bool OUT, typename G, bool SELECT>
-__device__ __forceinline__ void scan_gate_warp(ScanShared &sm, const ScanArgs &a, const ScanPlan &plan, int lane) {
+__device__ __forceinline__ void scan_gate_warp(ScanShared &sm, const ScanArgs &a, int lane) {
   ScanItem it;
   RawGates<G, SELECT> next;
-  int item = blockIdx.x, b = 0, c = -1;
-  bool more = false, ok = true;
-  for (;; c++) {
+  int t = 0, b = 0, c = 0;
+  bool more = false, over = false, ok = true;
+  it.blocks = 0;
+  while (more || !over) {
     const RawGates<G, SELECT> now = next;
-    const bool none = !more;
-    more = false;
-    while (item < plan.items) {                // the block that b and item point to, or the first one behind
-      if ((b > 0 || it.get<OUT>(a, plan, item)) && b < it.blocks) {
-        next.load(a, it.row + b * SB, min(it.rows - b * SB, SB), it.h, lane);
-        b++;
-        more = true;
-        break;
-      }
-      item += gridDim.x, b = 0;
+    const bool have = more;
+    // One item ahead at most: the one behind it is not handed out before everybody has taken this one, for which they wait for these gates.
+    if (!over && b >= it.blocks) {
+      if (!(ok = take(sm, it, t, lane))) break;
+      over = it.rows < 0;
+      b = 0;
     }
-    if (none) {
-      if (more) continue;                      // (the first one)
-      break;
+    more = !over && b < it.blocks;
+    if (more) {
+      next.load(a, it.row + b * SB, min(it.rows - b * SB, SB), it.h, lane);
+      b++;
     }
+    if (!have) continue;
     const LaneGates g = scan_gates(a, now, lane);
     if (c >= 2 && !(ok = wait_for(sm.weights_empty[c & 1], ((c >> 1) + 1) & 1))) break;
     ScanWeights &w = sm.weights[c & 1];
@@ -811,6 +827,7 @@ __device__ __forceinline__ void scan_gate_warp(ScanShared &sm, const ScanArgs &a
       reinterpret_cast<float4 *>(sm.sums.beta)[lane] = g.beta;
       warp_arrive(sm.sums_full, lane);
     }
+    c++;
   }
   gave_up(!ok);
 }
@@ -827,6 +844,7 @@ __global__ void __launch_bounds__(SCAN_THREADS, 1) scan_blocks_kernel(const __gr
   if (threadIdx.x == 0) {
     auto init = [](uint64_t &bar, int count) { bar_init(shared_addr(&bar), count); };
     for (int i = 0; i < 2; i++) {              // K is left by two products, V by two products and the eight warps that add the skip
+      init(sm.items_full[i], 1), init(sm.items_empty[i], OUT ? 27 : 14);   // (every warp with a part but the first)
       init(sm.k_full[i], 1), init(sm.k_empty[i], OUT ? 2 : 1), init(sm.q_full[i], 1), init(sm.q_empty[i], 1);
       init(sm.v_full[i], 1), init(sm.v_empty[i], OUT ? 10 : 1);
       init(sm.weights_full[i], 1), init(sm.weights_empty[i], OUT ? 16 : 12);
@@ -855,20 +873,20 @@ __global__ void __launch_bounds__(SCAN_THREADS, 1) scan_blocks_kernel(const __gr
     if (warp == 0) {
       if (lane == 0) scan_copies<OUT>(sm, maps, a, plan);
     } else if (warp == 1) {
-      if (OUT) scan_products(sm, a, plan);
+      if (OUT) scan_products(sm, lane);
     } else if (warp == 2) {
-      scan_gate_warp<OUT, G, SELECT>(sm, a, plan, lane);
+      scan_gate_warp<OUT, G, SELECT>(sm, a, lane);
     } else {
-      scan_state_product<OUT>(sm, a, plan);
+      scan_state_product(sm, lane);
     }
   } else if (warp < 8) {
-    if (OUT) scan_weights(sm, a, plan, warp - 4, lane);
+    if (OUT) scan_weights(sm, warp - 4, lane);
   } else if (warp < 16) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
-    if (OUT) scan_outputs(sm, a, plan, warp - 8, lane);
+    if (OUT) scan_outputs(sm, a, warp - 8, lane);
   } else if (warp < 24) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    scan_values<OUT>(sm, a, plan, warp - 16, lane);
+    scan_values(sm, warp - 16, lane);
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
     scan_state<OUT>(sm, a, plan, warp - 24, lane);

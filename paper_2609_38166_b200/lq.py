@@ -7,7 +7,9 @@ There is no fallback of any kind: if ``liblq.so`` is missing or a call fails, an
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
+import struct
 from dataclasses import dataclass
 from typing import Optional
 
@@ -104,17 +106,32 @@ class _Kept:
         field changes, however it is changed: a decode step is one call per token and layer, and at small batches its
         marshalling took longer than its kernels (10.1 us of host time a call, 2.7 us with the struct kept; comparing the
         fields is 0.2 us of it)."""
-        fields = self.__dict__
         try:
-            of, ref = self._kept
-            if of == fields:
-                return ref
+            of, kept = self._kept
+            if of == self.__dict__:
+                return kept[0]
         except AttributeError:
             pass
-        of, ref = dict(fields), C.byref(self.c())
-        if of == fields:                     # (another thread may be changing a field)
-            self._kept = (of, ref)
-        return ref
+        return self._keep()[0]
+
+    def kept(self):
+        """The same with what the binding wants of the tensors (``wants``)."""
+        try:
+            of, kept = self._kept
+            if of == self.__dict__:
+                return kept
+        except AttributeError:
+            pass
+        return self._keep()
+
+    def _keep(self):
+        of, kept = dict(self.__dict__), (C.byref(self.c()), self.wants())
+        if of == self.__dict__:              # (another thread may be changing a field)
+            self._kept = (of, kept)
+        return kept
+
+    def wants(self):
+        return None
 
     def __getstate__(self):                  # (copies and pickles carry the fields only)
         return self.__dict__
@@ -429,6 +446,10 @@ class ConvShape(_Kept):
     def c(self) -> _Conv:
         return _Conv(self.tokens, self.seqs, self.channels, self.width, self.n_slots, self.silu, self.type)
 
+    def wants(self):
+        return (_DTYPES.get(self.type), (self.tokens, self.channels), (self.channels, self.width), (self.channels,),
+                (self.n_slots, self.width - 1, self.channels), (self.seqs + 1,), (self.seqs,))
+
 
 @dataclass
 class NormShape(_Kept):
@@ -449,6 +470,10 @@ class NormShape(_Kept):
         return _Norm(self.tokens, self.heads_q, self.heads_k, self.dim, self.rot, self.pairs, self.norm, self.type, self.eps, self.scale_q,
                      self.scale_k)
 
+    def wants(self):
+        return (_DTYPES.get(self.type), (self.tokens, self.heads_q, self.dim), (self.tokens, self.heads_k, self.dim), (self.dim,), (self.tokens,),
+                (self.rot // 2,))
+
 
 @dataclass
 class ScanShape(_Kept):
@@ -467,54 +492,66 @@ class ScanShape(_Kept):
     def c(self) -> _Scan:
         return _Scan(self.tokens, self.seqs, self.max_len, self.heads_v, self.heads_qk, self.d_k, self.d_v, self.n_slots, self.select, self.gate_type)
 
+    def wants(self):
+        T, H = self.tokens, self.heads_v
+        return (_DTYPES.get(self.gate_type), (T, self.heads_qk, self.d_k), (T, H, self.d_v), (T, H), (H,), (self.n_slots, H, self.d_k, self.d_v),
+                (self.seqs + 1,), (self.seqs,))
 
-def _need(ok: bool, what: str, t) -> None:
-    if not ok:
-        raise LqError(f"{what}: " + ("missing" if t is None else f"{t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}"))
+
+_SCAN_IO = struct.Struct("=3Q3q2Q2q8Q")        # lq_scan_io, as _ScanIo
+_device = torch._C._cuda_getDevice
 
 
-def _rows(t, what: str, dtype, rows: int, *cols: int):
-    """(address, row stride) of [rows, *cols] of ``dtype`` whose rows are contiguous, on the current device."""
-    if t is None or t.dtype is not dtype or t.get_device() != torch.cuda.current_device() or t.shape != (rows, *cols):
-        _need(False, what, t)
+def _refuse(t, what: str, want) -> None:
+    raise LqError(f"{what}: " + ("missing" if t is None else f"{t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}") +
+                  f", wanted {want} on cuda:{torch.cuda.current_device()}")
+
+
+def _rows(t, what: str, dtype, shape, device: int):
+    """(address, row stride) of a tensor of ``shape``, [rows, ...], and ``dtype`` whose rows are contiguous, on the current device."""
+    if t is None or t.dtype is not dtype or t.shape != shape or t.get_device() != device:
+        _refuse(t, what, (dtype, shape))
+    if t.is_contiguous():
+        return t.data_ptr(), t.stride(0) if shape[0] > 1 else math.prod(shape[1:])
     stride, run = t.stride(), 1
-    for n, s in zip(reversed(cols), reversed(stride)):
-        _need(n == 1 or s == run, what, t)
+    for n, s in zip(shape[:0:-1], stride[:0:-1]):
+        if n != 1 and s != run:
+            _refuse(t, what, (dtype, shape, "contiguous rows"))
         run *= n
-    return t.data_ptr(), stride[0] if rows > 1 else max(stride[0], run)
+    return t.data_ptr(), stride[0] if shape[0] > 1 else max(stride[0], run)
 
 
-def _dense(t, what: str, dtype, *shape: int):
+def _dense(t, what: str, dtype, shape, device: int):
     """Address of a contiguous tensor of that shape on the current device; None stays None."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.get_device() != torch.cuda.current_device() or t.shape != shape or not t.is_contiguous():
-        _need(False, what, t)
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+        _refuse(t, what, (dtype, shape, "contiguous"))
     return t.data_ptr()
 
 
 def conv_prompt(sh: ConvShape, x, w, bias, state, out, seq_start, slots=None, resume=None, stream=None) -> None:
     """lq_conv_prompt: ``x``, ``out`` [tokens, channels] (rows may be strided), ``w`` [channels, width], ``bias`` [channels] or None,
     ``state`` [n_slots, width-1, channels] or None, ``seq_start`` int32 [seqs+1], ``slots``, ``resume`` int32 [seqs] or None."""
-    dt, i32 = _DTYPES.get(sh.type), torch.int32
-    px, sx = _rows(x, "x", dt, sh.tokens, sh.channels)
-    po, so = _rows(out, "out", dt, sh.tokens, sh.channels)
-    rc = lib().lq_conv_prompt(sh.ref(), px, sx, _dense(w, "w", dt, sh.channels, sh.width), _dense(bias, "bias", dt, sh.channels),
-                              _dense(state, "state", dt, sh.n_slots, sh.width - 1, sh.channels), po, so,
-                              _dense(seq_start, "seq_start", i32, sh.seqs + 1), _dense(slots, "slots", i32, sh.seqs),
-                              _dense(resume, "resume", i32, sh.seqs), _stream(stream))
+    ref, (dt, rows, taps, chan, states, starts, seqs) = sh.kept()
+    d, i32 = _device(), torch.int32
+    px, sx = _rows(x, "x", dt, rows, d)
+    po, so = _rows(out, "out", dt, rows, d)
+    rc = (_lib or lib()).lq_conv_prompt(ref, px, sx, _dense(w, "w", dt, taps, d), _dense(bias, "bias", dt, chan, d), _dense(state, "state", dt, states, d), po, so,
+                                        _dense(seq_start, "seq_start", i32, starts, d), _dense(slots, "slots", i32, seqs, d),
+                                        _dense(resume, "resume", i32, seqs, d), _stream(stream))
     if rc:
         _check(rc, "lq_conv_prompt")
 
 
 def conv_step(sh: ConvShape, x, w, bias, state, out, slots=None, stream=None) -> None:
     """lq_conv_step: one row per sequence; ``out`` may be ``x``."""
-    dt = _DTYPES.get(sh.type)
-    px, sx = _rows(x, "x", dt, sh.tokens, sh.channels)
-    po, so = _rows(out, "out", dt, sh.tokens, sh.channels)
-    rc = lib().lq_conv_step(sh.ref(), px, sx, _dense(w, "w", dt, sh.channels, sh.width), _dense(bias, "bias", dt, sh.channels),
-                            _dense(state, "state", dt, sh.n_slots, sh.width - 1, sh.channels), po, so,
-                            _dense(slots, "slots", torch.int32, sh.seqs), _stream(stream))
+    ref, (dt, rows, taps, chan, states, _, seqs) = sh.kept()
+    d = _device()
+    px, sx = _rows(x, "x", dt, rows, d)
+    po, so = (px, sx) if out is x else _rows(out, "out", dt, rows, d)
+    rc = (_lib or lib()).lq_conv_step(ref, px, sx, _dense(w, "w", dt, taps, d), _dense(bias, "bias", dt, chan, d), _dense(state, "state", dt, states, d), po, so,
+                                      _dense(slots, "slots", torch.int32, seqs, d), _stream(stream))
     if rc:
         _check(rc, "lq_conv_step")
 
@@ -522,28 +559,31 @@ def conv_step(sh: ConvShape, x, w, bias, state, out, slots=None, stream=None) ->
 def norm_rotate(sh: NormShape, q, k, out_q, out_k, w_q=None, w_k=None, positions=None, inv_freq=None, stream=None) -> None:
     """lq_norm_rotate: ``q``, ``out_q`` [tokens, heads_q, dim], ``k``, ``out_k`` [tokens, heads_k, dim] (rows may be strided; an output
     may be its input), ``w_q``, ``w_k`` fp32 [dim] or None, ``positions`` int32 [tokens], ``inv_freq`` fp32 [rot/2]."""
-    dt, f32 = _DTYPES.get(sh.type), torch.float32
-    pq, sq = _rows(q, "q", dt, sh.tokens, sh.heads_q, sh.dim) if sh.heads_q else (None, 0)
-    pk, sk = _rows(k, "k", dt, sh.tokens, sh.heads_k, sh.dim) if sh.heads_k else (None, 0)
-    poq, soq = _rows(out_q, "out_q", dt, sh.tokens, sh.heads_q, sh.dim) if sh.heads_q else (None, 0)
-    pok, sok = _rows(out_k, "out_k", dt, sh.tokens, sh.heads_k, sh.dim) if sh.heads_k else (None, 0)
-    rc = lib().lq_norm_rotate(sh.ref(), pq, sq, pk, sk, poq, soq, pok, sok, _dense(w_q, "w_q", f32, sh.dim), _dense(w_k, "w_k", f32, sh.dim),
-                              _dense(positions, "positions", torch.int32, sh.tokens), _dense(inv_freq, "inv_freq", f32, sh.rot // 2),
-                              _stream(stream))
+    ref, (dt, rows_q, rows_k, dim, toks, freqs) = sh.kept()
+    d, f32 = _device(), torch.float32
+    none = (None, 0)
+    pq, sq = _rows(q, "q", dt, rows_q, d) if rows_q[1] else none
+    pk, sk = _rows(k, "k", dt, rows_k, d) if rows_k[1] else none
+    poq, soq = _rows(out_q, "out_q", dt, rows_q, d) if rows_q[1] else none
+    pok, sok = _rows(out_k, "out_k", dt, rows_k, d) if rows_k[1] else none
+    rc = (_lib or lib()).lq_norm_rotate(ref, pq, sq, pk, sk, poq, soq, pok, sok, _dense(w_q, "w_q", f32, dim, d), _dense(w_k, "w_k", f32, dim, d),
+                                        _dense(positions, "positions", torch.int32, toks, d), _dense(inv_freq, "inv_freq", f32, freqs, d), _stream(stream))
     if rc:
         _check(rc, "lq_norm_rotate")
 
 
-def _scan_io(sh: ScanShape, q, k, v, beta, alpha, S0, S, seq_start, slots, resume, A, dt_bias, skip) -> _ScanIo:
-    bf, f32, i32, gate, H = torch.bfloat16, torch.float32, torch.int32, _DTYPES.get(sh.gate_type), sh.heads_v
-    pq, sq = _rows(q, "q", bf, sh.tokens, sh.heads_qk, sh.d_k)
-    pk, sk = _rows(k, "k", bf, sh.tokens, sh.heads_qk, sh.d_k)
-    pv, sv = _rows(v, "v", bf, sh.tokens, H, sh.d_v)
-    pb, sb = _rows(beta, "beta", gate, sh.tokens, H)
-    pa, sa = (None, 0) if alpha is None else _rows(alpha, "alpha", gate, sh.tokens, H)
-    return _ScanIo(pq, pk, pv, sq, sk, sv, pb, pa, sb, sa, _dense(A, "A", f32, H), _dense(dt_bias, "dt_bias", f32, H), _dense(skip, "skip", f32, H),
-                   _dense(S0, "S0", f32, sh.n_slots, H, sh.d_k, sh.d_v), _dense(S, "S", f32, sh.n_slots, H, sh.d_k, sh.d_v), _dense(seq_start, "seq_start", i32, sh.seqs + 1),
-                   _dense(slots, "slots", i32, sh.seqs), _dense(resume, "resume", i32, sh.seqs))
+def _scan_io(want, d: int, q, k, v, beta, alpha, S0, S, seq_start, slots, resume, A, dt_bias, skip) -> bytes:
+    gate, qk, vo, gates, heads, states, starts, seqs = want
+    bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
+    pq, sq = _rows(q, "q", bf, qk, d)
+    pk, sk = _rows(k, "k", bf, qk, d)
+    pv, sv = _rows(v, "v", bf, vo, d)
+    pb, sb = _rows(beta, "beta", gate, gates, d)
+    pa, sa = (0, 0) if alpha is None else _rows(alpha, "alpha", gate, gates, d)
+    return _SCAN_IO.pack(pq, pk, pv, sq, sk, sv, pb, pa, sb, sa, _dense(A, "A", f32, heads, d) or 0, _dense(dt_bias, "dt_bias", f32, heads, d) or 0,
+                         _dense(skip, "skip", f32, heads, d) or 0, _dense(S0, "S0", f32, states, d) or 0, _dense(S, "S", f32, states, d) or 0,
+                         _dense(seq_start, "seq_start", i32, starts, d) or 0, _dense(slots, "slots", i32, seqs, d) or 0,
+                         _dense(resume, "resume", i32, seqs, d) or 0)
 
 
 def scan_prompt_bytes(sh: ScanShape) -> int:
@@ -555,25 +595,30 @@ def scan_prompt(sh: ScanShape, q, k, v, beta, alpha, o, S, seq_start, slots=None
                 work=None, stream=None) -> None:
     """lq_scan_prompt: ``q``, ``k`` bf16 [tokens, heads_qk, d_k], ``v``, ``o`` bf16 [tokens, heads_v, d_v], ``beta``, ``alpha``
     [tokens, heads_v] (rows of all of them may be strided; with ``sh.select`` beta is dt and alpha None), ``S`` fp32 [n_slots, heads_v,
-    d_k, d_v], ``S0`` the same or None (resumed from S), ``A``, ``dt_bias``, ``skip`` fp32 [heads_v], ``work`` uint8 [scan_prompt_bytes] (None where that is 0)."""
-    io = _scan_io(sh, q, k, v, beta, alpha, S0, S, seq_start, slots, resume, A, dt_bias, skip)
-    po, so = _rows(o, "o", torch.bfloat16, sh.tokens, sh.heads_v, sh.d_v)
+    d_k, d_v], ``S0`` the same or None (resumed from S), ``A``, ``dt_bias``, ``skip`` fp32 [heads_v], ``work`` uint8 [scan_prompt_bytes]
+    (None where that is 0)."""
+    ref, want = sh.kept()
+    d = _device()
+    io = _scan_io(want, d, q, k, v, beta, alpha, S0, S, seq_start, slots, resume, A, dt_bias, skip)
+    po, so = _rows(o, "o", torch.bfloat16, want[2], d)
+    pw = None
     if work is not None and work.numel():
         need = scan_prompt_bytes(sh)
-        _need(work.dtype is torch.uint8 and work.is_contiguous() and work.numel() >= need and work.get_device() == torch.cuda.current_device(),
-              f"work of {need} bytes", work)
-    else:
-        work = None
-    rc = lib().lq_scan_prompt(sh.ref(), C.byref(io), po, so, None if work is None else work.data_ptr(), _stream(stream))
+        if work.dtype is not torch.uint8 or not work.is_contiguous() or work.numel() < need or work.get_device() != d:
+            _refuse(work, "work", f"{need} bytes of torch.uint8")
+        pw = work.data_ptr()
+    rc = (_lib or lib()).lq_scan_prompt(ref, io, po, so, pw, _stream(stream))
     if rc:
         _check(rc, "lq_scan_prompt")
 
 
 def scan_step(sh: ScanShape, q, k, v, beta, alpha, o, S, slots=None, A=None, dt_bias=None, skip=None, S0=None, stream=None) -> None:
     """lq_scan_step: one row per sequence, as in ``scan_prompt``; ``o`` is fp32 [seqs, heads_v, d_v]."""
-    io = _scan_io(sh, q, k, v, beta, alpha, S0, S, None, slots, None, A, dt_bias, skip)
-    po, so = _rows(o, "o", torch.float32, sh.tokens, sh.heads_v, sh.d_v)
-    rc = lib().lq_scan_step(sh.ref(), C.byref(io), po, so, _stream(stream))
+    ref, want = sh.kept()
+    d = _device()
+    io = _scan_io(want, d, q, k, v, beta, alpha, S0, S, None, slots, None, A, dt_bias, skip)
+    po, so = _rows(o, "o", torch.float32, want[2], d)
+    rc = (_lib or lib()).lq_scan_step(ref, io, po, so, _stream(stream))
     if rc:
         _check(rc, "lq_scan_step")
 
