@@ -549,41 +549,36 @@ __device__ __forceinline__ void scan_weights(ScanShared &sm, int w, int lane) {
       if (!(ok = wait_for(sm.p_full, c & 1))) break;
       tmem_fence_after();
 #pragma unroll 1
-      for (int col = 0; col <= w; col++) {
-        uint32_t p[32], packed[16];
-        tmem_load32(mine + TM_P + 32 * col, p);
-        tmem_wait_loads(p);
-        if (col < w) {                         // all rows below these columns: exp(G_i - G_end) exp(G_end - G_j), the second at most 1
-          const float f = exp2_fast((whole - g.end_whole[col]) + (frac - g.end_frac[col]));
-          const float2 ff = make_float2(f, f);
-          const float4 *e = reinterpret_cast<const float4 *>(g.e + 32 * col);
+      for (int col = 0; col < 32 * (w + 1); col += 16) {
+        uint32_t p[16], packed[8];
+        tmem_load16(mine + TM_P + col, p);
+        const int group = col / 32;
+        float2 x[8];
+        if (group < w) {                       // all rows below these columns: exp(G_i - G_end) exp(G_end - G_j), the second at most 1
+          const float f = exp2_fast((whole - g.end_whole[group]) + (frac - g.end_frac[group]));
 #pragma unroll
-          for (int j = 0; j < 8; j++) {
-            const float4 x = e[j];
-            const float2 y = __fmul2_rn(ff, __fmul2_rn(make_float2(x.x, x.y), make_float2(__uint_as_float(p[4 * j]), __uint_as_float(p[4 * j + 1]))));
-            const float2 z = __fmul2_rn(ff, __fmul2_rn(make_float2(x.z, x.w), make_float2(__uint_as_float(p[4 * j + 2]), __uint_as_float(p[4 * j + 3]))));
-            packed[2 * j] = pack_bf16(y.x, y.y);
-            packed[2 * j + 1] = pack_bf16(z.x, z.y);
-          }
+          for (int j = 0; j < 8; j++) x[j] = __fmul2_rn(make_float2(f, f), *reinterpret_cast<const float2 *>(g.e + col + 2 * j));
         } else {
-          const int last = min(lane, rows - 1 - 32 * col);   // (columns of rows that are not there: nothing, whatever P holds)
-          const float2 whole2 = make_float2(whole, whole), frac2 = make_float2(frac, frac);
-          const float4 *gw = reinterpret_cast<const float4 *>(sm.sums.minus_whole + 32 * col),
-                       *gf = reinterpret_cast<const float4 *>(sm.sums.minus_frac + 32 * col), *gb = reinterpret_cast<const float4 *>(sm.sums.beta + 32 * col);
+          const int last = min(i, rows - 1) - col;   // (columns of rows that are not there: nothing, whatever P holds)
 #pragma unroll
           for (int j = 0; j < 8; j++) {
-            const float4 x = gw[j], y = gf[j], z = gb[j];
-            auto weighted = [&](float2 xw, float2 xf, float2 beta, int k) {
-              const float2 d = __fadd2_rn(__fadd2_rn(whole2, xw), __fadd2_rn(frac2, xf));
-              const float2 e = __fmul2_rn(__fmul2_rn(beta, make_float2(exp2_fast(d.x), exp2_fast(d.y))),
-                                          make_float2(__uint_as_float(p[4 * j + k]), __uint_as_float(p[4 * j + k + 1])));
-              return pack_bf16(4 * j + k <= last ? e.x : 0.0f, 4 * j + k + 1 <= last ? e.y : 0.0f);
-            };
-            packed[2 * j] = weighted(make_float2(x.x, x.y), make_float2(y.x, y.y), make_float2(z.x, z.y), 0);
-            packed[2 * j + 1] = weighted(make_float2(x.z, x.w), make_float2(y.z, y.w), make_float2(z.z, z.w), 2);
+            const float2 d = __fadd2_rn(__fadd2_rn(make_float2(whole, whole), *reinterpret_cast<const float2 *>(sm.sums.minus_whole + col + 2 * j)),
+                                        __fadd2_rn(make_float2(frac, frac), *reinterpret_cast<const float2 *>(sm.sums.minus_frac + col + 2 * j)));
+            x[j] = __fmul2_rn(*reinterpret_cast<const float2 *>(sm.sums.beta + col + 2 * j), make_float2(exp2_fast(d.x), exp2_fast(d.y)));
           }
+          tmem_wait_loads(p);
+#pragma unroll
+          for (int j = 0; j < 16; j++) p[j] = j <= last ? p[j] : 0;
+#pragma unroll
+          for (int j = 0; j < 8; j++) x[j] = make_float2(2 * j <= last ? x[j].x : 0.0f, 2 * j + 1 <= last ? x[j].y : 0.0f);
         }
-        tmem_store16(mine + TM_P + 16 * col, packed);
+        tmem_wait_loads(p);
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+          const float2 y = __fmul2_rn(x[j], make_float2(__uint_as_float(p[2 * j]), __uint_as_float(p[2 * j + 1])));
+          packed[j] = pack_bf16(y.x, y.y);
+        }
+        tmem_store8(mine + TM_P + col / 2, packed);
       }
 #pragma unroll 1
       for (int col = w + 1; col < 4; col++) {  // above the diagonal there is nothing

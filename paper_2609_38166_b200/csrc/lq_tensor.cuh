@@ -101,6 +101,11 @@ __device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t (&r)[16
       : "memory");
 }
 
+__device__ __forceinline__ void tmem_store8(uint32_t at, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]),
+               "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(at)
+               : "memory");
+}
 // Sixteen lanes by eight columns, from four 8 x 8 matrices of 16-bit pairs as ldmatrix leaves them: lanes 0 - 7 and 8 - 15 by columns 0 - 3, the
 // same by columns 4 - 7
 __device__ __forceinline__ void tmem_store_16x8(uint32_t at, const uint32_t (&r)[4]) {
