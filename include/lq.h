@@ -398,7 +398,8 @@ lq_status lq_norm_rotate(const lq_norm *shape, const void *q, int64_t q_stride, 
  *   S0 : fp32, as S, read only: resumed sequences start from here and S0 stays as it is (a kept prefix that several continuations share);
  *       null: from S.  S itself, or without an element in common with it.
  * lq_scan_prompt: o is bf16.  The outputs are rounded to bf16 once; in front of that the state and the weighted scores of a
- * block of tokens are rounded to bf16 where they enter a product, as the inputs are; S is held and updated in binary32.
+ * block of tokens are rounded to bf16 where they enter a product, as the inputs are; S is held and updated in binary32.  A product of decays
+ * since the start of a block (128 rows) that is below 2^-126 counts as 0 in S, and as 2^-60 where it is below that in the share S^T q of o.
  * A NaN or an infinity in a row makes o undefined from the first row of its block (128 rows from the sequence's first on) to
  * the end of its sequence, and S of that sequence; other sequences never see it.
  * lq_scan_step: one row per sequence (tokens = seqs), every sequence is resumed, o is fp32 [seqs][Hv][d_v] in strided rows.
@@ -434,7 +435,8 @@ lq_status lq_scan_step(const lq_scan *shape, const lq_scan_io *io, float *o, int
 
 /*
  * Device-side error flags of the current device (0 = none), written to *flags (a host pointer).  Waits inside
- * the kernels are bounded; bit 0 is set when a warp gave up waiting for its asynchronous copies.  After
+ * the kernels are bounded; bit 0 is set when a warp gave up waiting for its asynchronous copies (lq_scan_prompt: or products), bit 1 when
+ * lq_scan_prompt did not find its shared or tensor memory where it counts on it (it then did nothing).  After
  * that, neither the outputs of that launch NOR THE STATE it worked on are valid (records may be missing or
  * half written): restore the state from a checkpoint.  Bit 3 belongs to lq_selftest_bounded_wait; the
  * others are not used.

@@ -133,7 +133,8 @@ __global__ void __launch_bounds__(256) scan_step_kernel(const ScanArgs a) {
 // dS does not depend on S, so the only chain from block to block is S's update between two products.
 //
 // Both parts of o_i add up in one accumulator, S^T q_i + sum_j exp(-G_j) beta_j P_ij v_j, and exp(G_i) comes on in the end; where G_i is below
-// -100 (of log2), the accumulator is held at 2^100 o_i instead: S^T q_i then enters with 2^-100 rather than with less, which is nothing next to it.
+// -60 (of log2), the accumulator is held at 2^60 o_i instead (so that it overflows for outputs beyond 2^67 only): S^T q_i then enters with 2^-60
+// rather than with less, 44 bits below what a bf16 output next to it can show.
 //
 // A sum G of log2 decays is held as a whole number and a fraction, added up apart: differences of sums lose nothing however far the
 // sums have come (a decay of 0 counts as 2^-200).
@@ -160,7 +161,7 @@ constexpr uint32_t HALF = TILE / 2;
 // as bf16, takes the place of the first half of P: a thread has all of a row and has read what it overwrites.
 constexpr int TM_P = 0, TM_O = 128, TM_DS = 256, TM_W = 384;
 
-constexpr float LEAST = -100.0f;               // of G in the factor of an output
+constexpr float LEAST = -60.0f;                // of G (log2) in the factor of an output
 
 struct ScanSums {
   float minus_whole[SB], minus_frac[SB];       // -G of every row
@@ -367,9 +368,11 @@ __device__ __forceinline__ void scan_copies(ScanShared &sm, const ScanMaps &maps
   ScanItem it;
   int c = 0, asked[3] = {0, 0, 0};             // blocks; tiles of K, Q, V that have been asked for
   bool ok = true;
-  tensor_map_prefetch(&maps.k);
-  tensor_map_prefetch(&maps.v);
-  if (OUT) tensor_map_prefetch(&maps.q);
+  if (a.sq.tokens > 0) {                       // (without rows there are no maps)
+    tensor_map_prefetch(&maps.k);
+    tensor_map_prefetch(&maps.v);
+    if (OUT) tensor_map_prefetch(&maps.q);
+  }
   auto copy = [&](const CUtensorMap *map, uint8_t (&to)[2][TILE], int head, int row, uint64_t (&full)[2], uint64_t (&empty)[2], int &count) {
     const int r = c & 1;
     if (c >= 2 && !(ok = wait_one(empty[r], ((c >> 1) + 1) & 1))) return false;

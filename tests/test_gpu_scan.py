@@ -151,6 +151,14 @@ def test_signs_and_sizes_of_beta():
     c.check()
 
 
+def test_large_values_behind_strong_decays():
+    """Outputs of 10^9 and more where the decays since the start of a block are far below 2^-60."""
+    c = Case([300], 2, 1, gates=torch.float32, resume=[1], slow=3.0)
+    c.v = (c.v.float() * 2.0 ** 30).bfloat16()
+    c.S = c.S * 2.0 ** 20
+    c.check()
+
+
 def test_long_prompt_few_heads():
     """Cut into pieces along the prompt."""
     Case([2500], 1, 1, resume=[1], slow=0.01, skip=True).check()
