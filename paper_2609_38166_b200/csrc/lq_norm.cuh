@@ -23,7 +23,7 @@ struct NormArgs {
 
 constexpr int NORM_THREADS = 256;
 constexpr int NORM_MAX_ROWS = 16;             // rows of a CTA
-constexpr int NORM_TRIPS = 20;                // heads that a lane has in turn
+constexpr int NORM_TRIPS = 10;                // heads that a lane has in turn (16384 rows of 40 heads: 16 rows to a CTA 76 us, 8 rows 72, 4 rows 74, 1 row 117)
 
 template <typename T, int DIM, bool WIDE>
 __global__ void __launch_bounds__(NORM_THREADS, 3) norm_rotate_kernel(const NormArgs a) {

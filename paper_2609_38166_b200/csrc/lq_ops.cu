@@ -62,7 +62,10 @@ static lq_status launch_conv_t(const lq_conv *s, ConvArgs a, bool step, cudaStre
   if (step) {
     conv_step_kernel<T, W, VEC><<<dim3(s->seqs, blocks_c), CONV_THREADS, 0, stream>>>(a);
   } else {
-    a.rows_per_tile = s->tokens * blocks_c >= 64l * 148 * 16 ? 64 : 32;
+    // The largest tile that leaves three CTAs to an SM (8192 channels: 32768 rows in tiles of 64, 32, 16, 8 take 258, 274, 312, 406 us; 1024 rows
+    // 18.4, 16.4, 18.2, 18.5; 128 rows 14.3, 10.2, 9.0, 8.5).
+    a.rows_per_tile = 64;
+    while (a.rows_per_tile > 8 && ceil_div(s->tokens, a.rows_per_tile) * blocks_c < 3 * 148) a.rows_per_tile /= 2;
     conv_prompt_kernel<T, W, VEC><<<dim3(ceil_div(s->tokens, a.rows_per_tile), blocks_c), CONV_THREADS, 0, stream>>>(a);
   }
   return launched();
@@ -163,34 +166,49 @@ static ScanArgs scan_args(const lq_scan *s, const lq_scan_io *io, void *o, int64
           s->heads_qk, s->max_len < s->tokens ? s->max_len : s->tokens, s->select, s->gate_type == LQ_F32};
 }
 
-// How a call's prompts are cut.  Uncut, a CTA has all blocks of a head, and `heads` of them keep at most that many SMs busy; in p pieces
-// the blocks are gone through twice (the first time for the state alone).
+// How a call's prompts are cut.  Uncut, a CTA has all blocks of a head, and few heads keep few SMs busy; in pieces the blocks are gone through
+// twice, the first time (all pieces but the last) for the state alone, which takes 0.65 of the time, and a piece costs one and a half blocks
+// more.  1 x 16384 rows of 32 heads in 1, 2, 3, 4, 5, 9, 13 pieces: 399, 324, 229, 184, 240, 188, 192 us; 4 x 4096 rows of 32 heads in 1, 2,
+// 4 pieces: 117, 195, 198 us.
+constexpr int SMS = 148, MOST_ORDERED = 4096;   // (what scan_order_kernel has room for)
+
 static ScanPlan scan_plan(const lq_scan *s, void *work) {
-  constexpr int SMS = 148;
   const long max_len = s->max_len < s->tokens ? s->max_len : s->tokens;
-  const long heads = (long)s->seqs * s->heads_v, blocks = ceil_div(max_len, SB);
-  long best = 1;
-  double least = (double)ceil_div(heads, SMS) * blocks;
+  const long heads = (long)s->seqs * s->heads_v, blocks = max_len > 0 ? ceil_div(max_len, SB) : 1;
+  long best = blocks;                          // blocks of a piece
+  double least = (double)ceil_div(heads, SMS) * (blocks + 1.5);
   for (long p = 2; p <= 64 && 2 * p <= blocks; p++) {
-    const double t = (double)ceil_div(heads * p, SMS) * ceil_div(blocks, p) * 1.65 + 4.0;
-    if (t < least) least = t, best = p;
+    const long piece = ceil_div(blocks, p), pieces = ceil_div(blocks, piece);
+    const double t = (piece + 1.5) * (ceil_div(heads * pieces, SMS) + 0.65 * ceil_div(heads * (pieces - 1), SMS)) + 3.0;
+    if (t < least) least = t, best = piece;
   }
   ScanPlan plan{};
-  plan.piece = (int)ceil_div(blocks > 0 ? blocks : 1, best) * SB;
-  plan.pieces = max_len > 0 ? (int)ceil_div(max_len, plan.piece) : 1;
+  plan.piece = (int)best * SB;
+  plan.pieces = (int)ceil_div(blocks, best);
   plan.items = (int)(heads * plan.pieces);
   plan.heads.set(s->heads_v);
   plan.cuts.set(plan.pieces);
   plan.group.set(s->heads_v / s->heads_qk);
-  if (plan.items > SMS) plan.next = static_cast<int *>(work);   // more heads than CTAs: whoever is through takes the next
-  plan.states = static_cast<float *>(work) + 4;
+  // More heads than CTAs: whoever is through takes the next, those of long prompts first where one of them can be more than a quarter of a
+  // CTA's share (12 prompts, the longest with a quarter of 24000 rows: 258 -> 240 us; 64 prompts of up to 216 rows: 103 -> 109, the
+  // additional launch).
+  int *at = static_cast<int *>(work);
+  if (plan.items > SMS) {
+    plan.next = at;
+    at += 4;
+    const long share = (s->tokens / SB * s->heads_v + heads) / SMS;
+    if (s->seqs <= MOST_ORDERED && s->seqs > 1 && 4 * best > share) plan.order = at, at += ceil_div(s->seqs, 4) * 4;
+  }
+  plan.states = reinterpret_cast<float *>(at);
   plan.decays = plan.states + (size_t)plan.items * (SD * SD);
   return plan;
 }
 
-static uint64_t scan_bytes(const ScanPlan &plan) {
-  if (plan.items <= 148 && plan.pieces == 1) return 0;
-  return 16 + (plan.pieces > 1 ? (uint64_t)plan.items * (SD * SD + 1) * sizeof(float) : 0);
+static uint64_t scan_bytes(const lq_scan *s) {
+  char base[16];                               // (an address to measure from)
+  const ScanPlan plan = scan_plan(s, base);
+  const uint64_t front = reinterpret_cast<char *>(plan.states) - base;
+  return front + (plan.pieces > 1 ? (uint64_t)plan.items * (SD * SD + 1) * sizeof(float) : 0);
 }
 
 using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
@@ -230,11 +248,15 @@ static lq_status launch_scan_t(const ScanMaps &maps, const ScanArgs &a, const Sc
     }
     ready.fetch_or(bit, std::memory_order_relaxed);
   }
-  if (plan.next && cudaMemsetAsync(plan.next, 0, sizeof(int), stream) != cudaSuccess) {
+  if (plan.order) {
+    scan_order_kernel<<<1, 1024, 0, stream>>>(a, plan);
+    const lq_status rc = launched();
+    if (rc != LQ_OK) return rc;
+  } else if (plan.next && cudaMemsetAsync(plan.next, 0, sizeof(int), stream) != cudaSuccess) {
     cudaGetLastError();
     return LQ_ERR_CUDA;
   }
-  scan_blocks_kernel<OUT, G, SELECT><<<plan.items < 148 ? plan.items : 148, SCAN_THREADS, smem, stream>>>(maps, a, plan);
+  scan_blocks_kernel<OUT, G, SELECT><<<plan.items < SMS ? plan.items : SMS, SCAN_THREADS, smem, stream>>>(maps, a, plan);
   return launched();
 }
 
@@ -313,7 +335,7 @@ lq_status lq_norm_rotate(const lq_norm *s, const void *q, int64_t q_stride, cons
   return launch_norm<__nv_bfloat16>(s, a, cuda_stream(stream));
 }
 
-uint64_t lq_scan_prompt_bytes(const lq_scan *s) { return check_scan(s, false) == LQ_OK ? scan_bytes(scan_plan(s, nullptr)) : 0; }
+uint64_t lq_scan_prompt_bytes(const lq_scan *s) { return check_scan(s, false) == LQ_OK ? scan_bytes(s) : 0; }
 
 lq_status lq_scan_prompt(const lq_scan *s, const lq_scan_io *io, uint16_t *o, int64_t o_stride, void *work, lq_stream stream) {
   lq_status rc = check_scan(s, false);
@@ -321,7 +343,7 @@ lq_status lq_scan_prompt(const lq_scan *s, const lq_scan_io *io, uint16_t *o, in
   if (s->seqs == 0) return LQ_OK;
   if ((rc = check_scan_io(s, io, o, o_stride, false)) != LQ_OK) return rc;
   const ScanPlan plan = scan_plan(s, work);
-  if (scan_bytes(plan) > 0 && (rc = check_arrays(16, {work})) != LQ_OK) return rc;
+  if (scan_bytes(s) > 0 && (rc = check_arrays(16, {work})) != LQ_OK) return rc;
   ScanMaps maps{};
   if (s->tokens > 0 && !(row_map(&maps.q, io->q, s->tokens, s->heads_qk, io->q_stride) && row_map(&maps.k, io->k, s->tokens, s->heads_qk, io->k_stride) &&
                          row_map(&maps.v, io->v, s->tokens, s->heads_v, io->v_stride)))

@@ -150,6 +150,7 @@ struct ScanPlan {
   int items;                    // seqs * pieces * heads_v
   Divisor heads, cuts, group;   // division by heads_v, by pieces, by the value heads of a q/k head
   int *next;                    // how many items have been taken beyond the first of every CTA (null: they are dealt out in turn)
+  int *order;                   // the sequences by length, the longest first (null: as they come)
   float *states, *decays;       // [seqs][pieces][heads_v][128][128]: the state in front of a piece; [seqs][pieces][heads_v]
 };
 
@@ -213,9 +214,9 @@ struct ScanItem {
   // false: there is nothing to do
   template <bool OUT>
   __device__ __forceinline__ bool find(const ScanArgs &a, const ScanPlan &plan, int item) {
-    const int r = plan.heads.quotient(item), n = plan.cuts.quotient(r), part = r - n * plan.pieces;
+    const int r = plan.heads.quotient(item), m = plan.cuts.quotient(r), n = plan.order ? plan.order[m] : m, part = r - m * plan.pieces;
     h = item - r * a.heads_v;
-    at = item;
+    at = (n * plan.pieces + part) * a.heads_v + h;
     slot = a.sq.slot(n);
     const int start = a.sq.first(n), len = min(max(a.sq.first(n + 1) - start, 0), a.max_len);
     const int from = part * plan.piece;        // (pieces * piece is less than max_len + piece)
@@ -894,6 +895,21 @@ __global__ void __launch_bounds__(SCAN_THREADS, 1) scan_blocks_kernel(const __gr
   __syncthreads();
   tmem_fence_after();
   if (warp == 3) tmem_free(0, 512);
+}
+
+// In front of a pass with more heads than CTAs (one CTA): the count of those taken is 0, and the sequences by length.  A long prompt that is
+// begun last ends long after everything else.
+__global__ void __launch_bounds__(1024) scan_order_kernel(const ScanArgs a, const ScanPlan plan) {
+  if (threadIdx.x == 0) *plan.next = 0;
+  __shared__ int len[4096];
+  for (int n = threadIdx.x; n < a.sq.seqs; n += 1024) len[n] = a.sq.slot(n) < 0 ? -1 : min(max(a.sq.first(n + 1) - a.sq.first(n), 0), a.max_len);
+  __syncthreads();
+  for (int n = threadIdx.x; n < a.sq.seqs; n += 1024) {
+    const int mine = len[n];
+    int before = 0;
+    for (int m = 0; m < a.sq.seqs; m++) before += len[m] > mine || (len[m] == mine && m < n);
+    plan.order[before] = n;
+  }
 }
 
 // From every piece's own sum (in the place of the state in front of the next piece) to the states in front of the pieces.

@@ -151,6 +151,12 @@ def test_signs_and_sizes_of_beta():
     c.check()
 
 
+def test_one_long_prompt_behind_many_short_ones():
+    """More heads than multiprocessors: the long prompt's are handed out first, whatever its place."""
+    lens = [20] * 18 + [1700] + [33, 0]
+    Case(lens, 8, 4, resume=[i % 2 for i in range(len(lens))], slots=list(range(len(lens)))[::-1], skip=True).check()
+
+
 def test_large_values_behind_strong_decays():
     """Outputs of 10^9 and more where the decays since the start of a block are far below 2^-60."""
     c = Case([300], 2, 1, gates=torch.float32, resume=[1], slow=3.0)
