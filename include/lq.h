@@ -323,7 +323,7 @@ lq_status lq_ref_decode_step_bf16(const lq_shape *shape, uint16_t *S, const uint
  *    sequences of a call may share a slot.
  *  - resume (int32 [seqs] in device memory; null: zero): where it is zero the prompt starts from an empty state (what the
  *    slot holds is not read), elsewhere it goes on from what its slot holds.
- *  - Sums are taken in binary32 (of a position's rotation: in binary64), in an order that depends on the shapes alone:
+ *  - Sums are taken in binary32, in an order that depends on the shapes alone:
  *    the same call gives the same bits again.
  */
 typedef enum { LQ_BF16 = 0, LQ_F16 = 1, LQ_F32 = 2 } lq_type;
@@ -366,7 +366,7 @@ lq_status lq_conv_step(const lq_conv *shape, const void *x, int64_t x_stride, co
  *   w_q, w_k : fp32 [dim] or null       positions : int32 [tokens]      inv_freq : fp32 [rot/2] (positions, inv_freq: null if
  *                                                                        rot = 0)
  * A row with a negative position is padding: it is not written.  An output may be its own input (same pointer and stride);
- * no other overlap is allowed.  The angle is taken in binary64, so far positions lose nothing.
+ * no other overlap is allowed.  The angle is taken modulo one turn in 64 bits, so far positions lose nothing.
  * heads_q or heads_k may be zero (its pointers are not looked at then).
  */
 enum { LQ_NORM_NONE = 0, LQ_NORM_L2 = 1, LQ_NORM_RMS = 2 };

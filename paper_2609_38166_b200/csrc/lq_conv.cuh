@@ -16,7 +16,7 @@ struct ConvArgs {
   void *state, *out;
   int64_t x_stride, out_stride;
   Sequences sq;
-  int channels, silu, rows_per_tile;
+  int channels, silu, rows_per_tile, blocks_c;   // blocks_c: CTAs side by side in a row
 };
 
 constexpr int CONV_THREADS = 128;
@@ -36,11 +36,6 @@ __device__ __forceinline__ float reciprocal(float x) {
 template <int VEC>
 struct ConvRow {
   float x[VEC];
-  template <typename T>
-  __device__ __forceinline__ void unpack(const T (&t)[VEC]) {
-#pragma unroll
-    for (int e = 0; e < VEC; e++) x[e] = to_float(t[e]);
-  }
   // x + a * b, channel by channel
   __device__ __forceinline__ void add(const ConvRow &a, const ConvRow &b) {
     if constexpr (VEC % 2 == 0) {
@@ -55,17 +50,6 @@ struct ConvRow {
     }
   }
 };
-
-template <typename T, int VEC>
-__device__ __forceinline__ void pack(const ConvRow<VEC> &s, T (&y)[VEC]) {
-#pragma unroll
-  for (int e = 0; e < VEC; e++) y[e] = from_float<T>(s.x[e]);
-}
-template <>
-__device__ __forceinline__ void pack<__nv_bfloat16, 4>(const ConvRow<4> &s, __nv_bfloat16 (&y)[4]) {
-  reinterpret_cast<__nv_bfloat162 *>(y)[0] = __floats2bfloat162_rn(s.x[0], s.x[1]);
-  reinterpret_cast<__nv_bfloat162 *>(y)[1] = __floats2bfloat162_rn(s.x[2], s.x[3]);
-}
 
 // The taps of a thread's channels and the sum over them, in binary32.
 template <typename T, int W, int VEC>
@@ -93,7 +77,7 @@ struct ConvTaps {
 #pragma unroll
       for (int e = 0; e < VEC; e++) s.x[e] *= reciprocal(1.0f + exp2_ftz(s.x[e] * -1.44269504088896340736f));
     }
-    pack(s, y);
+    pack(s.x, y);
   }
 };
 
@@ -102,7 +86,8 @@ __global__ void __launch_bounds__(CONV_THREADS) conv_prompt_kernel(const ConvArg
   constexpr int H = W - 1, U = 8;             // rows of history; rows on their way while as many are worked on
   constexpr bool WIDE = VEC != 1;
   const Sequences &sq = a.sq;
-  const int c = (blockIdx.y * CONV_THREADS + threadIdx.x) * VEC;
+  // (CTAs that run at the same time have whole rows between them: neighbouring pieces of memory)
+  const int tile = blockIdx.x / a.blocks_c, c = ((blockIdx.x - tile * a.blocks_c) * CONV_THREADS + threadIdx.x) * VEC;
   // A tile whose border falls on one of the first rows of a sequence but its very first leaves these to the tile in front of it: the
   // slot is read and written by the tile that has a sequence's first row, and no other tile looks at it.
   auto border = [&](int t, int n) {
@@ -110,7 +95,7 @@ __global__ void __launch_bounds__(CONV_THREADS) conv_prompt_kernel(const ConvArg
     const int s = sq.first(n), e = sq.first(n + 1);
     return t > s && t < s + H ? max(t, min(s + H, e)) : t;
   };
-  const int t0 = blockIdx.x * a.rows_per_tile, t1 = min(t0 + a.rows_per_tile, sq.tokens);
+  const int t0 = tile * a.rows_per_tile, t1 = min(t0 + a.rows_per_tile, sq.tokens);
   const int2 at = sequences_at(sq, t0, t1);
   int n = at.x, t = border(t0, at.x);
   const int end = t1 < sq.tokens ? border(t1, at.y) : t1;
@@ -159,7 +144,7 @@ __global__ void __launch_bounds__(CONV_THREADS) conv_prompt_kernel(const ConvArg
     }
     ConvRow<VEC> rows[W];                     // the rows that the taps meet, in binary32
 #pragma unroll
-    for (int i = 0; i < H; i++) rows[i + 1].unpack(hist[i]);
+    for (int i = 0; i < H; i++) unpack(hist[i], rows[i + 1].x);
     alignas(16) T next[U][VEC];
     const T *in = x + from * a.x_stride;
     T *to_row = out + from * a.out_stride;
@@ -189,7 +174,7 @@ __global__ void __launch_bounds__(CONV_THREADS) conv_prompt_kernel(const ConvArg
       for (int i = 0; i < U; i++) {
 #pragma unroll
         for (int k = 0; k < H; k++) rows[k] = rows[k + 1];
-        rows[H].unpack(now[i]);
+        unpack(now[i], rows[H].x);
         alignas(16) T y[VEC];
         taps.apply(rows, y);
         if (all || r + i < to) store_row<WIDE>(to_row + i * a.out_stride, y);
@@ -204,7 +189,7 @@ template <typename T, int W, int VEC>
 __global__ void __launch_bounds__(CONV_THREADS) conv_step_kernel(const ConvArgs a) {
   constexpr int H = W - 1;
   constexpr bool WIDE = VEC != 1;
-  const int c = (blockIdx.y * CONV_THREADS + threadIdx.x) * VEC, n = blockIdx.x;
+  const int n = blockIdx.x / a.blocks_c, c = ((blockIdx.x - n * a.blocks_c) * CONV_THREADS + threadIdx.x) * VEC;
   const int slot = a.sq.slot(n);
   if (c >= a.channels || slot < 0) return;
   T *state = static_cast<T *>(a.state) + (size_t)slot * H * a.channels + c;
@@ -217,7 +202,7 @@ __global__ void __launch_bounds__(CONV_THREADS) conv_step_kernel(const ConvArgs 
   taps.load(a, c);
   ConvRow<VEC> x[W];
 #pragma unroll
-  for (int i = 0; i < W; i++) x[i].unpack(rows[i]);
+  for (int i = 0; i < W; i++) unpack(rows[i], x[i].x);
   taps.apply(x, y);
   store_row<WIDE>(static_cast<T *>(a.out) + n * a.out_stride + c, y);
 #pragma unroll

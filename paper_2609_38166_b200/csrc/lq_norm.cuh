@@ -97,8 +97,12 @@ __global__ void __launch_bounds__(NORM_THREADS, 3) norm_rotate_kernel(const Norm
       const bool is_q = h < a.heads_q;
       const int64_t row = row0 + r;
       float x[2][F];
+      unpack(in[i][0], x[0]);
+      unpack(in[i][1], x[1]);
+      if (!there) {                           // (a lane without a head has registers that were never loaded)
 #pragma unroll
-      for (int e = 0; e < 2 * F; e++) x[e / F][e % F] = there ? to_float(in[i][e / F][e % F]) : 0.0f;
+        for (int e = 0; e < 2 * F; e++) x[e / F][e % F] = 0.0f;
+      }
       float scale = is_q ? a.scale_q : a.scale_k;
       if (a.norm != LQ_NORM_NONE) {
         float s = 0.0f;
@@ -143,8 +147,8 @@ __global__ void __launch_bounds__(NORM_THREADS, 3) norm_rotate_kernel(const Norm
       }
       if (there && (!a.positions || a.positions[row] >= 0)) {
         alignas(16) T y[2][F];
-#pragma unroll
-        for (int e = 0; e < 2 * F; e++) y[e / F][e % F] = from_float<T>(x[e / F][e % F]);
+        pack(x[0], y[0]);
+        pack(x[1], y[1]);
         T *dst = is_q ? static_cast<T *>(a.out_q) + row * a.out_q_stride + h * DIM
                       : static_cast<T *>(a.out_k) + row * a.out_k_stride + (h - a.heads_q) * DIM;
         store_row<WIDE>(dst + c0, y[0]);

@@ -58,15 +58,18 @@ static lq_status check_conv(const lq_conv *s, bool step) {
 template <typename T, int W, int VEC>
 static lq_status launch_conv_t(const lq_conv *s, ConvArgs a, bool step, cudaStream_t stream) {
   const long blocks_c = ceil_div(s->channels, CONV_THREADS * VEC);
-  if (blocks_c > 65535) return LQ_ERR_UNSUPPORTED;
+  a.blocks_c = (int)blocks_c;
   if (step) {
-    conv_step_kernel<T, W, VEC><<<dim3(s->seqs, blocks_c), CONV_THREADS, 0, stream>>>(a);
+    if (blocks_c * s->seqs > INT32_MAX) return LQ_ERR_UNSUPPORTED;
+    conv_step_kernel<T, W, VEC><<<blocks_c * s->seqs, CONV_THREADS, 0, stream>>>(a);
   } else {
     // The largest tile that leaves three CTAs to an SM (8192 channels: 32768 rows in tiles of 64, 32, 16, 8 take 258, 274, 312, 406 us; 1024 rows
     // 18.4, 16.4, 18.2, 18.5; 128 rows 14.3, 10.2, 9.0, 8.5).
     a.rows_per_tile = 64;
     while (a.rows_per_tile > 8 && ceil_div(s->tokens, a.rows_per_tile) * blocks_c < 3 * 148) a.rows_per_tile /= 2;
-    conv_prompt_kernel<T, W, VEC><<<dim3(ceil_div(s->tokens, a.rows_per_tile), blocks_c), CONV_THREADS, 0, stream>>>(a);
+    const long grid = ceil_div(s->tokens, a.rows_per_tile) * blocks_c;
+    if (grid > INT32_MAX) return LQ_ERR_UNSUPPORTED;
+    conv_prompt_kernel<T, W, VEC><<<grid, CONV_THREADS, 0, stream>>>(a);
   }
   return launched();
 }
@@ -99,7 +102,7 @@ static lq_status conv(const lq_conv *s, const void *x, int64_t x_stride, const v
       rows_overlap(x, x_stride, s->channels, out, out_stride, s->channels, s->tokens, bytes))
     return LQ_ERR_UNSUPPORTED;
   ConvArgs a{x, w, bias, state, out, x_stride, out_stride, {seq_start, slots, resume, s->tokens, s->seqs, state ? s->n_slots : INT32_MAX},
-             s->channels, s->silu, 0};
+             s->channels, s->silu, 0, 0};
   if (s->type == LQ_F32) return launch_conv<float>(s, a, step, cuda_stream(stream));
   if (s->type == LQ_F16) return launch_conv<__half>(s, a, step, cuda_stream(stream));
   return launch_conv<__nv_bfloat16>(s, a, step, cuda_stream(stream));

@@ -5,6 +5,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "../../include/lq.h"
 
 namespace lq {
@@ -45,6 +47,44 @@ __device__ __forceinline__ void store_row(T *dst, const T (&x)[N]) {
   } else {
 #pragma unroll
     for (int i = 0; i < N; i++) dst[i] = x[i];
+  }
+}
+
+// N elements in binary32; pairs of bf16 by a shift and a mask of the register that they share (one by one they take twice the instructions).
+template <typename T, int N>
+__device__ __forceinline__ void unpack(const T (&t)[N], float (&x)[N]) {
+  if constexpr (sizeof(T) == 2 && N % 2 == 0) {
+#pragma unroll
+    for (int e = 0; e < N; e += 2) {
+      const uint32_t two = *reinterpret_cast<const uint32_t *>(&t[e]);
+      if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+        x[e] = __uint_as_float(two << 16);
+        x[e + 1] = __uint_as_float(two & 0xFFFF0000u);
+      } else {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&two));
+        x[e] = f.x;
+        x[e + 1] = f.y;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; e++) x[e] = to_float(t[e]);
+  }
+}
+// The same, rounded to T (nearest even).
+template <typename T, int N>
+__device__ __forceinline__ void pack(const float (&x)[N], T (&t)[N]) {
+  if constexpr (sizeof(T) == 2 && N % 2 == 0) {
+#pragma unroll
+    for (int e = 0; e < N; e += 2) {
+      uint32_t two;
+      if constexpr (std::is_same_v<T, __nv_bfloat16>) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(two) : "f"(x[e + 1]), "f"(x[e]));
+      else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(two) : "f"(x[e + 1]), "f"(x[e]));
+      *reinterpret_cast<uint32_t *>(&t[e]) = two;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; e++) t[e] = from_float<T>(x[e]);
   }
 }
 
