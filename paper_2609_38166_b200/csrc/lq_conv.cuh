@@ -4,8 +4,9 @@
 // 2 x 2 bytes of traffic - bound by memory.  A thread owns VEC neighbouring channels (four; one where
 // their number, strides or addresses do not divide) and walks down the rows of its
 // tile with the last width-1 rows in registers, so a row is read once per tile (and width-1 rows of the tile before it).
-// 32768 rows x 8192 channels: bf16 253 us, 4.2 TB/s (the exponential and the quotient alone are 119 us of the special-function units; eight
-// channels to a thread left room for fewer warps: 360 us); 16384 rows in binary32 186 us, 5.8 TB/s.
+// 32768 rows x 8192 channels: bf16 191 us, 5.6 TB/s (the exponential and the quotient alone are 119 us of the special-function units; 253 us
+// with elements taken apart and rounded one by one, 360 with eight channels to a thread, which leave room for fewer warps); 16384 rows in
+// binary32 183 us, 5.9 TB/s.
 #pragma once
 #include "lq_rows.cuh"
 

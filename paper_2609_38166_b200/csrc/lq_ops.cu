@@ -63,9 +63,10 @@ static lq_status launch_conv_t(const lq_conv *s, ConvArgs a, bool step, cudaStre
     if (blocks_c * s->seqs > INT32_MAX) return LQ_ERR_UNSUPPORTED;
     conv_step_kernel<T, W, VEC><<<blocks_c * s->seqs, CONV_THREADS, 0, stream>>>(a);
   } else {
-    // The largest tile that leaves three CTAs to an SM (8192 channels: 32768 rows in tiles of 64, 32, 16, 8 take 258, 274, 312, 406 us; 1024 rows
-    // 18.4, 16.4, 18.2, 18.5; 128 rows 14.3, 10.2, 9.0, 8.5).
-    a.rows_per_tile = 64;
+    // The largest tile that leaves three CTAs to an SM; 128 rows only for 16-bit types and twelve CTAs to an SM.  8192 channels, bf16: 32768
+    // rows in tiles of 128, 64, 32, 16, 8 take 192, 200, 217, 285, 426 us; 16384 rows 102, 106, 115, 147; 8192 rows 63, 59, 65, 80; 1024 rows in
+    // 64, 32, 16, 8 16.4, 16.4, 16.4, 18.4; 128 rows 12.3, 10.2, 8.2, 8.2; binary32, 16384 rows in 128, 64, 32: 190, 182, 190.
+    a.rows_per_tile = sizeof(T) == 2 && ceil_div(s->tokens, 128) * blocks_c >= 12 * 148 ? 128 : 64;
     while (a.rows_per_tile > 8 && ceil_div(s->tokens, a.rows_per_tile) * blocks_c < 3 * 148) a.rows_per_tile /= 2;
     const long grid = ceil_div(s->tokens, a.rows_per_tile) * blocks_c;
     if (grid > INT32_MAX) return LQ_ERR_UNSUPPORTED;
