@@ -336,8 +336,8 @@ typedef enum { LQ_BF16 = 0, LQ_F16 = 1, LQ_F32 = 2 } lq_type;
  *   state  : [n_slots][width-1][channels], the last width-1 rows of x, oldest first, in and out (lq_conv_prompt: null
  *            if the prompts are fresh and no state is wanted)                                          - all of `type`
  * The slot of a sequence without rows is left as it is.
- * lq_conv_step's out may be its x (same pointer and stride).  Otherwise out must not overlap x: LQ_ERR_UNSUPPORTED where
- * the two ranges show that it does.
+ * lq_conv_step's out may be its x (same pointer and stride).  Otherwise out must not overlap x, nor state either of them:
+ * LQ_ERR_UNSUPPORTED where the ranges show that they do.
  */
 typedef struct {
   int tokens;   /* rows (lq_conv_step: equal to seqs)  */
@@ -404,7 +404,7 @@ lq_status lq_norm_rotate(const lq_norm *shape, const void *q, int64_t q_stride, 
  * the end of its sequence, and S of that sequence; other sequences never see it.
  * lq_scan_step: one row per sequence (tokens = seqs), every sequence is resumed, o is fp32 [seqs][Hv][d_v] in strided rows.
  * A sequence without rows has the state it starts from in its slot afterwards: what it is resumed from, or zeros.
- * Neither may have S, o and the inputs overlap.
+ * Neither may have S, S0, o and the inputs overlap (but for S0 = S): LQ_ERR_UNSUPPORTED where the ranges of S, S0, o, q, k and v show it.
  *
  * `work`: lq_scan_prompt_bytes(shape) bytes of device memory, 16-byte aligned, for the states between the pieces that long prompts are
  * cut into and for handing out the heads (null if that is 0).  Its contents mean nothing between calls; calls that may run at the same time need one each.

@@ -44,6 +44,12 @@ static bool rows_overlap(const void *a, int64_t sa, long wa, const void *b, int6
   return d < wa * (intptr_t)bytes || d + wb * (intptr_t)bytes > period;
 }
 
+// Whether `bytes` bytes at p, without gaps, meet the range of those strided rows.
+static bool meets_rows(const void *p, uint64_t bytes, const void *a, int64_t sa, long wa, long rows, unsigned size) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(p), y = reinterpret_cast<uintptr_t>(a);
+  return rows > 0 && x < y + ((rows - 1) * (uint64_t)sa + wa) * size && y < x + bytes;
+}
+
 // ---- short causal convolution ----
 
 static lq_status check_conv(const lq_conv *s, bool step) {
@@ -102,6 +108,9 @@ static lq_status conv(const lq_conv *s, const void *x, int64_t x_stride, const v
   if (!(step && x == out && x_stride == out_stride) &&
       rows_overlap(x, x_stride, s->channels, out, out_stride, s->channels, s->tokens, bytes))
     return LQ_ERR_UNSUPPORTED;
+  const uint64_t states = state ? (uint64_t)s->n_slots * (s->width - 1) * s->channels * bytes : 0;
+  if (meets_rows(state, states, x, x_stride, s->channels, s->tokens, bytes) || meets_rows(state, states, out, out_stride, s->channels, s->tokens, bytes))
+    return LQ_ERR_UNSUPPORTED;
   ConvArgs a{x, w, bias, state, out, x_stride, out_stride, {seq_start, slots, resume, s->tokens, s->seqs, state ? s->n_slots : INT32_MAX},
              s->channels, s->silu, 0, 0};
   if (s->type == LQ_F32) return launch_conv<float>(s, a, step, cuda_stream(stream));
@@ -152,6 +161,8 @@ static lq_status check_scan_io(const lq_scan *s, const lq_scan_io *io, const voi
   if ((rc = check_arrays(16, {io->S}, {io->S0})) != LQ_OK) return rc;
   if (!step && !io->seq_start) return LQ_ERR_NULL;
   if ((rc = check_arrays(4, {}, {io->A, io->dt_bias, io->skip, io->seq_start, io->slots, io->resume})) != LQ_OK) return rc;
+  const uint64_t states = (uint64_t)s->n_slots * s->heads_v * (SD * SD) * sizeof(float);
+  if (io->S0 && io->S0 != io->S && meets_rows(io->S, states, io->S0, 0, (long)states, 1, 1)) return LQ_ERR_UNSUPPORTED;
   if (s->tokens == 0) return LQ_OK;
   if ((rc = check_arrays(16, {io->q, io->k, io->v, o})) != LQ_OK) return rc;
   if ((rc = check_arrays(type_size(s->gate_type), {io->beta}, {io->alpha})) != LQ_OK) return rc;
@@ -160,6 +171,16 @@ static lq_status check_scan_io(const lq_scan *s, const lq_scan_io *io, const voi
   if (io->q_stride < wq || io->k_stride < wq || io->v_stride < wv || o_stride < wv) return LQ_ERR_SHAPE;
   if (io->beta_stride < s->heads_v || (!s->select && io->alpha_stride < s->heads_v)) return LQ_ERR_SHAPE;
   if (io->q_stride % 8 || io->k_stride % 8 || io->v_stride % 8 || o_stride % 8) return LQ_ERR_ALIGN;
+  // (the heads of a group, and the blocks' other roles, read q, k and v after the first outputs are written)
+  const unsigned size = step ? sizeof(float) : 2;   // of an output
+  if (rows_overlap(io->q, io->q_stride * 2, wq * 2, o, o_stride * size, wv * size, s->tokens, 1) ||
+      rows_overlap(io->k, io->k_stride * 2, wq * 2, o, o_stride * size, wv * size, s->tokens, 1) ||
+      rows_overlap(io->v, io->v_stride * 2, wv * 2, o, o_stride * size, wv * size, s->tokens, 1))
+    return LQ_ERR_UNSUPPORTED;
+  if (meets_rows(io->S, states, o, o_stride, wv, s->tokens, size) || meets_rows(io->S, states, io->q, io->q_stride, wq, s->tokens, 2) ||
+      meets_rows(io->S, states, io->k, io->k_stride, wq, s->tokens, 2) || meets_rows(io->S, states, io->v, io->v_stride, wv, s->tokens, 2))
+    return LQ_ERR_UNSUPPORTED;
+  if (io->S0 && meets_rows(io->S0, states, o, o_stride, wv, s->tokens, size)) return LQ_ERR_UNSUPPORTED;
   return LQ_OK;
 }
 

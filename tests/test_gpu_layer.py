@@ -201,3 +201,37 @@ def test_arrays_of_sequences_that_make_no_sense_touch_nothing_else():
     assert lq.check_device() == 0
     for x, lead, tail in ((mixed, 32, 32), (o, 32, 32), (state, 1, 1), (S, 1, 1)):
         assert bool((x[:lead] == guard).all()) and bool((x[-tail:] == guard).all())
+
+
+def test_arrays_side_by_side_in_one_buffer():
+    """Column slices of one buffer and the states right behind its last row: neighbours, not overlaps; the bits are those of arrays of their own."""
+    T, H, G, D = 150, 2, 1, 128
+    g = torch.Generator(device="cuda").manual_seed(5)
+    W = (2 * G + 2 * H) * D                                                       # q | k | v | o
+    n = T * W * 2
+    buf = torch.empty(n + H * D * D * 4, device="cuda", dtype=torch.uint8)
+    rows, S = buf[:n].view(torch.bfloat16).view(T, W), buf[n:].view(torch.float32).view(1, H, D, D)
+    rows.copy_(torch.randn(T, W, device="cuda", generator=g) * 0.1)
+    cut = lambda a, b, h: rows[:, a * D:b * D].unflatten(1, (h, D))               # noqa: E731
+    q, k, v, o = cut(0, G, G), cut(G, 2 * G, G), cut(2 * G, 2 * G + H, H), cut(2 * G + H, 2 * G + 2 * H, H)
+    beta, alpha = (torch.rand(T, H, device="cuda", generator=g).bfloat16() for _ in range(2))
+    start = torch.tensor([0, T], device="cuda", dtype=torch.int32)
+    sh = lq.ScanShape(T, 1, H, G, max_len=T, n_slots=1)
+    own_o, own_S = torch.empty(T, H, D, device="cuda", dtype=torch.bfloat16), torch.empty(1, H, D, D, device="cuda")
+    work = torch.empty(lq.scan_prompt_bytes(sh), device="cuda", dtype=torch.uint8)
+    lq.scan_prompt(sh, q.contiguous(), k.contiguous(), v.contiguous(), beta, alpha, own_o, own_S, start, work=work)
+    lq.scan_prompt(sh, q, k, v, beta, alpha, o, S, start, work=work)
+    assert torch.equal(o, own_o) and torch.equal(S, own_S)
+
+    C = 64
+    n = T * 2 * C * 2
+    buf = torch.empty(n + 3 * C * 2, device="cuda", dtype=torch.uint8)
+    rows, state = buf[:n].view(torch.bfloat16).view(T, 2 * C), buf[n:].view(torch.bfloat16).view(1, 3, C)
+    rows.copy_(torch.randn(T, 2 * C, device="cuda", generator=g))
+    w = torch.randn(C, 4, device="cuda", generator=g).bfloat16()
+    x, out = rows[:, :C], rows[:, C:]
+    own, own_state = torch.empty(T, C, device="cuda", dtype=torch.bfloat16), torch.empty(1, 3, C, device="cuda", dtype=torch.bfloat16)
+    sh = lq.ConvShape(T, 1, C, n_slots=1)
+    lq.conv_prompt(sh, x.contiguous(), w, None, own_state, own, start)
+    lq.conv_prompt(sh, x, w, None, state, out, start)
+    assert torch.equal(out, own) and torch.equal(state, own_state)

@@ -117,3 +117,28 @@ def test_binding_refuses_tensors_that_are_not_what_the_shape_says():
     sh = lq.ConvShape(4, 4, 64, n_slots=4)
     with pytest.raises((lq.LqError, AssertionError, RuntimeError)):
         lq.conv_step(sh, x, x, None, x, x)                                        # not on the device
+
+
+@pytest.mark.parametrize("step", [False, True])
+def test_scan_refuses_arrays_that_overlap(L, step):
+    """Offsets in bytes: a state of 4 slots of 4 heads has 1 MB (2^20), four rows of o 4 KB (bf16) or 8 KB (fp32)."""
+    sh = lq.ScanShape(4, 4, 4, 2, max_len=4, n_slots=4)
+    at = dict(q=P, k=P + 0x10000, v=P + 0x20000, S=P + 0x100000)
+    go = lambda **kw: scan(L, sh, step=step, **{**at, **kw})                      # noqa: E731
+    row = 4 * 128 * (4 if step else 2)
+    for kw in (dict(o=P), dict(o=P + 0x10000 + 16), dict(o=P + 0x20000), dict(o=P + 0x20000 - 4 * row + 16)):        # over q, k, v
+        assert go(**kw) == UNSUPPORTED, kw
+    for kw in (dict(o=P + 0x100000), dict(o=P + 0x200000 - 16), dict(o=P + 0x100000 - 4 * row + 16)):                # over S
+        assert go(**kw) == UNSUPPORTED, kw
+    for kw in (dict(q=P + 0x100000), dict(k=P + 0x200000 - 16), dict(v=P + 0x180000)):                               # S over an input
+        assert go(**kw) == UNSUPPORTED, kw
+    for kw in (dict(S0=P + 0x100000 + 16), dict(S0=P + 16), dict(S0=P + 0x200000 - 16), dict(S0=P << 3, o=P << 3)):   # S0 over S, o over S0
+        assert go(**kw) == UNSUPPORTED, kw
+
+
+def test_conv_refuses_a_state_that_overlaps(L):
+    sh = lq.ConvShape(4, 4, 64, n_slots=4)                                        # a state of 1536 bytes, rows of 512
+    for step in (False, True):
+        for state in (P, P + 510, P - 1534, 2 * P, 2 * P + 510, 2 * P - 1534):
+            assert conv(L, sh, x=P, out=2 * P, w=4 * P, state=state, step=step) == UNSUPPORTED, state
+
