@@ -183,7 +183,7 @@ struct ScanShared {                            // (all but 96 bytes of what a CT
   ScanWeights weights[2];
   int items[2][6];                             // h, slot, row, rows, at, flags
   uint64_t items_full[2], items_empty[2], k_full[2], k_empty[2], q_full[2], q_empty[2], v_full[2], v_empty[2], sums_full, sums_empty, weights_full[2], weights_empty[2];
-  uint64_t w_full[2], w_empty[2], p_full, pw_full, o1_full, o_full, o_free, ds_full, ds_free, s_full, clean[2], drained[2];
+  uint64_t w_full[2], w_empty[2], p_full, pw_full, o_full, o_free, ds_full, ds_free, s_full, s_empty, clean[2], drained[2];
   uint32_t tmem;
 };
 static_assert(sizeof(ScanShared) <= 232448, "");
@@ -470,13 +470,11 @@ __device__ __forceinline__ void scan_products(ScanShared &sm, int lane) {
         tmem_fence_after();
         if (elect_one()) {
           multiply_halves(TM_O, Q, S, KK);
+          mma_commit(shared_addr(&sm.s_empty));
         }
         __syncwarp();
       }
-      if (elect_one()) {
-        mma_commit(shared_addr(&sm.q_empty[r]));
-        mma_commit(shared_addr(&sm.o1_full));
-      }
+      if (elect_one()) mma_commit(shared_addr(&sm.q_empty[r]));
       __syncwarp();
       if (!(ok = wait_for(sm.v_full[r], (c >> 1) & 1))) break;
       if (!(ok = wait_for(sm.clean[r], (c >> 1) & 1))) break;
@@ -738,7 +736,7 @@ __device__ __forceinline__ void scan_state(ScanShared &sm, const ScanArgs &a, co
   const int channel = 32 * w + lane;
   uint8_t *s16 = sm.s16 + channel * 128;
   ScanItem it;
-  int t = 0, c = 0;
+  int t = 0, c = 0, ns = 0;                    // items, blocks, states published so far
   bool ok = true;
   while (ok && (ok = take(sm, it, t, lane)) && it.rows >= 0) {
     const size_t at = it.at;
@@ -751,9 +749,10 @@ __device__ __forceinline__ void scan_state(ScanShared &sm, const ScanArgs &a, co
     float decay = 1.0f;
     for (int b = 0; b < it.blocks; b++, c++) {
       if (OUT && (it.state() || b > 0)) {
-        // The product that reads the state in front of the last block.  (Waited for only where a state is published: until then the product
-        // behind does not run, so this phase cannot be passed twice.)
-        if (c > 0 && !(ok = wait_for(sm.o1_full, (c + 1) & 1))) break;
+        // The product that reads the state published last.  (One phase for every state, not for every block: fresh heads' first blocks have none,
+        // and a wait that they leave out would find a phase of blocks one behind and take it for the one after.)
+        if (ns > 0 && !(ok = wait_for(sm.s_empty, (ns + 1) & 1))) break;
+        ns++;
         publish_state(S, s16, lane);
         fence_async_shared();
         warp_arrive(sm.s_full, lane);
@@ -852,7 +851,7 @@ __global__ void __launch_bounds__(SCAN_THREADS, 1) scan_blocks_kernel(const __gr
       init(sm.w_full[i], 8), init(sm.w_empty[i], 1);
       init(sm.clean[i], 8), init(sm.drained[i], 1);
     }
-    for (uint64_t *b : {&sm.sums_full, &sm.p_full, &sm.o1_full, &sm.o_full, &sm.ds_full}) init(*b, 1);
+    for (uint64_t *b : {&sm.sums_full, &sm.p_full, &sm.s_empty, &sm.o_full, &sm.ds_full}) init(*b, 1);
     for (uint64_t *b : {&sm.pw_full, &sm.ds_free, &sm.s_full}) init(*b, 4);
     init(sm.o_free, 8);
     init(sm.sums_empty, 12);
