@@ -367,6 +367,7 @@ lq_status lq_conv_step(const lq_conv *shape, const void *x, int64_t x_stride, co
  *                                                                        rot = 0)
  * A row with a negative position is padding: it is not written.  An output may be its own input (same pointer and stride);
  * no other overlap is allowed.  The angle is taken modulo one turn in 64 bits, so far positions lose nothing.
+ * Channels that a frequency turns which is not finite become NaN.
  * heads_q or heads_k may be zero (its pointers are not looked at then).
  */
 enum { LQ_NORM_NONE = 0, LQ_NORM_L2 = 1, LQ_NORM_RMS = 2 };

@@ -35,6 +35,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 3) norm_rotate_kernel(const Norm
   __shared__ __align__(16) float2 turn[NORM_MAX_ROWS][F / 2][LANES][2];
   __shared__ __align__(16) float weight[2][2 * F / 4][LANES][4];
   __shared__ uint64_t step[DIM / 2];
+  __shared__ float nothing[DIM / 2];          // 0, or NaN where a frequency is not finite: no fraction of a turn can say so
   constexpr int BATCH = 1;                    // heads that a lane works on while it waits for as many
   const int row0 = blockIdx.x * a.rows_per_cta, rows = min(a.rows_per_cta, a.tokens - row0);
   const int half = a.rot / 2, heads = a.heads_q + a.heads_k;
@@ -63,13 +64,14 @@ __global__ void __launch_bounds__(NORM_THREADS, 3) norm_rotate_kernel(const Norm
     for (int f = threadIdx.x; f < half; f += NORM_THREADS) {
       const double turns = (double)a.inv_freq[f] * 0.15915494309189533577;   // of a turn a position, / (2 pi)
       step[f] = (uint64_t)(int64_t)((turns - rint(turns)) * 18446744073709551616.0);   // modulo 1, in units of 2^-64
+      nothing[f] = a.inv_freq[f] * 0.0f;
     }
     __syncthreads();
     for (int i = threadIdx.x; i < rows * half; i += NORM_THREADS) {
       const int r = a.half.quotient(i), f = i - r * half;
       const int32_t phase = (int32_t)((step[f] * (uint64_t)(int64_t)a.positions[row0 + r]) >> 32);
       float sn, cs;
-      sincospif((float)phase * 4.656612873077392578125e-10f, &sn, &cs);   // 2^-31: in half turns
+      sincospif(fmaf((float)phase, 4.656612873077392578125e-10f, nothing[f]), &sn, &cs);   // 2^-31: in half turns
       turn[r][f % F / 2][f / F][f % 2] = make_float2(cs, sn);
     }
   }

@@ -82,3 +82,24 @@ def test_a_row_of_zeros_and_large_values():
     lq.norm_rotate(lq.NormShape(3, 1, 0, type=lq.F32), x, None, y, None)
     assert torch.equal(y[0], torch.zeros_like(y[0])) and torch.allclose(y[1], torch.full_like(y[1], 128 ** -0.5), rtol=1e-6)
     assert torch.isnan(y[2]).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("pairs", [False, True])
+def test_frequencies_that_are_not_finite(dtype, dim, pairs):
+    """The channels that they turn are NaN, at position 0 too; all others stay as they are, bit for bit."""
+    T, H, half = 21, 3, dim // 4
+    x = torch.randn((T, H, dim), generator=torch.Generator().manual_seed(dim)).to(dtype).cuda()
+    freq = (10000.0 ** -(torch.arange(half) / half)).float()
+    pos = torch.arange(T, dtype=torch.int32).cuda()
+    sh = lq.NormShape(T, H, 0, dim=dim, rot=2 * half, pairs=int(pairs), type=lq.TYPES[dtype])
+    want, got = torch.empty_like(x), torch.empty_like(x)
+    lq.norm_rotate(sh, x, None, want, None, positions=pos, inv_freq=freq.cuda())
+    freq[1], freq[4], freq[half - 1] = float("nan"), float("inf"), float("-inf")
+    lq.norm_rotate(sh, x, None, got, None, positions=pos, inv_freq=freq.cuda())
+    i = torch.tensor([1, 4, half - 1])
+    bad = torch.zeros(dim, dtype=torch.bool)
+    bad[torch.cat([2 * i, 2 * i + 1] if pairs else [i, i + half])] = True
+    assert torch.isnan(got.cpu()[..., bad]).all()
+    assert torch.equal(got.cpu()[..., ~bad], want.cpu()[..., ~bad]) and torch.isfinite(want).all()
