@@ -325,6 +325,7 @@ lq_status lq_ref_decode_step_bf16(const lq_shape *shape, uint16_t *S, const uint
  *    slot holds is not read), elsewhere it goes on from what its slot holds.
  *  - Sums are taken in binary32, in an order that depends on the shapes alone:
  *    the same call gives the same bits again.
+ *  - Convolution and scan: at most 2^31 - 1024 rows and sequences, scan: seqs * heads_v at most 2^30 (LQ_ERR_UNSUPPORTED beyond).
  */
 typedef enum { LQ_BF16 = 0, LQ_F16 = 1, LQ_F32 = 2 } lq_type;
 

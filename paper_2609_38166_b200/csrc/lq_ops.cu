@@ -21,6 +21,9 @@ static long ceil_div(long a, long b) { return (a + b - 1) / b; }
 
 static bool bad_count(int n) { return n < 0; }
 
+// Row and sequence numbers up to a tile or a CTA beyond the last one are formed in 32 bits.
+constexpr int MOST_ROWS = INT32_MAX - 1023;
+
 // Required and optional (may be null) arrays with elements of `bytes` bytes.
 static lq_status check_arrays(unsigned bytes, std::initializer_list<const void *> required, std::initializer_list<const void *> optional = {}) {
   for (const void *p : required) {
@@ -57,7 +60,7 @@ static lq_status check_conv(const lq_conv *s, bool step) {
   if (bad_count(s->tokens) || bad_count(s->seqs) || s->channels <= 0 || s->width <= 0 || bad_count(s->n_slots)) return LQ_ERR_SHAPE;
   if (s->type < LQ_BF16 || s->type > LQ_F32 || (s->silu != 0 && s->silu != 1)) return LQ_ERR_SHAPE;
   if (step && s->tokens != s->seqs) return LQ_ERR_SHAPE;
-  if (s->width < 2 || s->width > 4) return LQ_ERR_UNSUPPORTED;
+  if (s->width < 2 || s->width > 4 || s->tokens > MOST_ROWS || s->seqs > MOST_ROWS) return LQ_ERR_UNSUPPORTED;
   return LQ_OK;
 }
 
@@ -151,7 +154,8 @@ static lq_status check_scan(const lq_scan *s, bool step) {
   if (s->heads_v % s->heads_qk != 0 || (s->select != 0 && s->select != 1)) return LQ_ERR_SHAPE;
   if (step ? s->tokens != s->seqs : s->max_len < 0) return LQ_ERR_SHAPE;
   if (s->gate_type != LQ_BF16 && s->gate_type != LQ_F32) return LQ_ERR_UNSUPPORTED;
-  if (s->d_k != SD || s->d_v != SD || (long)s->seqs * s->heads_v > INT32_MAX) return LQ_ERR_UNSUPPORTED;
+  // (2^30 heads: numbers of items go on beyond the last one by as many as there are CTAs)
+  if (s->d_k != SD || s->d_v != SD || s->tokens > MOST_ROWS || (long)s->seqs * s->heads_v > 1 << 30) return LQ_ERR_UNSUPPORTED;
   return LQ_OK;
 }
 

@@ -144,3 +144,33 @@ def test_binding_scan(host, select):
     del args["seq_start"], args["resume"]
     args["o"] = rand(T, H, 128, dtype=f32)
     check(lambda a: lq.scan_step(sh, stream=0, **a), args, ("q", "k", "v", "beta", "o"))
+
+
+# ---- counts near 2^31: row numbers up to a tile, sequence numbers up to a CTA and items up to a wave beyond the last are formed in 32 bits ----
+
+MOST = 2 ** 31 - 1024
+
+
+def scan(L, sh, step):
+    w = (sh.heads_qk * 128, sh.heads_v * 128)
+    io = lq._ScanIo(q=X, k=X, v=X, q_stride=w[0], k_stride=w[0], v_stride=w[1], beta=X, alpha=X, beta_stride=sh.heads_v, alpha_stride=sh.heads_v, S=STATE,
+                    seq_start=STARTS)
+    if step:
+        return L.lq_scan_step(C.byref(sh.c()), C.byref(io), OUT, w[1], None)
+    return L.lq_scan_prompt(C.byref(sh.c()), C.byref(io), OUT, w[1], TAPS, None)
+
+
+@pytest.mark.parametrize("n", [MOST + 1, 2 ** 31 - 129, 2 ** 31 - 1])
+def test_conv_counts_near_two_to_the_31(L, n):
+    assert conv(L, lq.ConvShape(n, 4, 64, n_slots=4), False) == UNSUPPORTED
+    assert conv(L, lq.ConvShape(40, n, 64, n_slots=4), False) == UNSUPPORTED
+    assert conv(L, lq.ConvShape(n, n, 64, n_slots=4), True) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("seqs,heads", [(2 ** 31 - 1, 1), (2 ** 24 - 1, 128), (2 ** 23 + 1, 128)])
+def test_scan_counts_near_two_to_the_31(L, seqs, heads):
+    """Few rows in very many sequences: 2^30 heads at most."""
+    sh = lq.ScanShape(8, seqs, heads, 1, max_len=8, n_slots=8)
+    assert scan(L, sh, False) == UNSUPPORTED and L.lq_scan_prompt_bytes(C.byref(sh.c())) == 0
+    assert scan(L, dataclasses.replace(sh, tokens=seqs), True) == UNSUPPORTED
+    assert scan(L, lq.ScanShape(MOST + 1, 8, 1, 1, max_len=8, n_slots=8), False) == UNSUPPORTED
