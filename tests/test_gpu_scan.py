@@ -258,3 +258,22 @@ def test_prompt_then_steps_are_the_longer_prompt():
         lq.scan_step(one, q[t:t + 1], k[t:t + 1], v[t:t + 1], dt[t:t + 1], None, ot, S, **kw)
         assert ((ot.cpu()[0].double() - wo[t]).abs() / (2.0 ** -16 * so[t])).max() <= 1
     assert ((S.cpu().double() - wS).abs() / (2.0 ** -16 * sS + 1e-30)).max() <= 1
+
+
+@pytest.mark.parametrize("lens,hv,hq,select,slow", [([300, 128, 77], 4, 2, False, 0.05), ([300, 128, 77], 4, 2, False, 1.0), ([520], 6, 6, True, 0.05),
+                                                    ([2500], 1, 1, False, 0.01)])
+def test_all_outputs_together(lens, hv, hq, select, slow):
+    """The 2-norm of what all outputs are off by, below that of three roundings to bf16 at independent places.
+
+    A rounding to bf16 (steps of 2^-7 of the power of two below) is off by 2^-7 / sqrt(12) = 2.26e-3 of the value in the mean square at most.
+    The output has one; in front of it are one of the state's elements, which q weighs, and one of the weighted scores, which weigh v.  These are
+    sums of many terms with errors that do not know of one another, so that each part is off by 2.26e-3 of its own size, and the parts, which
+    do not know of one another either, have the output's size together: sqrt(2) * 2.26e-3 = 3.2e-3, and half a percent for the number of
+    outputs (50 thousand at least) and for binary32.
+    """
+    c = Case(lens, hv, hq, select=select, slow=slow, resume=[1] * len(lens), gates=torch.float32)
+    o, S = c.prompt()
+    wo, _, wS, _ = c.want()
+    off = float(torch.linalg.norm(o.double() - wo) / torch.linalg.norm(wo))
+    print(f"o {off:.3e}, S {float(torch.linalg.norm(S.double() - wS) / torch.linalg.norm(wS)):.3e}")
+    assert off <= 1.005 * 2 ** 0.5 * 2.0 ** -7 / 12 ** 0.5
