@@ -36,7 +36,6 @@ __global__ void __launch_bounds__(NORM_THREADS, 3) norm_rotate_kernel(const Norm
   __shared__ __align__(16) float weight[2][2 * F / 4][LANES][4];
   __shared__ uint64_t step[DIM / 2];
   __shared__ float nothing[DIM / 2];          // 0, or NaN where a frequency is not finite: no fraction of a turn can say so
-  constexpr int BATCH = 1;                    // heads that a lane works on while it waits for as many
   const int row0 = blockIdx.x * a.rows_per_cta, rows = min(a.rows_per_cta, a.tokens - row0);
   const int half = a.rot / 2, heads = a.heads_q + a.heads_k;
   const int lane = threadIdx.x % LANES;
@@ -44,19 +43,15 @@ __global__ void __launch_bounds__(NORM_THREADS, 3) norm_rotate_kernel(const Norm
   const int c0 = apart ? F * lane : 2 * F * lane, c1 = apart ? half + F * lane : c0 + F;   // where the lane's pieces start
   const int units = rows * heads;             // heads of all rows
   constexpr int SIDE = NORM_THREADS / LANES;  // heads that the CTA has at a time
-  alignas(16) T next[BATCH][2][F];
-  auto load = [&](int u0) {
-#pragma unroll
-    for (int i = 0; i < BATCH; i++) {
-      const int u = u0 + i * SIDE;
-      if (u >= units) continue;
-      const int r = a.heads.quotient(u), h = u - r * heads;
-      const int64_t row = row0 + r;
-      const T *src = h < a.heads_q ? static_cast<const T *>(a.q) + row * a.q_stride + h * DIM
-                                   : static_cast<const T *>(a.k) + row * a.k_stride + (h - a.heads_q) * DIM;
-      load_row<WIDE>(src + c0, next[i][0]);
-      load_row<WIDE>(src + c1, next[i][1]);
-    }
+  alignas(16) T next[2][F];                   // the head on its way while one is worked on
+  auto load = [&](int u) {
+    if (u >= units) return;
+    const int r = a.heads.quotient(u), h = u - r * heads;
+    const int64_t row = row0 + r;
+    const T *src = h < a.heads_q ? static_cast<const T *>(a.q) + row * a.q_stride + h * DIM
+                                 : static_cast<const T *>(a.k) + row * a.k_stride + (h - a.heads_q) * DIM;
+    load_row<WIDE>(src + c0, next[0]);
+    load_row<WIDE>(src + c1, next[1]);
   };
   const int mine = threadIdx.x / LANES;
   load(mine);                                 // (on their way while the angles are worked out)
@@ -84,79 +79,72 @@ __global__ void __launch_bounds__(NORM_THREADS, 3) norm_rotate_kernel(const Norm
     }
   __syncthreads();
 #pragma unroll 1
-  for (int u0 = mine; u0 - mine < units; u0 += BATCH * SIDE) {   // (the same trips for all lanes of a warp)
-    alignas(16) T in[BATCH][2][F];
+  for (int u = mine; u - mine < units; u += SIDE) {   // (the same trips for all lanes of a warp)
+    alignas(16) T in[2][F];
 #pragma unroll
-    for (int i = 0; i < BATCH; i++)
+    for (int e = 0; e < 2 * F; e++) in[e / F][e % F] = next[e / F][e % F];
+    load(u + SIDE);
+    const bool there = u < units;
+    const int r = there ? a.heads.quotient(u) : 0, h = there ? u - r * heads : 0;
+    const bool is_q = h < a.heads_q;
+    const int64_t row = row0 + r;
+    float x[2][F];
+    unpack(in[0], x[0]);
+    unpack(in[1], x[1]);
+    if (!there) {                             // (a lane without a head has registers that were never loaded)
 #pragma unroll
-      for (int e = 0; e < 2 * F; e++) in[i][e / F][e % F] = next[i][e / F][e % F];
-    load(u0 + BATCH * SIDE);
+      for (int e = 0; e < 2 * F; e++) x[e / F][e % F] = 0.0f;
+    }
+    float scale = is_q ? a.scale_q : a.scale_k;
+    if (a.norm != LQ_NORM_NONE) {
+      float s = 0.0f;
 #pragma unroll
-    for (int i = 0; i < BATCH; i++) {
-      const int u = u0 + i * SIDE;
-      if (u - mine >= units) break;
-      const bool there = u < units;
-      const int r = there ? a.heads.quotient(u) : 0, h = there ? u - r * heads : 0;
-      const bool is_q = h < a.heads_q;
-      const int64_t row = row0 + r;
-      float x[2][F];
-      unpack(in[i][0], x[0]);
-      unpack(in[i][1], x[1]);
-      if (!there) {                           // (a lane without a head has registers that were never loaded)
+      for (int e = 0; e < 2 * F; e++) s = fmaf(x[e / F][e % F], x[e / F][e % F], s);
 #pragma unroll
-        for (int e = 0; e < 2 * F; e++) x[e / F][e % F] = 0.0f;
+      for (int m = 1; m < LANES; m *= 2) s += __shfl_xor_sync(0xffffffffu, s, m);
+      scale *= rsqrtf((a.norm == LQ_NORM_RMS ? s * (1.0f / DIM) : s) + a.eps);
+    }
+    if (a.norm == LQ_NORM_RMS) {
+#pragma unroll
+      for (int e = 0; e < 2 * F; e += 4) {
+        const float4 w = *reinterpret_cast<const float4 *>(weight[is_q ? 0 : 1][e / 4][lane]);
+        x[e / F][e % F] *= scale * w.x;
+        x[e / F][e % F + 1] *= scale * w.y;
+        x[e / F][e % F + 2] *= scale * w.z;
+        x[e / F][e % F + 3] *= scale * w.w;
       }
-      float scale = is_q ? a.scale_q : a.scale_k;
-      if (a.norm != LQ_NORM_NONE) {
-        float s = 0.0f;
+    } else {
 #pragma unroll
-        for (int e = 0; e < 2 * F; e++) s = fmaf(x[e / F][e % F], x[e / F][e % F], s);
+      for (int e = 0; e < 2 * F; e++) x[e / F][e % F] *= scale;
+    }
+    if (turned) {                             // pairs: neighbours in either piece, or the pieces element by element
+      float cs[F], sn[F];
 #pragma unroll
-        for (int m = 1; m < LANES; m *= 2) s += __shfl_xor_sync(0xffffffffu, s, m);
-        scale *= rsqrtf((a.norm == LQ_NORM_RMS ? s * (1.0f / DIM) : s) + a.eps);
+      for (int p = 0; p < F; p += 2) {
+        const float4 t = *reinterpret_cast<const float4 *>(turn[r][p / 2][lane]);
+        cs[p] = t.x, sn[p] = t.y, cs[p + 1] = t.z, sn[p + 1] = t.w;
       }
-      if (a.norm == LQ_NORM_RMS) {
+      auto rotate = [](float &p0, float &p1, float cs, float sn) {
+        const float y0 = p0, y1 = p1;
+        p0 = fmaf(y0, cs, -(y1 * sn));
+        p1 = fmaf(y1, cs, y0 * sn);
+      };
+      if (a.pairs) {
 #pragma unroll
-        for (int e = 0; e < 2 * F; e += 4) {
-          const float4 w = *reinterpret_cast<const float4 *>(weight[is_q ? 0 : 1][e / 4][lane]);
-          x[e / F][e % F] *= scale * w.x;
-          x[e / F][e % F + 1] *= scale * w.y;
-          x[e / F][e % F + 2] *= scale * w.z;
-          x[e / F][e % F + 3] *= scale * w.w;
-        }
+        for (int p = 0; p < F; p++) rotate(x[2 * p / F][2 * p % F], x[2 * p / F][2 * p % F + 1], cs[p], sn[p]);
       } else {
 #pragma unroll
-        for (int e = 0; e < 2 * F; e++) x[e / F][e % F] *= scale;
+        for (int p = 0; p < F; p++) rotate(x[0][p], x[1][p], cs[p], sn[p]);
       }
-      if (turned) {                           // pairs: neighbours in either piece, or the pieces element by element
-        float cs[F], sn[F];
-#pragma unroll
-        for (int p = 0; p < F; p += 2) {
-          const float4 t = *reinterpret_cast<const float4 *>(turn[r][p / 2][lane]);
-          cs[p] = t.x, sn[p] = t.y, cs[p + 1] = t.z, sn[p + 1] = t.w;
-        }
-        auto rotate = [](float &p0, float &p1, float cs, float sn) {
-          const float y0 = p0, y1 = p1;
-          p0 = fmaf(y0, cs, -(y1 * sn));
-          p1 = fmaf(y1, cs, y0 * sn);
-        };
-        if (a.pairs) {
-#pragma unroll
-          for (int p = 0; p < F; p++) rotate(x[2 * p / F][2 * p % F], x[2 * p / F][2 * p % F + 1], cs[p], sn[p]);
-        } else {
-#pragma unroll
-          for (int p = 0; p < F; p++) rotate(x[0][p], x[1][p], cs[p], sn[p]);
-        }
-      }
-      if (there && (!a.positions || a.positions[row] >= 0)) {
-        alignas(16) T y[2][F];
-        pack(x[0], y[0]);
-        pack(x[1], y[1]);
-        T *dst = is_q ? static_cast<T *>(a.out_q) + row * a.out_q_stride + h * DIM
-                      : static_cast<T *>(a.out_k) + row * a.out_k_stride + (h - a.heads_q) * DIM;
-        store_row<WIDE>(dst + c0, y[0]);
-        store_row<WIDE>(dst + c1, y[1]);
-      }
+    }
+    if (there && (!a.positions || a.positions[row] >= 0)) {
+      alignas(16) T y[2][F];
+      pack(x[0], y[0]);
+      pack(x[1], y[1]);
+      T *dst = is_q ? static_cast<T *>(a.out_q) + row * a.out_q_stride + h * DIM
+                    : static_cast<T *>(a.out_k) + row * a.out_k_stride + (h - a.heads_q) * DIM;
+      store_row<WIDE>(dst + c0, y[0]);
+      store_row<WIDE>(dst + c1, y[1]);
     }
   }
 }

@@ -80,7 +80,6 @@ __device__ __forceinline__ float scan_fetch(const ScanArgs &a, ScanToken &t, int
   return alpha;
 }
 
-template <typename O>
 __device__ __forceinline__ void scan_emit(const ScanArgs &a, ScanToken &t, float4 o, int64_t row, int h) {
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, tid = threadIdx.x;
   *reinterpret_cast<float4 *>(&t.part[warp][4 * lane]) = o;
@@ -90,7 +89,7 @@ __device__ __forceinline__ void scan_emit(const ScanArgs &a, ScanToken &t, float
 #pragma unroll
     for (int w = 0; w < 8; w++) s += t.part[w][tid];
     if (a.skip) s = fmaf(a.skip[h], t.v[tid], s);
-    static_cast<O *>(a.o)[row * a.o_stride + h * SD + tid] = from_float<O>(s);
+    static_cast<float *>(a.o)[row * a.o_stride + h * SD + tid] = s;
   }
 }
 
@@ -108,7 +107,7 @@ __global__ void __launch_bounds__(256) scan_step_kernel(const ScanArgs a) {
   __syncthreads();
   const float4 o = st.token(alpha, t.bk + 16 * warp, t.q + 16 * warp, *reinterpret_cast<const float4 *>(t.v + 4 * lane));
   st.store(a.S + at, warp, lane);
-  scan_emit<float>(a, t, o, n, h);
+  scan_emit(a, t, o, n, h);
 }
 
 // ---------------------------------------------------------------------------------------------
