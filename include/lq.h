@@ -309,11 +309,15 @@ lq_status lq_ref_decode_step_bf16(const lq_shape *shape, uint16_t *S, const uint
  * token is decoded:
  *     prompt:  lq_conv_prompt -> lq_norm_rotate -> lq_scan_prompt -> lq_quantize_state
  *     token:   lq_conv_step   -> lq_norm_rotate -> lq_decode_step (or, on the dense state, lq_scan_step)
+ * The scans are those of the instances with b = 0 and a scalar decay (lq_shape.delta = 0, LQ_GATE_SCALAR).  For the delta rule and for decays per
+ * key channel nothing here goes from a prompt to its dense state: lq_quantize_state takes one that the caller has made.
+ * lq_decode_step takes dense arrays: slices of rows that lq_conv_step has left are copied in front of it.  It has neither `select` nor `skip`: its beta
+ * and alpha are gates, and the skip is added to its o.
  *
  * Conventions of these entry points, next to those at the top of this file:
  *  - Tokens are ROWS.  The rows of the sequences of a call lie back to back: sequence n has rows seq_start[n] to
  *    seq_start[n+1] - 1 (int32 [seqs + 1] in device memory, not decreasing; rows in front of seq_start[0] and from
- *    seq_start[seqs] on belong to nobody: nothing of them is read or written).  The single-token forms have one row
+ *    seq_start[seqs] on belong to nobody: they are not written, and what they hold does not matter).  The single-token forms have one row
  *    per sequence, row n.
  *  - A row's channels are contiguous, `..._stride` is the distance between rows in elements, at least a row long:
  *    slices of a wider projection are taken as they are.  Such arrays need the alignment of their element type only,
@@ -332,7 +336,8 @@ typedef enum { LQ_BF16 = 0, LQ_F16 = 1, LQ_F32 = 2 } lq_type;
 /*
  * Short causal depthwise convolution with an optional bias and SiLU:
  *     out[t][c] = f( bias[c] + sum_{i < width} w[c][i] x[t - (width-1) + i][c] ),    f(y) = y or y / (1 + exp(-y))
- * in binary32, rounded once to `type`.  Rows in front of the sequence's first are the state's (resumed) or zero.
+ * in binary32, rounded once to `type` (SiLU: within 2^-21 + 2^-23 |y| of itself in front of that, and 0 for y below -87.3, where it is smaller than
+ * 2^-119).  Rows in front of the sequence's first are the state's (resumed) or zero.
  *   x, out : [tokens][channels], strided rows     w : [channels][width]     bias : [channels] or null
  *   state  : [n_slots][width-1][channels], the last width-1 rows of x, oldest first, in and out (lq_conv_prompt: null
  *            if the prompts are fresh and no state is wanted)                                          - all of `type`
@@ -401,7 +406,8 @@ lq_status lq_norm_rotate(const lq_norm *shape, const void *q, int64_t q_stride, 
  *       null: from S.  S itself, or without an element in common with it.
  * lq_scan_prompt: o is bf16.  The outputs are rounded to bf16 once; in front of that the state and the weighted scores of a
  * block of tokens are rounded to bf16 where they enter a product, as the inputs are; S is held and updated in binary32.  A product of decays
- * since the start of a block (128 rows) that is below 2^-126 counts as 0 in S, and as 2^-60 where it is below that in the share S^T q of o.
+ * since the start of a block (128 rows) that is below 2^-126 counts as 0 in S, and as 2^-60 where it is below that in the share S^T q of o; where a long
+ * prompt of few heads is cut, so does one since the start of a piece in S.  Outputs beyond 2^67 may overflow.
  * A NaN or an infinity in a row makes o undefined from the first row of its block (128 rows from the sequence's first on) to
  * the end of its sequence, and S of that sequence; other sequences never see it.
  * lq_scan_step: one row per sequence (tokens = seqs), every sequence is resumed, o is fp32 [seqs][Hv][d_v] in strided rows.

@@ -5,8 +5,9 @@
 // Where channels i and i + rot/2 are a pair, a lane's pieces are one of either half, so that its pairs are its own.  A CTA takes the angles of its
 // rows once for all heads: a frequency in turns as a fraction of 64 bits (from binary64), times the position modulo one turn - whole
 // turns drop out exactly, and what binary32 gets is at most half a turn whatever the position.
-// 16384 rows of 40 heads of 128 bf16 channels, 64 of them rotated: 70 us, 4.8 TB/s (115 us with one row to a CTA, angles in binary64 and
-// partners exchanged between lanes; the same 70 us with half the arithmetic instructions, two channels each: it is the memory's latency and
+// What sincospif gets is a phase of 32 bits, as binary32: off by 2^-25 of a half turn at most.
+// 16384 rows of 40 heads of 128 bf16 channels, 64 of them rotated: 64 us, 5.2 TB/s (115 us with one row to a CTA, angles in binary64 and
+// partners exchanged between lanes; half the arithmetic instructions, two channels each, took as long: it is the memory's latency and
 // the call's start and end that are left); all 128 rotated, in binary32, 125 us, 5.4 TB/s.
 #pragma once
 #include "lq_rows.cuh"

@@ -118,11 +118,11 @@ __global__ void __launch_bounds__(256) scan_step_kernel(const ScanArgs a) {
 // split into three bf16 pieces that add up to all 24 bits - the state stays binary32, at the price of three products for one.  P's
 // weights and S are rounded to bf16 where they enter a product with an output that is itself rounded to bf16.
 //
-// Six products of 2 * 128^3 operations a block and head are 0.26 us each at what one SM has of the measured peak; the 64 KB of v and o (q and
-// k are shared by the heads of a group and come from L2) take 1.5 us at its share of the bandwidth.  Both bounds are
-// close, so everything runs side by side in one CTA per SM, every warp with one part.  Measured: 3.1 us a block where memory is quiet, 4.3 where
+// Six products of 2 * 128^3 operations a block and head are 0.38 us each at what one SM has of the measured peak (0.26 us, 512 clocks, at the
+// tensor pipe's own rate): 2.3 us (1.6).  The 64 KB of v and o (q and k are shared by the heads of a group and come from L2) take 1.5 us at its
+// share of the bandwidth.  Both bounds are close, so everything runs side by side in one CTA per SM, every warp with one part.  Measured: 3.1 us a block where memory is quiet, 4.3 where
 // all SMs load (8 prompts x 2048 rows x 32 heads: 122 us, 3.3 TB/s; the tensor pipe is active 48 % of the time).  What bounds it are the hand-overs
-// between the parts and the fetching of their code.
+// between the parts and the fetching of their code.  (The compiler spills 56 bytes a thread in the instances with outputs, 40 in those without.)
 //   warp 0       takes the next head and tells the others; tensor copies of the tiles of 32 KB, two slots each for K, Q and V
 //   warp 1       the products for the outputs: P, S^T q, weighted P times V
 //   warp 2       the block's gates: log decays, their sums, weights
@@ -175,7 +175,7 @@ struct ScanWeights {
   float rest[4];                               // exp(G_C - G at the end of every 32 rows)
   float total, pad[3];                         // exp(G_C)
 };
-struct ScanShared {                            // (all but 96 bytes of what a CTA can have)
+struct ScanShared {                            // (all but 24 bytes of what a CTA can have)
   uint8_t k[2][TILE], q[2][TILE], v[2][TILE];
   uint8_t s16[TILE];                           // S as bf16: rows of value channels, two halves of 64 key channels
   ScanSums sums;

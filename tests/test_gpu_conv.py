@@ -151,3 +151,18 @@ def test_large_strides_and_rows_beyond_32_bits():
     want, scale, after = ops_ref.conv(vals, w, bias, state, [0, rows], None, None, 1)
     check_rows(out.cpu(), want, scale, torch.bfloat16)
     assert torch.equal(st.cpu(), after)
+
+
+@pytest.mark.parametrize("channels", [64, 63])
+def test_silu_over_its_range(channels):
+    """y / (1 + exp(-y)) in binary32: exp2 to 2^-22, its argument -y log2(e) rounded twice (|y| (2^-24 + 2^-25)), 1 + exp to 2^-24, the reciprocal to 2^-23, the
+    product to 2^-24: below 2^-21 + 2^-23 |y| of the value together.  Where exp(-y) has no reciprocal of 2^-126 or more the result is 0."""
+    y = torch.cat([torch.linspace(-130, 130, 4097), torch.linspace(-90, -84, 1024), 10.0 ** torch.linspace(-30, 30, 128), -(10.0 ** torch.linspace(-30, 30, 128))])
+    y = y[:y.numel() // channels * channels].view(-1, channels).contiguous()
+    w = torch.tensor([0.0, 1.0]).repeat(channels, 1)
+    out = torch.empty(y.shape, device="cuda")
+    lq.conv_prompt(lq.ConvShape(y.shape[0], 1, channels, width=2, type=lq.F32), y.cuda(), w.cuda(), None, None, out, torch.tensor([0, y.shape[0]], dtype=torch.int32).cuda())
+    want = y.double() * torch.sigmoid(y.double())
+    off = (out.cpu().double() - want).abs()
+    assert (off <= (2.0 ** -21 + 2.0 ** -23 * y.double().abs()) * want.abs() + 2.0 ** -119).all()
+    assert (out.cpu()[y < -87.4] == 0).all()
