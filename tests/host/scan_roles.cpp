@@ -5,7 +5,8 @@
 // are as the hardware has them: a wait looks at a parity only, and who does not get his turn while a phase lasts has missed it.
 //
 // Tiles, tensor memory and states hold tags and small numbers in place of data.  A block's share of the state is a number of its head and
-// row, q reads the state as it is, and the weighted scores add 1/2: outputs and states are compared with sums over the blocks.  Apart
+// row, its first row decays by 1 or 1/2, q reads the state as it is, and the weighted scores add 1/2: outputs and states are compared with the
+// recurrence over the blocks.  Apart
 // from that, nothing that an instruction under way reads may change, nothing it writes may be looked at, and everybody has to come to the end.
 //
 // Usage: scan_roles FIRST_SEED SEEDS
@@ -143,7 +144,9 @@ static uint64_t seen(int i) {
   return x;
 }
 
-static float value_of(Tag t) { return 1 + (t.head * 7 + t.row / 16) % 13; }
+// (with at most three blocks and states up to 7, sums have five bits and three behind the point: exact as bf16)
+static float value_of(Tag t) { return 1 + (t.head * 5 + t.row / 16) % 7; }
+static float decay_of(int head, int row) { return (head + row / 16) % 3 ? 1.0f : 0.5f; }   // of the block that starts there
 
 struct {
   Tag tag;
@@ -409,7 +412,10 @@ static void run(unsigned seed) {
   const int tokens = start.back() + pick(3);
   what = "seed " + std::to_string(seed) + ", " + std::to_string(hv) + " heads of" + list + ", " + std::to_string(pieces) + " pieces, " + std::to_string(ctas) + " CTAs";
   const size_t SS = SD * SD;
-  std::vector<__nv_bfloat16> gates((tokens + 1) * hv, __float2bfloat16_rn(1.0f));
+  std::vector<__nv_bfloat16> beta((tokens + 1) * hv, __float2bfloat16_rn(1.0f)), alpha = beta;
+  for (int n = 0; n < seqs; n++)
+    for (int row = start[n]; row < start[n + 1]; row += SB)
+      for (int h = 0; h < hv; h++) alpha[row * hv + h] = __float2bfloat16_rn(decay_of(h, row));
   const int64_t o_stride = hv * SD + 8;       // (rows that are not whole sectors)
   std::vector<uint4> o_mem((tokens + 1) * o_stride / 8 + 1);
   memset(o_mem.data(), 0xFF, o_mem.size() * 16);
@@ -429,7 +435,7 @@ static void run(unsigned seed) {
   if (pick(2)) plan.next = &taken;
   ScanArgs a{};
   a.q_stride = a.k_stride = hq * SD, a.v_stride = hv * SD, a.beta_stride = a.alpha_stride = hv, a.o_stride = o_stride;
-  a.beta = a.alpha = gates.data();
+  a.beta = beta.data(), a.alpha = alpha.data();
   a.S0 = a.S = S.data(), a.o = o;
   a.sq = {start.data(), slots.data(), resume.data(), tokens, seqs, seqs};
   a.heads_v = hv, a.heads_qk = hq, a.max_len = longest;
@@ -454,10 +460,11 @@ static void run(unsigned seed) {
           written[r] = 1;
           for (int c = 0; c < SD; c++) {
             const float got = __bfloat162float(o[(int64_t)r * o_stride + h * SD + c]);
-            CHECK(got == s + 0.5f, "row %d of head %d is %g, not %g", r, h, got, s + 0.5f);
+            const float want = (s + 0.5f) * (r == row ? decay_of(h, row) : 1);   // (lane 0 of the gates' warp has a block's first four rows)
+            CHECK(got == want, "row %d of head %d is %g, not %g", r, h, got, want);
           }
         }
-        s += value_of({h, row});
+        s = s * decay_of(h, row) + value_of({h, row});
       }
       for (int c = 0; c < SD; c += 32)
         for (int j = 0; j < SD; j++) CHECK(S[at + j * SD + c] == s, "the state of sequence %d, head %d is %g, not %g", n, h, S[at + j * SD + c], s);
