@@ -309,6 +309,8 @@ lq_status lq_ref_decode_step_bf16(const lq_shape *shape, uint16_t *S, const uint
  * token is decoded:
  *     prompt:  lq_conv_prompt -> lq_norm_rotate -> lq_scan_prompt -> lq_quantize_state
  *     token:   lq_conv_step   -> lq_norm_rotate -> lq_decode_step (or, on the dense state, lq_scan_step)
+ * In front of and behind either, from the residual stream and back to it, with activations and weights in 8 bits:
+ *     lq_norm_add -> lq_product (projections) -> ... -> lq_norm_gate -> lq_product (output projection) -> lq_norm_add ...
  * The scans are those of the instances with b = 0 and a scalar decay (lq_shape.delta = 0, LQ_GATE_SCALAR).  For the delta rule and for decays per
  * key channel nothing here goes from a prompt to its dense state: lq_quantize_state takes one that the caller has made.
  * lq_decode_step takes dense arrays: slices of rows that lq_conv_step has left are copied in front of it.  It has neither `select` nor `skip`: its beta
@@ -442,9 +444,82 @@ lq_status lq_scan_prompt(const lq_scan *shape, const lq_scan_io *io, uint16_t *o
 lq_status lq_scan_step(const lq_scan *shape, const lq_scan_io *io, float *o, int64_t o_stride, lq_stream stream);
 
 /*
+ * ---- The 8-bit linear layer: norms that leave e4m3 rows, products that take them -------------------------------
+ *
+ * A row of e4m3 codes has a scale for every block of 128 consecutive channels (the last block of a row may be shorter):
+ *     value = code * scale,     scale = max(max_block |y|, 448 * 2^-100) / 448,     code = y / scale rounded to e4m3 (nearest even)
+ * scale lies block by block: fp32 [ceil(channels/128)][scale_stride], the scales of neighbouring rows side by side, scale_stride at least
+ * the number of rows.  A block with an infinity stands for NaN throughout, a NaN for itself alone.  Codes are the 8-bit patterns of e4m3
+ * (torch.float8_e4m3fn).
+ *
+ * lq_norm_add: the residual's addition and the norm of whole rows, in one pass:
+ *     h = x + residual,  residual <- h,    y = norm(h) * w,     norm: LQ_NORM_NONE, LQ_NORM_L2 or LQ_NORM_RMS over `dim` channels
+ * in binary32 (y from h before it is rounded); residual and out are rounded to `type` once, out8 and scale as above.
+ *   x, out, residual : [tokens][dim] of `type`, strided rows; residual null: h = x.  out may be x (same pointer and stride)
+ *   out8             : e4m3 [tokens][dim], strided rows, with `scale`.  Either out or out8 may be null
+ *   w                : fp32 [dim] or null (1; LQ_NORM_RMS only)
+ * dim at most LQ_NORM_ADD_MOST.  With LQ_NORM_NONE and no residual it turns rows of any origin into 8-bit ones.
+ */
+#define LQ_NORM_ADD_MOST 16384
+typedef struct {
+  int tokens;
+  int dim;
+  int norm;
+  int type;    /* lq_type of x, residual and out */
+  float eps;
+} lq_add;
+lq_status lq_norm_add(const lq_add *shape, const void *x, int64_t x_stride, void *residual, int64_t residual_stride, const float *w,
+                      void *out, int64_t out_stride, uint8_t *out8, int64_t out8_stride, float *scale, int64_t scale_stride, lq_stream stream);
+
+/*
+ * lq_norm_gate: the outputs of the recurrence normalised per head, weighted and gated:
+ *     y = norm(o) * w * f(z),     f(z) = z / (1 + exp(-z)) (silu) or 1 / (1 + exp(-z))
+ * in binary32 (f: within 2^-21 + 2^-23 |z| of itself, relative, and 0 where it is below 2^-119), outputs as in lq_norm_add with rows of heads * dim channels.
+ *   o : [tokens][heads][dim] of `o_type` - binary32 from lq_decode_step and lq_scan_step, bf16 from lq_scan_prompt; strided rows
+ *   z : [tokens][heads][dim] of `type`, strided rows      w : fp32 [dim] or null (1; LQ_NORM_RMS only)
+ * No output may overlap an input.
+ */
+typedef struct {
+  int tokens, heads;
+  int dim;     /* channels of a head: 64, 128 or 256 */
+  int norm;
+  int silu;
+  int o_type;  /* lq_type of o          */
+  int type;    /* lq_type of z and out  */
+  float eps;
+} lq_gated;
+lq_status lq_norm_gate(const lq_gated *shape, const void *o, int64_t o_stride, const void *z, int64_t z_stride, const float *w,
+                       void *out, int64_t out_stride, uint8_t *out8, int64_t out8_stride, float *scale, int64_t scale_stride, lq_stream stream);
+
+/*
+ * lq_product: rows of e4m3 codes times e4m3 weights, whose scales are of blocks of 128 output by 128 input channels:
+ *     out[t][n] = sum_b x_scale[b][t] w_scale[n/128][b] sum_{k in block b} x[t][k] w[n][k]
+ * The sum over a block is the tensor cores' (binary32 accumulator), the sum over blocks binary32; rounded once to `type`.
+ *   x   : e4m3 [rows][in], strided rows, 16-byte aligned, stride a multiple of 16      x_scale : fp32 [ceil(in/128)][x_scale_stride]
+ *   w   : e4m3 [out][in], dense, 16-byte aligned                                       w_scale : fp32 [ceil(out/128)][ceil(in/128)]
+ *   out : [rows][out] of `type`, strided rows
+ * `in` is a multiple of 16.
+ * lq_product_groups: the rows of group g, group_start[g] to group_start[g+1] - 1 (int32 [groups + 1] in device memory, not decreasing), take
+ * weight g: w [groups][out][in], w_scale [groups][ceil(out/128)][ceil(in/128)].  Groups may be empty; rows in front of group_start[0] and from
+ * group_start[groups] on belong to nobody: they are not written, and what they hold does not matter.  At most LQ_MOST_GROUPS groups.
+ * out must not overlap an input.  The order of all sums depends on the shapes and on group_start alone: the same call gives the same bits again.
+ */
+#define LQ_MOST_GROUPS 1024
+typedef struct {
+  int rows;
+  int in, out;  /* channels                  */
+  int groups;   /* lq_product: 1             */
+  int type;     /* lq_type of out            */
+} lq_linear;
+lq_status lq_product(const lq_linear *shape, const uint8_t *x, int64_t x_stride, const float *x_scale, int64_t x_scale_stride, const uint8_t *w,
+                     const float *w_scale, void *out, int64_t out_stride, lq_stream stream);
+lq_status lq_product_groups(const lq_linear *shape, const uint8_t *x, int64_t x_stride, const float *x_scale, int64_t x_scale_stride, const uint8_t *w,
+                            const float *w_scale, void *out, int64_t out_stride, const int32_t *group_start, lq_stream stream);
+
+/*
  * Device-side error flags of the current device (0 = none), written to *flags (a host pointer).  Waits inside
- * the kernels are bounded; bit 0 is set when a warp gave up waiting for its asynchronous copies (lq_scan_prompt: or products), bit 1 when
- * lq_scan_prompt did not find its shared or tensor memory where it counts on it (it then did nothing).  After
+ * the kernels are bounded; bit 0 is set when a warp gave up waiting for its asynchronous copies (lq_scan_prompt, lq_product: or products), bit 1 when
+ * one of these two did not find its shared or tensor memory where it counts on it (it then did nothing).  After
  * that, neither the outputs of that launch NOR THE STATE it worked on are valid (records may be missing or
  * half written): restore the state from a checkpoint.  Bit 3 belongs to lq_selftest_bounded_wait; the
  * others are not used.

@@ -15,7 +15,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblq.so")
 # the same library with per-CTA time stamps compiled in (a development aid: bench.py --timeline reads them)
 LIB_STAMPS = os.path.join(HERE, "liblq_stamps.so")
-SOURCES = ["lq_api.cu", "lq_ops.cu"]
+SOURCES = ["lq_api.cu", "lq_ops.cu", "lq_linear.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-fmad=false", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
 

@@ -1,0 +1,226 @@
+// C boundary of the 8-bit linear layer around the decode step: argument checks and launches.  Declarations and contracts: include/lq.h.
+#include <algorithm>
+#include <atomic>
+
+#include "lq_host.h"
+#include "lq_product.cuh"
+#include "lq_rownorm.cuh"
+
+namespace lq {
+
+// ---- norms ----
+
+// The memory from the first to the last element of an array of strided rows.
+struct Span {
+  const void *p;
+  int64_t stride;
+  long width, rows;
+  unsigned size;                               // bytes of an element
+};
+static bool spans_meet(const Span &a, const Span &b) {
+  if (!a.p || !b.p) return false;
+  if (a.rows == b.rows) return rows_overlap(a.p, a.stride * a.size, a.width * a.size, b.p, b.stride * b.size, b.width * b.size, a.rows, 1);
+  return meets_rows(a.p, ((a.rows - 1) * (uint64_t)a.stride + a.width) * a.size, b.p, b.stride, b.width, b.rows, b.size);
+}
+
+struct NormIo {
+  const void *in[2];                           // x and the residual, or o and z
+  int64_t in_stride[2];
+  unsigned in_size[2];
+  bool written;                                // the second input is an output too
+  const float *w;
+  NormOut o;
+};
+
+static lq_status check_norm_io(const NormIo &io, long tokens, long width, int type, bool in_place) {
+  lq_status rc;
+  const unsigned size = type_size(type);
+  if ((rc = check_arrays(io.in_size[0], {io.in[0]})) != LQ_OK) return rc;
+  if ((rc = check_arrays(io.in_size[1], {}, {io.in[1]})) != LQ_OK) return rc;
+  if ((rc = check_arrays(size, {}, {io.o.out})) != LQ_OK) return rc;
+  if ((rc = check_arrays(4, {}, {io.w, io.o.scale})) != LQ_OK) return rc;
+  if ((!io.o.out && !io.o.out8) || (io.o.out8 && !io.o.scale)) return LQ_ERR_NULL;
+  for (int i = 0; i < 2; i++)
+    if (io.in[i] && io.in_stride[i] < width) return LQ_ERR_SHAPE;
+  if ((io.o.out && io.o.out_stride < width) || (io.o.out8 && (io.o.out8_stride < width || io.o.scale_stride < tokens))) return LQ_ERR_SHAPE;
+  const Span in[2] = {{io.in[0], io.in_stride[0], width, tokens, io.in_size[0]}, {io.in[1], io.in_stride[1], width, tokens, io.in_size[1]}};
+  const Span out[3] = {{io.o.out, io.o.out_stride, width, tokens, size},
+                       {io.o.out8, io.o.out8_stride, width, tokens, 1},
+                       {io.o.out8 ? io.o.scale : nullptr, io.o.scale_stride, tokens, ceil_div(width, 128), 4}};
+  if (io.written && spans_meet(in[0], in[1])) return LQ_ERR_UNSUPPORTED;
+  for (int i = 0; i < 3; i++) {
+    for (int j = 0; j < 2; j++)
+      if (!(in_place && i == 0 && j == 0 && out[0].p == in[0].p && out[0].stride == in[0].stride) && spans_meet(out[i], in[j])) return LQ_ERR_UNSUPPORTED;
+    for (int j = 0; j < i; j++)
+      if (spans_meet(out[i], out[j])) return LQ_ERR_UNSUPPORTED;
+  }
+  return LQ_OK;
+}
+
+// Whether all rows can be taken in pieces of eight elements.
+static bool wide_norm(const NormIo &io, long width, int type) {
+  bool wide = width % LINE == 0 && aligned(io.w, 16) && aligned(io.o.out, 16) && aligned(io.o.out8, 8);
+  const long elements = 16 / type_size(type);
+  for (int i = 0; i < 2; i++) wide = wide && aligned(io.in[i], 16) && (!io.in[i] || io.in_stride[i] % (16 / io.in_size[i]) == 0);
+  return wide && (!io.o.out || io.o.out_stride % elements == 0) && (!io.o.out8 || io.o.out8_stride % LINE == 0);
+}
+
+template <typename T, bool WIDE>
+static lq_status launch_add(const AddArgs &a, cudaStream_t stream) {
+  int threads = 32;
+  while (threads < 512 && threads * LINE < a.dim) threads *= 2;
+  const int v = (int)ceil_div(a.dim, threads * LINE), rows = std::max(1, 256 / threads);
+  const dim3 block(threads, rows);
+  const long grid = ceil_div(a.tokens, rows);
+  if (v == 1) norm_add_kernel<T, WIDE, 1><<<grid, block, 0, stream>>>(a);
+  else if (v == 2) norm_add_kernel<T, WIDE, 2><<<grid, block, 0, stream>>>(a);
+  else norm_add_kernel<T, WIDE, 4><<<grid, block, 0, stream>>>(a);
+  return launched();
+}
+
+template <typename X, typename T>
+static lq_status launch_gate(GatedArgs a, bool wide, cudaStream_t stream) {
+  const long grid = ceil_div((long)a.tokens * a.warps, GATED_THREADS / 32);
+  if (wide) norm_gate_kernel<X, T, true><<<grid, GATED_THREADS, 0, stream>>>(a);
+  else norm_gate_kernel<X, T, false><<<grid, GATED_THREADS, 0, stream>>>(a);
+  return launched();
+}
+template <typename X>
+static lq_status launch_gate(const GatedArgs &a, int type, bool wide, cudaStream_t stream) {
+  if (type == LQ_F32) return launch_gate<X, float>(a, wide, stream);
+  if (type == LQ_F16) return launch_gate<X, __half>(a, wide, stream);
+  return launch_gate<X, __nv_bfloat16>(a, wide, stream);
+}
+
+// ---- products ----
+
+constexpr int SMS = 148, MOST_CHANNELS = 1 << 20;
+
+// [planes][rows][channels] bytes, copied in boxes of `box` rows of 128 channels of one plane
+static bool byte_map(CUtensorMap *map, const void *base, long channels, long rows, long planes, int64_t stride, int64_t plane, int box) {
+  const cuuint64_t size[3] = {(cuuint64_t)channels, (cuuint64_t)rows, (cuuint64_t)planes}, strides[2] = {(cuuint64_t)stride, (cuuint64_t)plane};
+  const cuuint32_t shape[3] = {PB, (cuuint32_t)box, 1}, one[3] = {1, 1, 1};
+  const EncodeTiled f = encode_tiled();
+  return f && f(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void *>(base), size, strides, shape, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename K>
+static lq_status give_shared(K kernel, size_t bytes, std::atomic<uint64_t> &ready) {   // ready: devices on which the kernel has its shared memory
+  int device = 0;
+  if (cudaGetDevice(&device) != cudaSuccess) return LQ_ERR_CUDA;
+  const uint64_t bit = uint64_t(1) << (device & 63);
+  if (ready.load(std::memory_order_relaxed) & bit) return LQ_OK;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) {
+    cudaGetLastError();
+    return LQ_ERR_CUDA;
+  }
+  ready.fetch_or(bit, std::memory_order_relaxed);
+  return LQ_OK;
+}
+
+template <int T>
+static lq_status launch_few(const lq_linear *s, ProductArgs a, const void *x, int64_t x_stride, const void *w, cudaStream_t stream) {
+  static std::atomic<uint64_t> ready{0};
+  constexpr size_t smem = sizeof(FewShared<T>);
+  const lq_status rc = give_shared(product_few_kernel<T>, smem, ready);
+  if (rc != LQ_OK) return rc;
+  a.tiles_n = (int)ceil_div(s->out, PB);
+  ProductMaps maps;
+  if (!byte_map(&maps.x, x, s->in, s->rows, 1, x_stride, x_stride * s->rows, T) ||
+      !byte_map(&maps.w, w, s->in, s->out, s->groups, s->in, (int64_t)s->in * s->out, PB))
+    return LQ_ERR_CUDA;
+  const long tiles = (ceil_div(s->rows, T) + s->groups - 1) * a.tiles_n;   // at most
+  product_few_kernel<T><<<(int)std::min<long>(tiles, SMS), FEW_THREADS, smem, stream>>>(maps, a);
+  return launched();
+}
+
+static lq_status product(const lq_linear *s, const uint8_t *x, int64_t x_stride, const float *x_scale, int64_t x_scale_stride, const uint8_t *w,
+                         const float *w_scale, void *out, int64_t out_stride, const int32_t *group_start, bool grouped, lq_stream stream) {
+  lq_status rc;
+  if (!s) return LQ_ERR_NULL;
+  if (bad_count(s->rows) || s->in <= 0 || s->out <= 0 || s->groups <= 0 || s->type < LQ_BF16 || s->type > LQ_F32) return LQ_ERR_SHAPE;
+  if (!grouped && s->groups != 1) return LQ_ERR_SHAPE;
+  if (s->in % 16 != 0 || s->in > MOST_CHANNELS || s->out > MOST_CHANNELS || s->groups > MOST_GROUPS || s->rows > MOST_ROWS) return LQ_ERR_UNSUPPORTED;
+  if ((ceil_div(s->rows, 16) + s->groups) * ceil_div(s->out, PB) > INT32_MAX - 1024) return LQ_ERR_UNSUPPORTED;   // tiles
+  if (s->rows == 0) return LQ_OK;
+  if ((rc = check_arrays(16, {x, w})) != LQ_OK) return rc;
+  if ((rc = check_arrays(4, {x_scale, w_scale})) != LQ_OK) return rc;
+  if ((rc = check_arrays(type_size(s->type), {out})) != LQ_OK) return rc;
+  if (grouped && !group_start) return LQ_ERR_NULL;
+  if (!aligned(group_start, 4)) return LQ_ERR_ALIGN;
+  if (x_stride < s->in || x_scale_stride < s->rows || out_stride < s->out) return LQ_ERR_SHAPE;
+  if (x_stride % 16 != 0) return LQ_ERR_ALIGN;
+  if (x_stride > (int64_t)1 << 32 || x_stride * s->rows >= (int64_t)1 << 40) return LQ_ERR_UNSUPPORTED;   // (what a tensor map can say)
+  const unsigned size = type_size(s->type);
+  const int blocks = (int)ceil_div(s->in, PB);
+  const Span o{out, out_stride, s->out, s->rows, size};
+  for (const Span &in : {Span{x, x_stride, s->in, s->rows, 1}, Span{x_scale, x_scale_stride, s->rows, blocks, 4},
+                         Span{w, s->in, s->in, (long)s->out * s->groups, 1}, Span{w_scale, blocks, blocks, ceil_div(s->out, PB) * s->groups, 4}})
+    if (spans_meet(o, in)) return LQ_ERR_UNSUPPORTED;
+  const ProductArgs a{x_scale, w_scale, out, x_scale_stride, out_stride, group_start, s->rows, blocks, s->out, s->groups, s->type, 0};
+  return launch_few<128>(s, a, x, x_stride, w, cuda_stream(stream));
+}
+
+// lq_check_device / lq_clear_device_flags: the flag of the kernels in this file
+bool linear_flags(int *flags) { return cudaMemcpyFromSymbol(flags, g_product_error, sizeof(int)) == cudaSuccess; }
+bool clear_linear_flags() {
+  const int zero = 0;
+  return cudaMemcpyToSymbol(g_product_error, &zero, sizeof(int)) == cudaSuccess;
+}
+
+}  // namespace lq
+
+using namespace lq;
+
+extern "C" {
+
+lq_status lq_norm_add(const lq_add *s, const void *x, int64_t x_stride, void *residual, int64_t residual_stride, const float *w, void *out,
+                      int64_t out_stride, uint8_t *out8, int64_t out8_stride, float *scale, int64_t scale_stride, lq_stream stream) {
+  if (!s) return LQ_ERR_NULL;
+  if (bad_count(s->tokens) || s->dim <= 0 || s->norm < LQ_NORM_NONE || s->norm > LQ_NORM_RMS || s->type < LQ_BF16 || s->type > LQ_F32) return LQ_ERR_SHAPE;
+  if (s->dim > LQ_NORM_ADD_MOST || s->tokens > MOST_ROWS) return LQ_ERR_UNSUPPORTED;
+  if (s->tokens == 0) return LQ_OK;
+  const unsigned size = type_size(s->type);
+  const NormIo io{{x, residual}, {x_stride, residual_stride}, {size, size}, true, w, {out, out8, scale, out_stride, out8_stride, scale_stride}};
+  const lq_status rc = check_norm_io(io, s->tokens, s->dim, s->type, true);
+  if (rc != LQ_OK) return rc;
+  const AddArgs a{x, residual, w, x_stride, residual_stride, io.o, s->tokens, s->dim, s->norm, s->eps};
+  const bool wide = wide_norm(io, s->dim, s->type);
+  if (s->type == LQ_F32) return wide ? launch_add<float, true>(a, cuda_stream(stream)) : launch_add<float, false>(a, cuda_stream(stream));
+  if (s->type == LQ_F16) return wide ? launch_add<__half, true>(a, cuda_stream(stream)) : launch_add<__half, false>(a, cuda_stream(stream));
+  return wide ? launch_add<__nv_bfloat16, true>(a, cuda_stream(stream)) : launch_add<__nv_bfloat16, false>(a, cuda_stream(stream));
+}
+
+lq_status lq_norm_gate(const lq_gated *s, const void *o, int64_t o_stride, const void *z, int64_t z_stride, const float *w, void *out,
+                       int64_t out_stride, uint8_t *out8, int64_t out8_stride, float *scale, int64_t scale_stride, lq_stream stream) {
+  if (!s) return LQ_ERR_NULL;
+  if (bad_count(s->tokens) || s->heads <= 0 || s->dim <= 0 || s->norm < LQ_NORM_NONE || s->norm > LQ_NORM_RMS) return LQ_ERR_SHAPE;
+  if ((s->silu != 0 && s->silu != 1) || s->type < LQ_BF16 || s->type > LQ_F32 || s->o_type < LQ_BF16 || s->o_type > LQ_F32) return LQ_ERR_SHAPE;
+  const long warps = ceil_div((long)s->heads * s->dim, 32 * LINE);
+  if ((s->dim != 64 && s->dim != 128 && s->dim != 256) || s->heads > (1 << 16) || warps * s->tokens > MOST_ROWS) return LQ_ERR_UNSUPPORTED;
+  if (s->tokens == 0) return LQ_OK;
+  if (!z) return LQ_ERR_NULL;
+  const long width = (long)s->heads * s->dim;
+  const NormIo io{{o, z}, {o_stride, z_stride}, {type_size(s->o_type), type_size(s->type)}, false, w, {out, out8, scale, out_stride, out8_stride, scale_stride}};
+  const lq_status rc = check_norm_io(io, s->tokens, width, s->type, false);
+  if (rc != LQ_OK) return rc;
+  GatedArgs a{o, z, w, o_stride, z_stride, io.o, s->tokens, s->heads, s->dim, s->norm, s->silu, s->eps, (int)warps, {}};
+  a.by_warps.set((uint32_t)warps);
+  const bool wide = wide_norm(io, width, s->type);
+  if (s->o_type == LQ_F32) return launch_gate<float>(a, s->type, wide, cuda_stream(stream));
+  if (s->o_type == LQ_F16) return launch_gate<__half>(a, s->type, wide, cuda_stream(stream));
+  return launch_gate<__nv_bfloat16>(a, s->type, wide, cuda_stream(stream));
+}
+
+lq_status lq_product(const lq_linear *shape, const uint8_t *x, int64_t x_stride, const float *x_scale, int64_t x_scale_stride, const uint8_t *w,
+                     const float *w_scale, void *out, int64_t out_stride, lq_stream stream) {
+  return product(shape, x, x_stride, x_scale, x_scale_stride, w, w_scale, out, out_stride, nullptr, false, stream);
+}
+
+lq_status lq_product_groups(const lq_linear *shape, const uint8_t *x, int64_t x_stride, const float *x_scale, int64_t x_scale_stride, const uint8_t *w,
+                            const float *w_scale, void *out, int64_t out_stride, const int32_t *group_start, lq_stream stream) {
+  return product(shape, x, x_stride, x_scale, x_scale_stride, w, w_scale, out, out_stride, group_start, true, stream);
+}
+
+}  // extern "C"

@@ -1,57 +1,13 @@
 // C boundary of the operators around the decode step: argument checks and launches.  Declarations and contracts: include/lq.h.
 #include <algorithm>
 #include <atomic>
-#include <initializer_list>
 
 #include "lq_conv.cuh"
+#include "lq_host.h"
 #include "lq_norm.cuh"
 #include "lq_scan.cuh"
 
 namespace lq {
-
-static cudaStream_t cuda_stream(lq_stream s) { return reinterpret_cast<cudaStream_t>(s); }
-
-static bool aligned(const void *p, unsigned bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
-
-static lq_status launched() { return cudaGetLastError() == cudaSuccess ? LQ_OK : LQ_ERR_CUDA; }
-
-static unsigned type_size(int type) { return type == LQ_F32 ? 4 : 2; }
-
-static long ceil_div(long a, long b) { return (a + b - 1) / b; }
-
-static bool bad_count(int n) { return n < 0; }
-
-// Row and sequence numbers up to a tile or a CTA beyond the last one are formed in 32 bits.
-constexpr int MOST_ROWS = INT32_MAX - 1023;
-
-// Required and optional (may be null) arrays with elements of `bytes` bytes.
-static lq_status check_arrays(unsigned bytes, std::initializer_list<const void *> required, std::initializer_list<const void *> optional = {}) {
-  for (const void *p : required) {
-    if (!p) return LQ_ERR_NULL;
-    if (!aligned(p, bytes)) return LQ_ERR_ALIGN;
-  }
-  for (const void *p : optional)
-    if (!aligned(p, bytes)) return LQ_ERR_ALIGN;
-  return LQ_OK;
-}
-
-// Whether two arrays of strided rows have an element in common.  Exact where the strides are equal (slices of one buffer), else
-// by the ranges they span.
-static bool rows_overlap(const void *a, int64_t sa, long wa, const void *b, int64_t sb, long wb, long rows, unsigned bytes) {
-  if (rows <= 0) return false;
-  const intptr_t x = reinterpret_cast<intptr_t>(a), y = reinterpret_cast<intptr_t>(b);
-  const intptr_t ex = x + ((rows - 1) * sa + wa) * (intptr_t)bytes, ey = y + ((rows - 1) * sb + wb) * (intptr_t)bytes;
-  if (ex <= y || ey <= x) return false;
-  if (sa != sb) return true;
-  const intptr_t period = sa * (intptr_t)bytes, d = ((y - x) % period + period) % period;   // b's rows start d bytes into a's
-  return d < wa * (intptr_t)bytes || d + wb * (intptr_t)bytes > period;
-}
-
-// Whether `bytes` bytes at p, without gaps, meet the range of those strided rows.
-static bool meets_rows(const void *p, uint64_t bytes, const void *a, int64_t sa, long wa, long rows, unsigned size) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(p), y = reinterpret_cast<uintptr_t>(a);
-  return rows > 0 && x < y + ((rows - 1) * (uint64_t)sa + wa) * size && y < x + bytes;
-}
 
 // ---- short causal convolution ----
 
@@ -238,20 +194,6 @@ static uint64_t scan_bytes(const lq_scan *s) {
   const ScanPlan plan = scan_plan(s, base);
   const uint64_t front = reinterpret_cast<char *>(plan.states) - base;
   return front + (plan.pieces > 1 ? (uint64_t)plan.items * (SD * SD + 1) * sizeof(float) : 0);
-}
-
-using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
-                                 const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-static EncodeTiled encode_tiled() {
-  static const EncodeTiled f = [] {
-    void *p = nullptr;
-    cudaDriverEntryPointQueryResult found;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) p = nullptr;
-    cudaGetLastError();
-    return reinterpret_cast<EncodeTiled>(p);
-  }();
-  return f;
 }
 
 // [rows][heads][128] bf16 with strided rows, copied in boxes of SB rows of 64 channels of one head

@@ -1,0 +1,258 @@
+// Products of e4m3 rows with e4m3 weights, scales for each 128 channels of a row and for each block of 128 x 128 of the weights:
+//     out[t][n] = sum_b xs[b][t] ws[n / 128][b] sum_{k in block b} x[t][k] w[n][k]
+#pragma once
+#include "lq_rows.cuh"
+#include "lq_tensor.cuh"
+
+namespace lq {
+
+constexpr int PB = 128;                        // channels (and outputs) of a scale; a K block
+constexpr int MOST_GROUPS = LQ_MOST_GROUPS;
+
+__device__ int g_product_error = 0;
+constexpr int PRODUCT_WAIT_LIMIT = 1 << 20;    // tries of a wait
+
+// Bounded wait; false: it ran out, leave (everybody else's next wait will too).
+__device__ __forceinline__ bool reached(uint32_t bar, uint32_t parity) {
+  int left = PRODUCT_WAIT_LIMIT;
+#pragma unroll 1
+  while (!bar_try(bar, parity))
+    if (--left == 0) return false;
+  return true;
+}
+__device__ __forceinline__ bool all_reached(uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, reached(bar, parity)); }
+
+struct ProductMaps {
+  CUtensorMap x, w;
+};
+struct ProductArgs {
+  const float *x_scale, *w_scale;
+  void *out;
+  int64_t x_scale_stride, out_stride;
+  const int32_t *group_start;                  // null: one group of all rows
+  int rows, blocks, outs, groups, type;        // blocks: K blocks; outs: output channels
+  int tiles_n;                                 // tiles of output channels
+};
+
+// The tiles of all groups: a group's tiles of rows, for one tile of output channels after another (those that run at the same time have
+// their weights in common).  What group_start holds is brought into [0, rows] and into order here: nothing outside of the arrays is
+// touched whatever it holds.
+struct GroupTiles {
+  int first[MOST_GROUPS + 1];                  // tiles of rows in front of a group
+  int start[MOST_GROUPS + 1];
+
+  // all threads of the CTA; `rows_per_tile` of T
+  __device__ __forceinline__ void find(const ProductArgs &a, int T) {
+    for (int g = threadIdx.x; g <= a.groups; g += blockDim.x) start[g] = a.group_start ? min(max(a.group_start[g], 0), a.rows) : g ? a.rows : 0;
+    __syncthreads();
+    if (threadIdx.x < 32) {                    // (running maximum, running sum; 32 groups at a time)
+      const int lane = threadIdx.x;
+      int high = start[0], sum = 0;
+      for (int g0 = 0; g0 < a.groups; g0 += 32) {
+        const int g = g0 + lane;
+        int s = g < a.groups ? start[g + 1] : 0;
+        s = max(s, high);
+#pragma unroll
+        for (int m = 1; m < 32; m *= 2) {
+          const int o = __shfl_up_sync(0xffffffffu, s, m);
+          if (lane >= m) s = max(s, o);
+        }
+        int before = __shfl_up_sync(0xffffffffu, s, 1);
+        if (lane == 0) before = high;
+        const int mine = (s - before + T - 1) / T;
+        int n = mine;
+#pragma unroll
+        for (int m = 1; m < 32; m *= 2) {
+          const int o = __shfl_up_sync(0xffffffffu, n, m);
+          if (lane >= m) n += o;
+        }
+        __syncwarp();
+        if (g < a.groups) start[g + 1] = s, first[g] = sum + n - mine;
+        high = __shfl_sync(0xffffffffu, s, 31);
+        sum += __shfl_sync(0xffffffffu, n, 31);
+      }
+      if (lane == 0) first[a.groups] = sum;
+    }
+    __syncthreads();
+  }
+};
+
+struct ProductTile {
+  int group, row, rows, n;                     // rows [row, row + rows), output channels from n * (channels of a tile) on
+  __device__ __forceinline__ bool find(const ProductArgs &a, const GroupTiles &gt, int tile, int T) {
+    if (tile >= gt.first[a.groups] * a.tiles_n) return false;
+    const int q = tile / a.tiles_n;
+    int lo = 0, hi = a.groups;                 // the last group with first <= q
+    while (hi - lo > 1) {
+      const int m = (lo + hi) / 2;
+      if (gt.first[m] <= q) lo = m;
+      else hi = m;
+    }
+    group = lo;
+    const int in = tile - gt.first[lo] * a.tiles_n, tiles = gt.first[lo + 1] - gt.first[lo];
+    n = in / tiles;
+    const int t = in - n * tiles;
+    row = gt.start[lo] + t * T;
+    rows = min(gt.start[lo + 1] - row, T);
+    return true;
+  }
+};
+
+// ---------------------------------------------------------------------------------------------
+// Few rows: output channels are the rows of the accumulator (the lanes of tensor memory), rows of x its columns.
+// ---------------------------------------------------------------------------------------------
+constexpr int FEW_THREADS = 384;
+template <int T>
+struct FewShape {
+  static constexpr int STAGES = T >= 128 ? 6 : 8, FACTORS = 8;
+  static constexpr uint32_t W_BYTES = PB * PB, X_BYTES = T * PB;
+};
+template <int T>
+struct FewShared {
+  using S = FewShape<T>;
+  uint8_t w[S::STAGES][S::W_BYTES];
+  uint8_t x[S::STAGES][S::X_BYTES];
+  float factor[S::FACTORS][T];
+  uint64_t full[S::STAGES], empty[S::STAGES], factor_full[S::FACTORS], factor_empty[S::FACTORS], sum_full[2], sum_empty[2], drained;
+  uint32_t tmem;
+  GroupTiles tiles;
+};
+
+template <int T>
+__global__ void __launch_bounds__(FEW_THREADS, 1) product_few_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs a) {
+  extern __shared__ __align__(1024) uint8_t raw[];
+  using S = FewShape<T>;
+  FewShared<T> &sm = *reinterpret_cast<FewShared<T> *>(raw);
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  if (shared_addr(raw) % 1024 != 0) {          // (the swizzled tiles count on it)
+    if (threadIdx.x == 0) atomicOr(&g_product_error, 2);
+    return;
+  }
+  if (threadIdx.x == 0) {
+    auto init = [](uint64_t &bar, int count) { bar_init(shared_addr(&bar), count); };
+    for (int i = 0; i < S::STAGES; i++) init(sm.full[i], 1), init(sm.empty[i], 1);
+    for (int i = 0; i < S::FACTORS; i++) init(sm.factor_full[i], 1), init(sm.factor_empty[i], 8);
+    for (int i = 0; i < 2; i++) init(sm.sum_full[i], 1), init(sm.sum_empty[i], 8);
+    init(sm.drained, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) tmem_alloc(shared_addr(&sm.tmem), 2 * T < 32 ? 32 : 2 * T);
+  tmem_fence_before();
+  sm.tiles.find(a, T);
+  tmem_fence_after();
+  const uint32_t tmem = sm.tmem;
+  bool ok = true;
+  ProductTile tile;
+  int c = 0;                                   // K blocks so far
+  if (warp == 0) {                             // ---- tensor copies ----
+    if (lane == 0) {
+      for (int t = blockIdx.x; ok && tile.find(a, sm.tiles, t, T); t += gridDim.x)
+        for (int b = 0; b < a.blocks; b++, c++) {
+          const int s = c % S::STAGES, turn = c / S::STAGES;
+          if (turn > 0 && !(ok = reached(shared_addr(&sm.empty[s]), (turn + 1) & 1))) break;
+          const uint32_t bar = shared_addr(&sm.full[s]);
+          bar_expect(bar, S::W_BYTES + S::X_BYTES);
+          tensor_g2s(shared_addr(sm.w[s]), &maps.w, b * PB, tile.n * PB, tile.group, bar);
+          tensor_g2s(shared_addr(sm.x[s]), &maps.x, b * PB, tile.row, 0, bar);
+        }
+      if (!ok) {                               // the copies on their way, before their shared memory is gone
+        for (int i = max(c - S::STAGES, 0); i < c; i++) reached(shared_addr(&sm.full[i % S::STAGES]), (i / S::STAGES) & 1);
+      }
+    }
+  } else if (warp == 1) {                      // ---- products ----
+    constexpr uint32_t what = mma_e4m3(PB, T);
+    for (int t = blockIdx.x; ok && tile.find(a, sm.tiles, t, T); t += gridDim.x)
+      for (int b = 0; b < a.blocks; b++, c++) {
+        const int s = c % S::STAGES, turn = c / S::STAGES, half = c & 1;
+        if (c >= 2 && !(ok = all_reached(shared_addr(&sm.sum_empty[half]), ((c >> 1) + 1) & 1))) break;
+        if (!(ok = all_reached(shared_addr(&sm.full[s]), turn & 1))) break;
+        tmem_fence_after();
+        if (elect_one()) {
+          const Operand W = operand(shared_addr(sm.w[s]), 0, 1024), X = operand(shared_addr(sm.x[s]), 0, 1024);
+#pragma unroll
+          for (int k = 0; k < 4; k++) mma8_ss(tmem + half * T, W + 32 * k, X + 32 * k, what, k > 0);
+          mma_commit(shared_addr(&sm.empty[s]));
+          mma_commit(shared_addr(&sm.sum_full[half]));
+        }
+        __syncwarp();
+      }
+    if (!ok) {                                 // the products on their way
+      if (elect_one()) mma_commit(shared_addr(&sm.drained));
+      __syncwarp();
+      reached(shared_addr(&sm.drained), 0);
+    }
+  } else if (warp < 4) {                       // ---- factors: the scales of a K block, a row of x each ----
+    constexpr int N = (T + 31) / 32;
+    for (int t = blockIdx.x; ok && tile.find(a, sm.tiles, t, T); t += gridDim.x) {
+      const float *ws = a.w_scale + ((int64_t)tile.group * a.tiles_n + tile.n) * a.blocks;
+      for (int b = 0; b < a.blocks; b++, c++) {
+        if ((c & 1) != warp - 2) continue;
+        float f[N];
+        const float w = ws[b];
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+          const int r = 32 * i + lane;
+          f[i] = r < tile.rows ? a.x_scale[b * a.x_scale_stride + tile.row + r] * w : 0.0f;
+        }
+        const int s = c % S::FACTORS, turn = c / S::FACTORS;
+        if (turn > 0 && !(ok = all_reached(shared_addr(&sm.factor_empty[s]), (turn + 1) & 1))) break;
+#pragma unroll
+        for (int i = 0; i < N; i++)
+          if (32 * i + lane < T) sm.factor[s][32 * i + lane] = f[i];
+        __syncwarp();
+        if (lane == 0) bar_arrive(shared_addr(&sm.factor_full[s]));
+      }
+    }
+  } else {                                     // ---- sums in binary32, outputs: half of a tile's columns, 32 output channels ----
+    constexpr int COLS = T / 2, CHUNK = COLS < 16 ? COLS : 16;
+    const int part = warp % 4, col0 = (warp - 4) / 4 * COLS;
+    for (int t = blockIdx.x; ok && tile.find(a, sm.tiles, t, T); t += gridDim.x) {
+      float sum[COLS];
+#pragma unroll
+      for (int i = 0; i < COLS; i++) sum[i] = 0.0f;
+      for (int b = 0; b < a.blocks; b++, c++) {
+        const int half = c & 1, s = c % S::FACTORS;
+        if (!(ok = all_reached(shared_addr(&sm.factor_full[s]), (c / S::FACTORS) & 1))) break;
+        if (!(ok = all_reached(shared_addr(&sm.sum_full[half]), (c >> 1) & 1))) break;
+        tmem_fence_after();
+#pragma unroll
+        for (int j = 0; j < COLS; j += CHUNK) {
+          uint32_t d[16];
+          static_assert(CHUNK == 16, "");
+          tmem_load16(tmem + half * T + col0 + j + ((uint32_t)part << 21), d);
+          tmem_wait_loads(d);
+#pragma unroll
+          for (int i = 0; i < 16; i += 4) {
+            const float4 f = *reinterpret_cast<const float4 *>(&sm.factor[s][col0 + j + i]);
+            sum[j + i] = fmaf(__uint_as_float(d[i]), f.x, sum[j + i]);
+            sum[j + i + 1] = fmaf(__uint_as_float(d[i + 1]), f.y, sum[j + i + 1]);
+            sum[j + i + 2] = fmaf(__uint_as_float(d[i + 2]), f.z, sum[j + i + 2]);
+            sum[j + i + 3] = fmaf(__uint_as_float(d[i + 3]), f.w, sum[j + i + 3]);
+          }
+        }
+        tmem_fence_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive(shared_addr(&sm.sum_empty[half])), bar_arrive(shared_addr(&sm.factor_empty[s]));
+      }
+      const int n = tile.n * PB + 32 * part + lane;
+      if (ok && n < a.outs) {
+#pragma unroll
+        for (int i = 0; i < COLS; i++)
+          if (col0 + i < tile.rows) {
+            const int64_t at = (int64_t)(tile.row + col0 + i) * a.out_stride + n;
+            if (a.type == LQ_F32) static_cast<float *>(a.out)[at] = sum[i];
+            else if (a.type == LQ_F16) static_cast<__half *>(a.out)[at] = from_float<__half>(sum[i]);
+            else static_cast<__nv_bfloat16 *>(a.out)[at] = from_float<__nv_bfloat16>(sum[i]);
+          }
+      }
+    }
+  }
+  if (!ok) atomicOr(&g_product_error, 1);
+  __syncwarp();
+  tmem_fence_before();
+  __syncthreads();
+  tmem_fence_after();
+  if (warp == 1) tmem_free(tmem, 2 * T < 32 ? 32 : 2 * T);
+}
+
+}  // namespace lq

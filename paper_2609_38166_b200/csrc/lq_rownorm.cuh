@@ -1,0 +1,208 @@
+// Norms in front of a projection and behind the recurrence, with 8-bit outputs: whole rows with the residual's addition, heads with a gate.
+//
+// Every element is read and written once and a row (a head) stays in registers between its sum of squares and its outputs: bound by memory.  A thread
+// has pieces of eight consecutive channels, so that sixteen neighbouring lanes have a block of 128 and its largest value is a butterfly over them.
+#pragma once
+#include "lq_rows.cuh"
+
+namespace lq {
+
+constexpr int LINE = 8;                       // channels of a thread's piece
+constexpr float E4M3_MAX = 448.0f, LEAST_SCALE = 0x1p-100f;
+
+// Where outputs go: rounded to the type, and / or as e4m3 codes with a scale for every 128 channels of a row.
+struct NormOut {
+  void *out;
+  uint8_t *out8;
+  float *scale;
+  int64_t out_stride, out8_stride, scale_stride;
+};
+
+// Four values as e4m3, nearest even, beyond 448 as 448, the first at the lowest address.
+__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
+  uint16_t lo, hi;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
+  return lo | (uint32_t)hi << 16;
+}
+
+// `n` of eight values at channel c of a row, of which the others are 0; all lanes of a warp together, sixteen with the channels of a block.
+template <bool WIDE, typename T>
+__device__ __forceinline__ void norm_store(const NormOut &o, int64_t row, int c, int n, const float (&y)[LINE]) {
+  if (o.out && n > 0) {
+    alignas(16) T t[LINE];
+    pack(y, t);
+    T *dst = static_cast<T *>(o.out) + row * o.out_stride + c;
+    if (WIDE) {
+      store_row<true>(dst, t);
+    } else {
+#pragma unroll
+      for (int e = 0; e < LINE; e++)
+        if (e < n) dst[e] = t[e];
+    }
+  }
+  if (o.out8) {
+    float top = 0.0f;
+#pragma unroll
+    for (int e = 0; e < LINE; e++) top = fmaxf(top, fabsf(y[e]));
+#pragma unroll
+    for (int m = 1; m < 16; m *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
+    const float scale = fmaxf(top * (1.0f / E4M3_MAX), LEAST_SCALE), by = 1.0f / scale;   // (an infinity makes all of its block NaN: 0 * inf)
+    uint32_t code[2];
+#pragma unroll
+    for (int e = 0; e < 2; e++) code[e] = pack_e4m3(y[4 * e] * by, y[4 * e + 1] * by, y[4 * e + 2] * by, y[4 * e + 3] * by);
+    uint8_t *dst = o.out8 + row * o.out8_stride + c;
+    if (WIDE) {
+      if (n > 0) *reinterpret_cast<uint2 *>(dst) = make_uint2(code[0], code[1]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < LINE; e++)
+        if (e < n) dst[e] = (uint8_t)(code[e / 4] >> 8 * (e % 4));
+    }
+    if (c % 128 == 0 && n > 0) o.scale[c / 128 * o.scale_stride + row] = scale;
+  }
+}
+
+// Eight elements from channel c on; those from `n` on are 0.
+template <bool WIDE, typename T>
+__device__ __forceinline__ void norm_load(const T *src, int n, float (&x)[LINE]) {
+  alignas(16) T t[LINE];
+  if (WIDE) {
+    if (n > 0) load_row<true>(src, t);
+  } else {
+#pragma unroll
+    for (int e = 0; e < LINE; e++)
+      if (e < n) t[e] = src[e];
+  }
+  unpack(t, x);
+#pragma unroll
+  for (int e = 0; e < LINE; e++) x[e] = e < n ? x[e] : 0.0f;
+}
+
+// What a sum of squares of `count` channels makes of a norm.
+__device__ __forceinline__ float norm_factor(int norm, float squares, int count, float eps) {
+  if (norm == LQ_NORM_NONE) return 1.0f;
+  return rsqrtf((norm == LQ_NORM_RMS ? squares / (float)count : squares) + eps);
+}
+
+// ---- whole rows: h = x + residual, y = norm(h) w ----
+struct AddArgs {
+  const void *x;
+  void *residual;
+  const float *w;
+  int64_t x_stride, residual_stride;
+  NormOut o;
+  int tokens, dim, norm;
+  float eps;
+};
+
+// blockDim: (threads of a row, rows)
+template <typename T, bool WIDE, int V>
+__global__ void __launch_bounds__(512) norm_add_kernel(const AddArgs a) {
+  __shared__ float part[16];
+  const int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+  const bool there = row < a.tokens;
+  float h[V][LINE];
+  float squares = 0.0f;
+#pragma unroll
+  for (int v = 0; v < V; v++) {
+    const int c = (v * blockDim.x + threadIdx.x) * LINE, n = there ? min(a.dim - c, LINE) : 0;
+    norm_load<WIDE>(static_cast<const T *>(a.x) + row * a.x_stride + c, n, h[v]);
+    if (a.residual) {
+      T *r = static_cast<T *>(a.residual) + row * a.residual_stride + c;
+      float more[LINE];
+      norm_load<WIDE>(r, n, more);
+#pragma unroll
+      for (int e = 0; e < LINE; e++) h[v][e] += more[e];
+      alignas(16) T t[LINE];
+      pack(h[v], t);
+      if (WIDE) {
+        if (n > 0) store_row<true>(r, t);
+      } else {
+#pragma unroll
+        for (int e = 0; e < LINE; e++)
+          if (e < n) r[e] = t[e];
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < LINE; e++) squares = fmaf(h[v][e], h[v][e], squares);
+  }
+  float factor = 1.0f;
+  if (a.norm != LQ_NORM_NONE) {
+#pragma unroll
+    for (int m = 1; m < 32; m *= 2) squares += __shfl_xor_sync(0xffffffffu, squares, m);
+    const int warps = blockDim.x / 32, first = threadIdx.y * warps;
+    if (threadIdx.x % 32 == 0) part[first + threadIdx.x / 32] = squares;
+    __syncthreads();
+    squares = part[first];
+    for (int w = 1; w < warps; w++) squares += part[first + w];
+    factor = norm_factor(a.norm, squares, a.dim, a.eps);
+  }
+#pragma unroll
+  for (int v = 0; v < V; v++) {
+    const int c = (v * blockDim.x + threadIdx.x) * LINE, n = there ? min(a.dim - c, LINE) : 0;
+    float w[LINE];
+    if (a.norm == LQ_NORM_RMS && a.w) {
+      norm_load<WIDE>(a.w + c, n, w);
+#pragma unroll
+      for (int e = 0; e < LINE; e++) h[v][e] *= factor * w[e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < LINE; e++) h[v][e] *= factor;
+    }
+    norm_store<WIDE, T>(a.o, row, c, n, h[v]);
+  }
+}
+
+// ---- heads behind the recurrence: y = norm(o) w act(z) ----
+struct GatedArgs {
+  const void *x, *z;
+  const float *w;
+  int64_t x_stride, z_stride;
+  NormOut o;
+  int tokens, heads, dim, norm, silu;
+  float eps;
+  int warps;                                  // warps of a row
+  Divisor by_warps;
+};
+
+constexpr int GATED_THREADS = 256;
+
+__device__ __forceinline__ float gate_of(float z, int silu) {   // 1 / (1 + exp(-z)), times z; a quotient that overflows is a 0
+  float e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.44269504088896340736f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+  return silu ? z * r : r;
+}
+
+// A warp has 256 channels of a row: a head of 256, two of 128 or four of 64.
+template <typename X, typename T, bool WIDE>
+__global__ void __launch_bounds__(GATED_THREADS) norm_gate_kernel(const GatedArgs a) {
+  const int lane = threadIdx.x % 32;
+  const uint32_t unit = blockIdx.x * (GATED_THREADS / 32) + threadIdx.x / 32;
+  const int64_t row = a.by_warps.quotient(unit);
+  if (row >= a.tokens) return;
+  const int c = ((unit - (uint32_t)row * a.warps) * 32 + lane) * LINE, n = c < a.heads * a.dim ? LINE : 0;
+  float x[LINE], z[LINE];
+  norm_load<WIDE>(static_cast<const X *>(a.x) + row * a.x_stride + c, n, x);
+  norm_load<WIDE>(static_cast<const T *>(a.z) + row * a.z_stride + c, n, z);
+  float factor = 1.0f;
+  if (a.norm != LQ_NORM_NONE) {
+    float squares = 0.0f;
+#pragma unroll
+    for (int e = 0; e < LINE; e++) squares = fmaf(x[e], x[e], squares);
+    for (int m = 1; m < a.dim / LINE; m *= 2) squares += __shfl_xor_sync(0xffffffffu, squares, m);
+    factor = norm_factor(a.norm, squares, a.dim, a.eps);
+  }
+  if (a.norm == LQ_NORM_RMS && a.w) {
+    float w[LINE];
+    norm_load<WIDE>(a.w + c % a.dim, LINE, w);
+#pragma unroll
+    for (int e = 0; e < LINE; e++) x[e] *= w[e];
+  }
+#pragma unroll
+  for (int e = 0; e < LINE; e++) x[e] *= factor * gate_of(z[e], a.silu);
+  norm_store<WIDE, T>(a.o, row, c, n, x);
+}
+
+}  // namespace lq

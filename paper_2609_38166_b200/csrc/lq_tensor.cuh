@@ -130,6 +130,15 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, Operand b, uint32
       " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n}\n" ::"r"(d), "r"(a), "r"(b.low), "r"(b.high), "r"(what), "r"((uint32_t)add)
       : "memory");
 }
+// e4m3 operands, both with K along the 128 bytes (a K step of 32 is 32 bytes further), binary32 accumulators.
+__host__ __device__ constexpr uint32_t mma_e4m3(int m, int n) { return 1u << 4 | (uint32_t)(n / 8) << 17 | (uint32_t)(m / 16) << 24; }
+__device__ __forceinline__ void mma8_ss(uint32_t d, Operand a, Operand b, uint32_t what, bool add) {
+  asm volatile(
+      "{\n .reg .pred p;\n .reg .b64 a, b;\n setp.ne.u32 p, %6, 0;\n mov.b64 a, {%1, %2};\n mov.b64 b, {%3, %4};\n"
+      " tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %5, p;\n}\n" ::"r"(d), "r"(a.low), "r"(a.high), "r"(b.low), "r"(b.high), "r"(what),
+      "r"((uint32_t)add)
+      : "memory");
+}
 // The barrier completes when every matrix instruction that this thread has issued has.
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");

@@ -26,6 +26,7 @@ EXPORTS = ["lq_decode_step", "lq_decode_step_profiled", "lq_decode_step_host", "
            "lq_quantize_state", "lq_dequantize_state", "lq_ref_decode_step_f32", "lq_ref_decode_step_bf16",
            "lq_decode_launches", "lq_step_launches", "lq_check_device", "lq_clear_device_flags", "lq_selftest_bounded_wait",
            "lq_conv_prompt", "lq_conv_step", "lq_norm_rotate", "lq_scan_prompt", "lq_scan_prompt_bytes", "lq_scan_step",
+           "lq_norm_add", "lq_norm_gate", "lq_product", "lq_product_groups",
            "lq_static_stage_bytes", "lq_import_state", "lq_export_state", "lq_status_string", "lq_version"]
 
 
@@ -89,7 +90,12 @@ def lib() -> C.CDLL:
         L.lq_norm_rotate.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp]
         L.lq_scan_prompt.argtypes = [vp, vp, vp, i64, vp, vp]
         L.lq_scan_step.argtypes = [vp, vp, vp, i64, vp]
-        for name in ("lq_conv_prompt", "lq_conv_step", "lq_norm_rotate", "lq_scan_prompt", "lq_scan_step"):
+        L.lq_norm_add.argtypes = [vp, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp]
+        L.lq_norm_gate.argtypes = [vp, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp]
+        L.lq_product.argtypes = [vp, vp, i64, vp, i64, vp, vp, vp, i64, vp]
+        L.lq_product_groups.argtypes = [vp, vp, i64, vp, i64, vp, vp, vp, i64, vp, vp]
+        for name in ("lq_conv_prompt", "lq_conv_step", "lq_norm_rotate", "lq_scan_prompt", "lq_scan_step", "lq_norm_add", "lq_norm_gate", "lq_product",
+                     "lq_product_groups"):
             getattr(L, name).restype = C.c_int
         L.lq_scan_prompt_bytes.restype = C.c_uint64
         L.lq_scan_prompt_bytes.argtypes = [vp]
@@ -498,6 +504,78 @@ class ScanShape(_Kept):
                 (self.seqs + 1,), (self.seqs,))
 
 
+class _Add(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("tokens", "dim", "norm", "type")] + [("eps", C.c_float)]
+
+
+class _Gated(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("tokens", "heads", "dim", "norm", "silu", "o_type", "type")] + [("eps", C.c_float)]
+
+
+class _Linear(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("rows", "in_", "out", "groups", "type")]
+
+
+E4M3 = torch.float8_e4m3fn
+BLOCK = 128                                  # channels of a row to a scale, and output channels of weights
+
+
+@dataclass
+class AddShape(_Kept):
+    """``lq_add``: rows of ``dim`` channels, normalised as a whole."""
+    tokens: int
+    dim: int
+    norm: int = NORM_RMS
+    type: int = BF16
+    eps: float = 1e-6
+
+    def c(self) -> _Add:
+        return _Add(self.tokens, self.dim, self.norm, self.type, self.eps)
+
+    def wants(self):
+        return _DTYPES.get(self.type), (self.tokens, self.dim), (self.dim,), (-(-self.dim // BLOCK), self.tokens)
+
+
+@dataclass
+class GatedShape(_Kept):
+    """``lq_gated``: ``heads`` heads of ``dim`` channels, outputs of a recurrence of ``o_type``."""
+    tokens: int
+    heads: int
+    dim: int = 128
+    norm: int = NORM_RMS
+    silu: int = 1
+    o_type: int = F32
+    type: int = BF16
+    eps: float = 1e-6
+
+    def c(self) -> _Gated:
+        return _Gated(self.tokens, self.heads, self.dim, self.norm, self.silu, self.o_type, self.type, self.eps)
+
+    def wants(self):
+        width = self.heads * self.dim
+        return (_DTYPES.get(self.o_type), _DTYPES.get(self.type), (self.tokens, self.heads, self.dim), (self.tokens, width), (self.dim,),
+                (-(-width // BLOCK), self.tokens))
+
+
+@dataclass
+class ProductShape(_Kept):
+    """``lq_linear``: ``rows`` rows of ``channels_in`` channels, weights of ``channels_out`` (of every group)."""
+    rows: int
+    channels_in: int
+    channels_out: int
+    groups: int = 1
+    type: int = BF16
+
+    def c(self) -> _Linear:
+        return _Linear(self.rows, self.channels_in, self.channels_out, self.groups, self.type)
+
+    def wants(self):
+        n, k = self.channels_out, self.channels_in
+        scales = (-(-n // BLOCK), -(-k // BLOCK))
+        return (_DTYPES.get(self.type), (self.rows, k), (scales[1], self.rows), (n, k), scales, (self.rows, n), (self.groups, n, k), (self.groups, *scales),
+                (self.groups + 1,))
+
+
 _SCAN_IO = struct.Struct("=3Q3q2Q2q8Q")        # lq_scan_io, as _ScanIo
 _device = torch._C._cuda_getDevice
 
@@ -621,6 +699,64 @@ def scan_step(sh: ScanShape, q, k, v, beta, alpha, o, S, slots=None, A=None, dt_
     rc = (_lib or lib()).lq_scan_step(ref, io, po, so, _stream(stream))
     if rc:
         _check(rc, "lq_scan_step")
+
+
+def _norm_out(out, out8, scale, dt, rows, scales, d: int):
+    """The six arguments of a norm's outputs."""
+    none = (None, 0)
+    return (*(none if out is None else _rows(out, "out", dt, rows, d)), *(none if out8 is None else _rows(out8, "out8", E4M3, rows, d)),
+            *(none if scale is None else _rows(scale, "scale", torch.float32, scales, d)))
+
+
+def norm_add(sh: AddShape, x, residual=None, w=None, out=None, out8=None, scale=None, stream=None) -> None:
+    """lq_norm_add: ``x``, ``out``, ``residual`` [tokens, dim] (``residual`` in and out, or None; ``out`` may be ``x``), ``w`` fp32 [dim] or None,
+    ``out8`` float8_e4m3fn [tokens, dim] with ``scale`` fp32 [ceil(dim/128), tokens]; ``out`` or ``out8`` may be None.  Rows of all may be strided."""
+    ref, (dt, rows, dim, scales) = sh.kept()
+    d = _device()
+    px, sx = _rows(x, "x", dt, rows, d)
+    pr, sr = (None, 0) if residual is None else _rows(residual, "residual", dt, rows, d)
+    rc = (_lib or lib()).lq_norm_add(ref, px, sx, pr, sr, _dense(w, "w", torch.float32, dim, d), *_norm_out(out, out8, scale, dt, rows, scales, d), _stream(stream))
+    if rc:
+        _check(rc, "lq_norm_add")
+
+
+def norm_gate(sh: GatedShape, o, z, w=None, out=None, out8=None, scale=None, stream=None) -> None:
+    """lq_norm_gate: ``o``, ``z`` [tokens, heads, dim], ``w`` fp32 [dim] or None, ``out`` [tokens, heads * dim], ``out8`` float8_e4m3fn
+    [tokens, heads * dim] with ``scale`` fp32 [ceil(heads * dim / 128), tokens]; ``out`` or ``out8`` may be None.  Rows of all may be strided."""
+    ref, (odt, dt, heads, rows, dim, scales) = sh.kept()
+    d = _device()
+    po, so = _rows(o, "o", odt, heads, d)
+    pz, sz = _rows(z, "z", dt, heads, d)
+    rc = (_lib or lib()).lq_norm_gate(ref, po, so, pz, sz, _dense(w, "w", torch.float32, dim, d), *_norm_out(out, out8, scale, dt, rows, scales, d), _stream(stream))
+    if rc:
+        _check(rc, "lq_norm_gate")
+
+
+def product(sh: ProductShape, x, x_scale, w, w_scale, out, stream=None) -> None:
+    """lq_product: ``x`` float8_e4m3fn [rows, channels_in], ``x_scale`` fp32 [ceil(channels_in/128), rows], ``out`` [rows, channels_out] (rows of all
+    three may be strided), ``w`` float8_e4m3fn [channels_out, channels_in], ``w_scale`` fp32 [ceil(channels_out/128), ceil(channels_in/128)]."""
+    ref, (dt, rows, scales, weights, w_scales, outs, _, _, _) = sh.kept()
+    d, f32 = _device(), torch.float32
+    px, sx = _rows(x, "x", E4M3, rows, d)
+    ps, ss = _rows(x_scale, "x_scale", f32, scales, d)
+    po, so = _rows(out, "out", dt, outs, d)
+    rc = (_lib or lib()).lq_product(ref, px, sx, ps, ss, _dense(w, "w", E4M3, weights, d), _dense(w_scale, "w_scale", f32, w_scales, d), po, so, _stream(stream))
+    if rc:
+        _check(rc, "lq_product")
+
+
+def product_groups(sh: ProductShape, x, x_scale, w, w_scale, out, group_start, stream=None) -> None:
+    """lq_product_groups: as ``product`` with ``w`` [groups, channels_out, channels_in], ``w_scale`` [groups, ceil(channels_out/128),
+    ceil(channels_in/128)]; ``group_start`` int32 [groups + 1]."""
+    ref, (dt, rows, scales, _, _, outs, weights, w_scales, starts) = sh.kept()
+    d, f32 = _device(), torch.float32
+    px, sx = _rows(x, "x", E4M3, rows, d)
+    ps, ss = _rows(x_scale, "x_scale", f32, scales, d)
+    po, so = _rows(out, "out", dt, outs, d)
+    rc = (_lib or lib()).lq_product_groups(ref, px, sx, ps, ss, _dense(w, "w", E4M3, weights, d), _dense(w_scale, "w_scale", f32, w_scales, d), po, so,
+                                           _dense(group_start, "group_start", torch.int32, starts, d), _stream(stream))
+    if rc:
+        _check(rc, "lq_product_groups")
 
 
 def clear_device_flags() -> None:
