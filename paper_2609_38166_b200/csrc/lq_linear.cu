@@ -96,13 +96,14 @@ static lq_status launch_gate(const GatedArgs &a, int type, bool wide, cudaStream
 
 constexpr int SMS = 148, MOST_CHANNELS = 1 << 20;
 
-// [planes][rows][channels] bytes, copied in boxes of `box` rows of 128 channels of one plane
-static bool byte_map(CUtensorMap *map, const void *base, long channels, long rows, long planes, int64_t stride, int64_t plane, int box) {
+// [planes][rows][channels] bytes, copied in boxes of `box` rows of `width` (128 or 64) bytes of one plane, swizzled by as many
+static bool byte_map(CUtensorMap *map, const void *base, long channels, long rows, long planes, int64_t stride, int64_t plane, int box, int width = PB) {
   const cuuint64_t size[3] = {(cuuint64_t)channels, (cuuint64_t)rows, (cuuint64_t)planes}, strides[2] = {(cuuint64_t)stride, (cuuint64_t)plane};
-  const cuuint32_t shape[3] = {PB, (cuuint32_t)box, 1}, one[3] = {1, 1, 1};
+  const cuuint32_t shape[3] = {(cuuint32_t)width, (cuuint32_t)box, 1}, one[3] = {1, 1, 1};
   const EncodeTiled f = encode_tiled();
   return f && f(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void *>(base), size, strides, shape, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+                width == PB ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <typename K>
@@ -126,13 +127,36 @@ static lq_status launch_few(const lq_linear *s, ProductArgs a, const void *x, in
   const lq_status rc = give_shared(product_few_kernel<T>, smem, ready);
   if (rc != LQ_OK) return rc;
   a.tiles_n = (int)ceil_div(s->out, PB);
-  ProductMaps maps;
+  ProductMaps maps{};
   if (!byte_map(&maps.x, x, s->in, s->rows, 1, x_stride, x_stride * s->rows, T) ||
       !byte_map(&maps.w, w, s->in, s->out, s->groups, s->in, (int64_t)s->in * s->out, PB))
     return LQ_ERR_CUDA;
   const long tiles = (ceil_div(s->rows, T) + s->groups - 1) * a.tiles_n;   // at most
   product_few_kernel<T><<<(int)std::min<long>(tiles, SMS), FEW_THREADS, smem, stream>>>(maps, a);
   return launched();
+}
+
+template <typename T, bool WIDE>
+static lq_status launch_many_t(const ProductMaps &maps, const ProductArgs &a, long pairs, cudaStream_t stream) {
+  static std::atomic<uint64_t> ready{0};
+  const lq_status rc = give_shared(product_many_kernel<T, WIDE>, sizeof(ManyShared), ready);
+  if (rc != LQ_OK) return rc;
+  product_many_kernel<T, WIDE><<<2 * (int)std::min<long>(pairs, SMS / 2), MANY_THREADS, sizeof(ManyShared), stream>>>(maps, a);
+  return launched();
+}
+static lq_status launch_many(const lq_linear *s, ProductArgs a, const void *x, int64_t x_stride, const void *w, cudaStream_t stream) {
+  a.tiles_n = (int)ceil_div(s->out, MANY_OUTS);
+  ProductMaps maps{};
+  if (!byte_map(&maps.x, x, s->in, s->rows, 1, x_stride, x_stride * s->rows, 128) ||
+      !byte_map(&maps.w, w, s->in, s->out, s->groups, s->in, (int64_t)s->in * s->out, 128))
+    return LQ_ERR_CUDA;
+  const long pairs = (ceil_div(s->rows, MANY_ROWS) + s->groups - 1) * a.tiles_n;   // at most
+  const unsigned size = type_size(s->type);
+  const bool wide = aligned(a.out, 16) && a.out_stride % (16 / size) == 0 && a.out_stride * size * s->rows < (int64_t)1 << 40;   // (what a tensor map can say)
+  if (wide && !byte_map(&maps.out, a.out, (long)s->out * size, s->rows, 1, a.out_stride * size, a.out_stride * size * s->rows, 32, 64)) return LQ_ERR_CUDA;
+  if (s->type == LQ_F32) return wide ? launch_many_t<float, true>(maps, a, pairs, stream) : launch_many_t<float, false>(maps, a, pairs, stream);
+  if (s->type == LQ_F16) return wide ? launch_many_t<__half, true>(maps, a, pairs, stream) : launch_many_t<__half, false>(maps, a, pairs, stream);
+  return wide ? launch_many_t<__nv_bfloat16, true>(maps, a, pairs, stream) : launch_many_t<__nv_bfloat16, false>(maps, a, pairs, stream);
 }
 
 static lq_status product(const lq_linear *s, const uint8_t *x, int64_t x_stride, const float *x_scale, int64_t x_scale_stride, const uint8_t *w,
@@ -159,6 +183,7 @@ static lq_status product(const lq_linear *s, const uint8_t *x, int64_t x_stride,
                          Span{w, s->in, s->in, (long)s->out * s->groups, 1}, Span{w_scale, blocks, blocks, ceil_div(s->out, PB) * s->groups, 4}})
     if (spans_meet(o, in)) return LQ_ERR_UNSUPPORTED;
   const ProductArgs a{x_scale, w_scale, out, x_scale_stride, out_stride, group_start, s->rows, blocks, s->out, s->groups, s->type, 0};
+  if (s->rows >= 128 * s->groups) return launch_many(s, a, x, x_stride, w, cuda_stream(stream));
   return launch_few<128>(s, a, x, x_stride, w, cuda_stream(stream));
 }
 

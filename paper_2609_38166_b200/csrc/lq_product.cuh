@@ -13,7 +13,9 @@ __device__ int g_product_error = 0;
 constexpr int PRODUCT_WAIT_LIMIT = 1 << 20;    // tries of a wait
 
 // Bounded wait; false: it ran out, leave (everybody else's next wait will too).
+// (The first try stands by itself: a wait that is over takes 53 clocks, by way of the loop 100.)
 __device__ __forceinline__ bool reached(uint32_t bar, uint32_t parity) {
+  if (bar_try(bar, parity)) return true;
   int left = PRODUCT_WAIT_LIMIT;
 #pragma unroll 1
   while (!bar_try(bar, parity))
@@ -23,7 +25,7 @@ __device__ __forceinline__ bool reached(uint32_t bar, uint32_t parity) {
 __device__ __forceinline__ bool all_reached(uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, reached(bar, parity)); }
 
 struct ProductMaps {
-  CUtensorMap x, w;
+  CUtensorMap x, w, out;
 };
 struct ProductArgs {
   const float *x_scale, *w_scale;
@@ -32,6 +34,25 @@ struct ProductArgs {
   const int32_t *group_start;                  // null: one group of all rows
   int rows, blocks, outs, groups, type;        // blocks: K blocks; outs: output channels
   int tiles_n;                                 // tiles of output channels
+};
+
+// The same for warps whose lanes have to stay together: no lane leaves, it goes on with waits of one try each and says so in the end.  (A vote behind every wait
+// and what hangs on it made a K block of a product 15 % longer.)
+struct Patience {
+  int limit = PRODUCT_WAIT_LIMIT;
+  __device__ __forceinline__ void wait(uint32_t bar, uint32_t parity) {
+    if (!bar_try(bar, parity)) {
+      int left = limit;
+#pragma unroll 1
+      while (!bar_try(bar, parity))
+        if (--left <= 0) {
+          limit = 1;
+          break;
+        }
+    }
+    __syncwarp();
+  }
+  __device__ __forceinline__ bool gone() const { return __any_sync(0xffffffffu, limit == 1); }
 };
 
 // The tiles of all groups: a group's tiles of rows, for one tile of output channels after another (those that run at the same time have
@@ -253,6 +274,196 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) product_few_kernel(const __gri
   __syncthreads();
   tmem_fence_after();
   if (warp == 1) tmem_free(tmem, 2 * T < 32 ? 32 : 2 * T);
+}
+
+// ---------------------------------------------------------------------------------------------
+// Many rows: rows of x are the rows of the accumulator, a row's factor is one number of its thread.  Two CTAs of a cluster work on one tile of 256 rows and
+// 256 output channels: either has 128 rows of x and of the weights in its shared memory and 128 rows of the sums in its tensor memory.
+// Two accumulators: one is taken over while the next K block's product goes to the other.
+// ---------------------------------------------------------------------------------------------
+constexpr int MANY_THREADS = 384, MANY_ROWS = 256, MANY_OUTS = 256;
+struct ManyShared {
+  static constexpr int STAGES = 5;
+  static constexpr uint32_t BYTES = 128 * PB;  // of either operand in a CTA
+  uint8_t x[STAGES][BYTES], w[STAGES][BYTES];
+  uint8_t out[8][2][32 * 64];                  // 64 bytes of 32 rows, two of a warp each
+  uint64_t full[STAGES], empty[STAGES], sum_full[2], sum_empty[2], drained;   // (full, sum_empty: the first CTA's)
+  uint32_t tmem;
+  GroupTiles tiles;
+};
+
+// 64 bytes of output channels of a warp's 32 rows, a row to a lane, as T in shared memory (64-byte swizzle).
+template <typename T>
+__device__ __forceinline__ void stage_sums(uint8_t *stage, const float2 *v, int lane) {
+  constexpr int N = 16 / sizeof(T);
+#pragma unroll
+  for (int u = 0; u < 4; u++) {
+    float x[N];
+#pragma unroll
+    for (int e = 0; e < N / 2; e++) x[2 * e] = v[N / 2 * u + e].x, x[2 * e + 1] = v[N / 2 * u + e].y;
+    alignas(16) T t[N];
+    pack(x, t);
+    *reinterpret_cast<uint4 *>(stage + 64 * lane + 16 * (u ^ (lane / 2 % 4))) = *reinterpret_cast<const uint4 *>(t);
+  }
+}
+// From there to rows of which `rows`, and output channels of which `n` are there: neighbouring lanes write neighbouring channels.
+template <typename T>
+__device__ __forceinline__ void copy_sums(const uint8_t *stage, T *dst, int64_t stride, int rows, int n, int lane) {
+  constexpr int N = 64 / sizeof(T), F = 16 / sizeof(T);
+  if (lane >= N || lane >= n) return;
+#pragma unroll 1
+  for (int r = 0; r < rows; r++) dst[r * stride + lane] = reinterpret_cast<const T *>(stage + 64 * r + 16 * ((lane / F) ^ (r / 2 % 4)))[lane % F];
+}
+
+template <typename T, bool WIDE>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1) product_many_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs a) {
+  extern __shared__ __align__(1024) uint8_t raw[];
+  using S = ManyShared;
+  S &sm = *reinterpret_cast<S *>(raw);
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, rank = cluster_rank(), first = blockIdx.x / 2, units = gridDim.x / 2;
+  if (shared_addr(raw) % 1024 != 0) {          // (the swizzled tiles count on it)
+    if (threadIdx.x == 0) atomicOr(&g_product_error, 2);
+    return;
+  }
+  if (threadIdx.x == 0) {
+    auto init = [](uint64_t &bar, int count) { bar_init(shared_addr(&bar), count); };
+    for (int i = 0; i < S::STAGES; i++) init(sm.full[i], 1), init(sm.empty[i], 1);
+    for (int i = 0; i < 2; i++) init(sm.sum_full[i], 1), init(sm.sum_empty[i], 16);
+    init(sm.drained, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) pair_tmem_alloc(shared_addr(&sm.tmem), 512);
+  tmem_fence_before();
+  sm.tiles.find(a, MANY_ROWS);
+  cluster_sync();
+  tmem_fence_after();
+  const uint32_t tmem = sm.tmem;
+  bool ok = true;
+  ProductTile tile;
+  int c = 0;                                   // K blocks so far
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    if (warp == 0) {                          // ---- tensor copies: this CTA's half of either operand ----
+      if (lane == 0) {
+        for (int t = first; ok && tile.find(a, sm.tiles, t, MANY_ROWS); t += units)
+          for (int b = 0; b < a.blocks; b++, c++) {
+            const int s = c % S::STAGES, turn = c / S::STAGES;
+            if (turn > 0 && !(ok = reached(shared_addr(&sm.empty[s]), (turn + 1) & 1))) break;
+            const uint32_t bar = shared_of(shared_addr(&sm.full[s]), 0);
+            if (rank == 0) bar_expect(shared_addr(&sm.full[s]), 4 * S::BYTES);
+            pair_tensor_g2s(shared_addr(sm.x[s]), &maps.x, b * PB, tile.row + 128 * rank, 0, bar);
+            pair_tensor_g2s(shared_addr(sm.w[s]), &maps.w, b * PB, tile.n * MANY_OUTS + 128 * rank, tile.group, bar);
+          }
+        if (!ok && rank == 0) {                // the copies on their way, before their shared memory is gone
+          for (int i = max(c - S::STAGES, 0); i < c; i++) reached(shared_addr(&sm.full[i % S::STAGES]), (i / S::STAGES) & 1);
+        }
+      }
+    } else if (warp == 1) {                    // ---- products, for both CTAs: one thread ----
+      constexpr uint32_t what = mma_e4m3(MANY_ROWS, MANY_OUTS);
+      if (rank == 0 && elect_one()) {
+        for (int t = first; ok && tile.find(a, sm.tiles, t, MANY_ROWS); t += units)
+          for (int b = 0; ok && b < a.blocks; b++, c++) {
+            const int s = c % S::STAGES, turn = c / S::STAGES, buf = c & 1;
+            if (!(ok = reached(shared_addr(&sm.full[s]), turn & 1))) break;
+            const Operand X = operand(shared_addr(sm.x[s]), 0, 1024), W = operand(shared_addr(sm.w[s]), 0, 1024);
+            if (c >= 2 && !(ok = reached(shared_addr(&sm.sum_empty[buf]), ((c >> 1) + 1) & 1))) break;
+            tmem_fence_after();
+#pragma unroll
+            for (int k = 0; k < 4; k++) pair_mma8_ss(tmem + buf * MANY_OUTS, X + 32 * k, W + 32 * k, what, k > 0);
+            pair_mma_commit(shared_addr(&sm.sum_full[buf]));
+            pair_mma_commit(shared_addr(&sm.empty[s]));
+          }
+        if (!ok) {                             // the products on their way
+          pair_mma_commit(shared_addr(&sm.drained));
+          reached(shared_addr(&sm.drained), 0);
+        }
+      }
+    }
+  } else {                                     // ---- sums in binary32, outputs: a row each, half of the tile's output channels ----
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");   // (256 * 224 + 128 * 56 of the 384 * 168 that the block starts with)
+    const int part = warp % 4, half = (warp - 4) / 4, r = 128 * rank + 32 * part + lane;
+    const int blocks_n = (a.outs + PB - 1) / PB;
+    const uint32_t from = tmem + 128 * half + ((uint32_t)part << 21);
+    const uint32_t full = shared_addr(&sm.sum_full[0]), empty = shared_of(shared_addr(&sm.sum_empty[0]), 0);
+    Patience patience;
+    float x0, x1, w0, w1;                      // scales of this K block and of the next
+    const float *px, *pw;
+    bool mine;                                 // there is a row, and output channels
+    auto scales = [&](int b, float &x, float &w) {
+      const bool there = mine && b < a.blocks;
+      x = there ? px[b * a.x_scale_stride] : 0.0f;
+      w = there ? pw[b] : 0.0f;
+    };
+    auto find = [&](int t) {
+      if (!tile.find(a, sm.tiles, t, MANY_ROWS)) return false;
+      px = a.x_scale + tile.row + r;
+      pw = a.w_scale + ((int64_t)tile.group * blocks_n + 2 * tile.n + half) * a.blocks;
+      mine = r < tile.rows && 2 * tile.n + half < blocks_n;
+      scales(0, x0, w0);
+      scales(1, x1, w1);
+      return true;
+    };
+    int t = first;
+    bool more = find(t);
+    while (more) {
+      float2 sum[64];
+#pragma unroll
+      for (int i = 0; i < 64; i++) sum[i] = make_float2(0.0f, 0.0f);
+#pragma unroll 1
+      for (int b = 0; b < a.blocks; b++, c++) {
+        const int buf = c & 1;
+        const float f = x0 * w0;
+        const float2 ff = make_float2(f, f);
+        x0 = x1, w0 = w1;
+        scales(b + 2, x1, w1);
+        patience.wait(full + 8 * buf, (c >> 1) & 1);
+        tmem_fence_after();
+        uint32_t d[2][16];
+        tmem_load16(from + buf * MANY_OUTS, d[0]);
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+          tmem_wait_loads(d[j & 1]);
+          if (j < 7) tmem_load16(from + buf * MANY_OUTS + 16 * (j + 1), d[(j + 1) & 1]);
+          if (j == 7) {
+            tmem_fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive_cluster(empty + 8 * buf);
+          }
+#pragma unroll
+          for (int i = 0; i < 8; i++) sum[8 * j + i] = __ffma2_rn(make_float2(__uint_as_float(d[j & 1][2 * i]), __uint_as_float(d[j & 1][2 * i + 1])), ff, sum[8 * j + i]);
+        }
+      }
+      const int n = tile.n * MANY_OUTS + 128 * half, row = tile.row + 128 * rank + 32 * part, rows = min(tile.rows - 128 * rank - 32 * part, 32);
+      ok = !patience.gone();
+      t += units;
+      more = find(t);
+      constexpr int N = 64 / sizeof(T);
+#pragma unroll
+      for (int i = 0; i < 128 / N; i++)
+        if (ok && rows > 0 && n + N * i < a.outs) {
+          uint8_t *const stage = sm.out[warp - 4][i % 2];
+          if (WIDE && rows == 32) copies_read<1>();   // (the one in front of the last was from this place)
+          else copies_read<0>();
+          __syncwarp();
+          stage_sums<T>(stage, sum + N / 2 * i, lane);
+          fence_async_shared();
+          __syncwarp();
+          if (WIDE && rows == 32) {
+            if (lane == 0) tensor_s2g(&maps.out, shared_addr(stage), (n + N * i) * (int)sizeof(T), row, 0), copies_commit();
+          } else {
+            copy_sums(stage, static_cast<T *>(a.out) + (int64_t)row * a.out_stride + n + N * i, a.out_stride, rows, a.outs - n - N * i, lane);
+            __syncwarp();
+          }
+        }
+    }
+    copies_done();
+  }
+  if (!ok) atomicOr(&g_product_error, 1);
+  __syncwarp();
+  tmem_fence_before();
+  cluster_sync();
+  tmem_fence_after();
+  if (warp == 1) pair_tmem_free(tmem, 512);
 }
 
 }  // namespace lq
