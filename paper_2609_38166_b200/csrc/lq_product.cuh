@@ -287,6 +287,7 @@ struct ManyShared {
   static constexpr uint32_t BYTES = 128 * PB;  // of either operand in a CTA
   uint8_t x[STAGES][BYTES], w[STAGES][BYTES];
   uint8_t out[8][2][32 * 64];                  // 64 bytes of 32 rows, two of a warp each
+  float factor[4][2][128];                     // of four K blocks: of a row, for 128 output channels each
   uint64_t full[STAGES], empty[STAGES], sum_full[2], sum_empty[2], drained;   // (full, sum_empty: the first CTA's)
   uint32_t tmem;
   GroupTiles tiles;
@@ -328,7 +329,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1) pro
   if (threadIdx.x == 0) {
     auto init = [](uint64_t &bar, int count) { bar_init(shared_addr(&bar), count); };
     for (int i = 0; i < S::STAGES; i++) init(sm.full[i], 1), init(sm.empty[i], 1);
-    for (int i = 0; i < 2; i++) init(sm.sum_full[i], 1), init(sm.sum_empty[i], 16);
+    for (int i = 0; i < 2; i++) init(sm.sum_full[i], 2), init(sm.sum_empty[i], 16);
     init(sm.drained, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -378,48 +379,68 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1) pro
           reached(shared_addr(&sm.drained), 0);
         }
       }
+    } else {                                   // ---- factors: of every other K block each, four rows a lane, loaded two K blocks of its own ahead ----
+      // A K block's factors are in their place when sum_full says that its sums are.  The place was the K block's four in front of it: when the product of the one
+      // two in front has ended, that product's accumulator had been given back by all who read these factors in front of it.
+      float x[2][4], w[2][2];
+      ProductTile at;                          // of the K block that is loaded next
+      int t = first, b = warp - 2, n = warp - 2;
+      bool there = at.find(a, sm.tiles, t, MANY_ROWS);
+      const int blocks_n = (a.outs + PB - 1) / PB;
+      auto load = [&](int k) {
+        while (there && b >= a.blocks) {
+          b -= a.blocks, t += units;
+          there = at.find(a, sm.tiles, t, MANY_ROWS);
+        }
+        if (!there) return false;
+        const int rows = at.rows - 128 * rank;
+        const float *px = a.x_scale + b * a.x_scale_stride + at.row + 128 * rank + lane;
+        const float *pw = a.w_scale + ((int64_t)at.group * blocks_n + 2 * at.n) * a.blocks + b;
+        w[k][0] = pw[0];
+        w[k][1] = 2 * at.n + 1 < blocks_n ? pw[a.blocks] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; i++) x[k][i] = 32 * i + lane < rows ? px[32 * i] : 0.0f;
+        b += 2;
+        return true;
+      };
+      Patience patience;
+      bool more[2] = {load(0), load(1)};
+      while (more[0]) {
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+          if (!more[k]) break;
+          const int buf = n & 1;
+          if (n >= 2) patience.wait(shared_addr(&sm.sum_full[buf]), ((n >> 1) + 1) & 1);
+          float (*f)[128] = sm.factor[n & 3];
+#pragma unroll
+          for (int i = 0; i < 4; i++) f[0][32 * i + lane] = x[k][i] * w[k][0], f[1][32 * i + lane] = x[k][i] * w[k][1];
+          __syncwarp();
+          if (lane == 0) bar_arrive(shared_addr(&sm.sum_full[buf]));
+          n += 2;
+          more[k] = load(k);
+        }
+      }
+      ok = !patience.gone();
     }
   } else {                                     // ---- sums in binary32, outputs: a row each, half of the tile's output channels ----
     asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");   // (256 * 224 + 128 * 56 of the 384 * 168 that the block starts with)
-    const int part = warp % 4, half = (warp - 4) / 4, r = 128 * rank + 32 * part + lane;
-    const int blocks_n = (a.outs + PB - 1) / PB;
+    const int part = warp % 4, half = (warp - 4) / 4;
     const uint32_t from = tmem + 128 * half + ((uint32_t)part << 21);
     const uint32_t full = shared_addr(&sm.sum_full[0]), empty = shared_of(shared_addr(&sm.sum_empty[0]), 0);
     Patience patience;
-    float x0, x1, w0, w1;                      // scales of this K block and of the next
-    const float *px, *pw;
-    bool mine;                                 // there is a row, and output channels
-    auto scales = [&](int b, float &x, float &w) {
-      const bool there = mine && b < a.blocks;
-      x = there ? px[b * a.x_scale_stride] : 0.0f;
-      w = there ? pw[b] : 0.0f;
-    };
-    auto find = [&](int t) {
-      if (!tile.find(a, sm.tiles, t, MANY_ROWS)) return false;
-      px = a.x_scale + tile.row + r;
-      pw = a.w_scale + ((int64_t)tile.group * blocks_n + 2 * tile.n + half) * a.blocks;
-      mine = r < tile.rows && 2 * tile.n + half < blocks_n;
-      scales(0, x0, w0);
-      scales(1, x1, w1);
-      return true;
-    };
-    int t = first;
-    bool more = find(t);
-    while (more) {
+    for (int t = first; tile.find(a, sm.tiles, t, MANY_ROWS); t += units) {
       float2 sum[64];
 #pragma unroll
       for (int i = 0; i < 64; i++) sum[i] = make_float2(0.0f, 0.0f);
 #pragma unroll 1
       for (int b = 0; b < a.blocks; b++, c++) {
         const int buf = c & 1;
-        const float f = x0 * w0;
-        const float2 ff = make_float2(f, f);
-        x0 = x1, w0 = w1;
-        scales(b + 2, x1, w1);
         patience.wait(full + 8 * buf, (c >> 1) & 1);
         tmem_fence_after();
         uint32_t d[2][16];
         tmem_load16(from + buf * MANY_OUTS, d[0]);
+        const float f = sm.factor[c & 3][half][32 * part + lane];
+        const float2 ff = make_float2(f, f);
 #pragma unroll
         for (int j = 0; j < 8; j++) {
           tmem_wait_loads(d[j & 1]);
@@ -435,8 +456,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1) pro
       }
       const int n = tile.n * MANY_OUTS + 128 * half, row = tile.row + 128 * rank + 32 * part, rows = min(tile.rows - 128 * rank - 32 * part, 32);
       ok = !patience.gone();
-      t += units;
-      more = find(t);
       constexpr int N = 64 / sizeof(T);
 #pragma unroll
       for (int i = 0; i < 128 / N; i++)
