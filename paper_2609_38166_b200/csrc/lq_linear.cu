@@ -120,20 +120,36 @@ static lq_status give_shared(K kernel, size_t bytes, std::atomic<uint64_t> &read
   return LQ_OK;
 }
 
-template <int T>
-static lq_status launch_few(const lq_linear *s, ProductArgs a, const void *x, int64_t x_stride, const void *w, cudaStream_t stream) {
+template <typename T, bool WIDE>
+static lq_status launch_few_t(const ProductMaps &maps, const ProductArgs &a, int grid, cudaStream_t stream) {
   static std::atomic<uint64_t> ready{0};
-  constexpr size_t smem = sizeof(FewShared<T>);
-  const lq_status rc = give_shared(product_few_kernel<T>, smem, ready);
+  const lq_status rc = give_shared(product_few_kernel<T, WIDE>, sizeof(FewShared), ready);
   if (rc != LQ_OK) return rc;
+  cudaLaunchAttribute cluster{};
+  cluster.id = cudaLaunchAttributeClusterDimension;
+  cluster.val.clusterDim.x = a.split, cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+  cudaLaunchConfig_t config{};
+  config.gridDim = dim3(grid), config.blockDim = dim3(FEW_THREADS), config.dynamicSmemBytes = sizeof(FewShared), config.stream = stream;
+  config.attrs = &cluster, config.numAttrs = 1;
+  if (cudaLaunchKernelEx(&config, product_few_kernel<T, WIDE>, maps, a) != cudaSuccess) {
+    cudaGetLastError();
+    return LQ_ERR_CUDA;
+  }
+  return LQ_OK;
+}
+static lq_status launch_few(const lq_linear *s, ProductArgs a, const void *x, int64_t x_stride, const void *w, cudaStream_t stream) {
   a.tiles_n = (int)ceil_div(s->out, PB);
   ProductMaps maps{};
-  if (!byte_map(&maps.x, x, s->in, s->rows, 1, x_stride, x_stride * s->rows, T) ||
+  if (!byte_map(&maps.x, x, s->in, s->rows, 1, x_stride, x_stride * s->rows, FEW_BOX) ||
       !byte_map(&maps.w, w, s->in, s->out, s->groups, s->in, (int64_t)s->in * s->out, PB))
     return LQ_ERR_CUDA;
-  const long tiles = (ceil_div(s->rows, T) + s->groups - 1) * a.tiles_n;   // at most
-  product_few_kernel<T><<<(int)std::min<long>(tiles, SMS), FEW_THREADS, smem, stream>>>(maps, a);
-  return launched();
+  const long tiles = (ceil_div(s->rows, FEW_ROWS) + s->groups - 1) * a.tiles_n;   // at most
+  a.split = s->groups == 1 && !a.group_start ? (int)std::max(1l, std::min({SMS / tiles, 8l, (long)a.blocks / 2})) : 1;
+  const int grid = (int)std::min<long>(tiles, SMS) * a.split;
+  const bool wide = aligned(a.out, 16) && a.out_stride % (16 / type_size(s->type)) == 0;
+  if (s->type == LQ_F32) return wide ? launch_few_t<float, true>(maps, a, grid, stream) : launch_few_t<float, false>(maps, a, grid, stream);
+  if (s->type == LQ_F16) return wide ? launch_few_t<__half, true>(maps, a, grid, stream) : launch_few_t<__half, false>(maps, a, grid, stream);
+  return wide ? launch_few_t<__nv_bfloat16, true>(maps, a, grid, stream) : launch_few_t<__nv_bfloat16, false>(maps, a, grid, stream);
 }
 
 template <typename T, bool WIDE>
@@ -182,9 +198,9 @@ static lq_status product(const lq_linear *s, const uint8_t *x, int64_t x_stride,
   for (const Span &in : {Span{x, x_stride, s->in, s->rows, 1}, Span{x_scale, x_scale_stride, s->rows, blocks, 4},
                          Span{w, s->in, s->in, (long)s->out * s->groups, 1}, Span{w_scale, blocks, blocks, ceil_div(s->out, PB) * s->groups, 4}})
     if (spans_meet(o, in)) return LQ_ERR_UNSUPPORTED;
-  const ProductArgs a{x_scale, w_scale, out, x_scale_stride, out_stride, group_start, s->rows, blocks, s->out, s->groups, s->type, 0};
+  const ProductArgs a{x_scale, w_scale, out, x_scale_stride, out_stride, group_start, s->rows, blocks, s->out, s->groups, s->type, 0, 1};
   if (s->rows >= 128 * s->groups) return launch_many(s, a, x, x_stride, w, cuda_stream(stream));
-  return launch_few<128>(s, a, x, x_stride, w, cuda_stream(stream));
+  return launch_few(s, a, x, x_stride, w, cuda_stream(stream));
 }
 
 // lq_check_device / lq_clear_device_flags: the flag of the kernels in this file

@@ -22,7 +22,6 @@ __device__ __forceinline__ bool reached(uint32_t bar, uint32_t parity) {
     if (--left == 0) return false;
   return true;
 }
-__device__ __forceinline__ bool all_reached(uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, reached(bar, parity)); }
 
 struct ProductMaps {
   CUtensorMap x, w, out;
@@ -34,6 +33,7 @@ struct ProductArgs {
   const int32_t *group_start;                  // null: one group of all rows
   int rows, blocks, outs, groups, type;        // blocks: K blocks; outs: output channels
   int tiles_n;                                 // tiles of output channels
+  int split;                                   // CTAs of a cluster that share a tile's K blocks (few rows)
 };
 
 // The same for warps whose lanes have to stay together: no lane leaves, it goes on with waits of one try each and says so in the end.  (A vote behind every wait
@@ -120,30 +120,50 @@ struct ProductTile {
 };
 
 // ---------------------------------------------------------------------------------------------
-// Few rows: output channels are the rows of the accumulator (the lanes of tensor memory), rows of x its columns.
+// Few rows: output channels are the rows of the accumulator (the lanes of tensor memory), rows of x its columns, as many as there are (in steps of 16).
+// The weights are what such a call reads, so all that counts is that they are on their way: up to 96 KB to an SM.
+// Where there are fewer tiles than SMs, the CTAs of a cluster share a tile's K blocks and add up their sums by way of one another's shared memory, each for
+// some of the rows, in the order of the CTAs.
 // ---------------------------------------------------------------------------------------------
-constexpr int FEW_THREADS = 384;
-template <int T>
-struct FewShape {
-  static constexpr int STAGES = T >= 128 ? 6 : 8, FACTORS = 8;
-  static constexpr uint32_t W_BYTES = PB * PB, X_BYTES = T * PB;
-};
-template <int T>
+constexpr int FEW_THREADS = 384, FEW_ROWS = 128, FEW_BOX = 32;   // FEW_BOX: rows to a copy
 struct FewShared {
-  using S = FewShape<T>;
-  uint8_t w[S::STAGES][S::W_BYTES];
-  uint8_t x[S::STAGES][S::X_BYTES];
-  float factor[S::FACTORS][T];
-  uint64_t full[S::STAGES], empty[S::STAGES], factor_full[S::FACTORS], factor_empty[S::FACTORS], sum_full[2], sum_empty[2], drained;
+  static constexpr int STAGES = 6, SUMS = 4;
+  static constexpr uint32_t W_BYTES = PB * PB, BOX_BYTES = FEW_BOX * PB;
+  uint8_t w[STAGES][W_BYTES];                  // (behind a split tile's products: sums of all CTAs, [CTA][row][128 channels])
+  uint8_t x[STAGES][FEW_ROWS * PB];
+  uint8_t out[8][16 * 32 * 4];                 // 32 output channels of 16 rows, a warp each
+  float factor[2 * SUMS][FEW_ROWS];
+  uint64_t full[STAGES], empty[STAGES], sum_full[SUMS], sum_empty[SUMS], drained;
   uint32_t tmem;
   GroupTiles tiles;
 };
 
-template <int T>
+__device__ __forceinline__ void store_shared_of(uint32_t addr, float x) { asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(x) : "memory"); }
+
+// 32 output channels (a lane each) of 16 rows, of which `rows` and `n` are there, by way of shared memory: pieces of 16 bytes.
+template <bool WIDE, typename T>
+__device__ __forceinline__ void store_columns(uint8_t *stage, T *dst, int64_t stride, const float *v, int rows, int n, int lane) {
+  T *s = reinterpret_cast<T *>(stage);
+#pragma unroll
+  for (int i = 0; i < 16; i++) s[32 * i + lane] = from_float<T>(v[i]);
+  __syncwarp();
+  if (WIDE && n >= 32) {
+    constexpr int PIECES = 2 * sizeof(T), N = 16 / sizeof(T);   // pieces of a row
+#pragma unroll
+    for (int u = lane; u < 16 * PIECES; u += 32)
+      if (u / PIECES < rows) *reinterpret_cast<uint4 *>(dst + u / PIECES * stride + u % PIECES * N) = reinterpret_cast<const uint4 *>(stage)[u];
+  } else if (lane < n) {
+#pragma unroll 1
+    for (int i = 0; i < rows; i++) dst[i * stride + lane] = s[32 * i + lane];
+  }
+  __syncwarp();
+}
+
+template <typename T, bool WIDE>
 __global__ void __launch_bounds__(FEW_THREADS, 1) product_few_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs a) {
   extern __shared__ __align__(1024) uint8_t raw[];
-  using S = FewShape<T>;
-  FewShared<T> &sm = *reinterpret_cast<FewShared<T> *>(raw);
+  using S = FewShared;
+  S &sm = *reinterpret_cast<S *>(raw);
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   if (shared_addr(raw) % 1024 != 0) {          // (the swizzled tiles count on it)
     if (threadIdx.x == 0) atomicOr(&g_product_error, 2);
@@ -152,119 +172,176 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) product_few_kernel(const __gri
   if (threadIdx.x == 0) {
     auto init = [](uint64_t &bar, int count) { bar_init(shared_addr(&bar), count); };
     for (int i = 0; i < S::STAGES; i++) init(sm.full[i], 1), init(sm.empty[i], 1);
-    for (int i = 0; i < S::FACTORS; i++) init(sm.factor_full[i], 1), init(sm.factor_empty[i], 8);
-    for (int i = 0; i < 2; i++) init(sm.sum_full[i], 1), init(sm.sum_empty[i], 8);
+    for (int i = 0; i < S::SUMS; i++) init(sm.sum_full[i], 2), init(sm.sum_empty[i], 8);
     init(sm.drained, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 1) tmem_alloc(shared_addr(&sm.tmem), 2 * T < 32 ? 32 : 2 * T);
+  if (warp == 1) tmem_alloc(shared_addr(&sm.tmem), S::SUMS * FEW_ROWS);
   tmem_fence_before();
-  sm.tiles.find(a, T);
+  sm.tiles.find(a, FEW_ROWS);
   tmem_fence_after();
   const uint32_t tmem = sm.tmem;
+  const int rank = a.split > 1 ? cluster_rank() : 0, first = blockIdx.x / a.split, units = gridDim.x / a.split;
+  const int b0 = a.blocks * rank / a.split, b1 = a.blocks * (rank + 1) / a.split;   // K blocks of this CTA
   bool ok = true;
   ProductTile tile;
   int c = 0;                                   // K blocks so far
   if (warp == 0) {                             // ---- tensor copies ----
     if (lane == 0) {
-      for (int t = blockIdx.x; ok && tile.find(a, sm.tiles, t, T); t += gridDim.x)
-        for (int b = 0; b < a.blocks; b++, c++) {
+      for (int t = first; ok && tile.find(a, sm.tiles, t, FEW_ROWS); t += units) {
+        const int boxes = (tile.rows + FEW_BOX - 1) / FEW_BOX;
+        for (int b = b0; b < b1; b++, c++) {
           const int s = c % S::STAGES, turn = c / S::STAGES;
           if (turn > 0 && !(ok = reached(shared_addr(&sm.empty[s]), (turn + 1) & 1))) break;
           const uint32_t bar = shared_addr(&sm.full[s]);
-          bar_expect(bar, S::W_BYTES + S::X_BYTES);
+          bar_expect(bar, S::W_BYTES + boxes * S::BOX_BYTES);
           tensor_g2s(shared_addr(sm.w[s]), &maps.w, b * PB, tile.n * PB, tile.group, bar);
-          tensor_g2s(shared_addr(sm.x[s]), &maps.x, b * PB, tile.row, 0, bar);
+          for (int i = 0; i < boxes; i++) tensor_g2s(shared_addr(sm.x[s]) + i * S::BOX_BYTES, &maps.x, b * PB, tile.row + i * FEW_BOX, 0, bar);
         }
+      }
       if (!ok) {                               // the copies on their way, before their shared memory is gone
         for (int i = max(c - S::STAGES, 0); i < c; i++) reached(shared_addr(&sm.full[i % S::STAGES]), (i / S::STAGES) & 1);
       }
     }
-  } else if (warp == 1) {                      // ---- products ----
-    constexpr uint32_t what = mma_e4m3(PB, T);
-    for (int t = blockIdx.x; ok && tile.find(a, sm.tiles, t, T); t += gridDim.x)
-      for (int b = 0; b < a.blocks; b++, c++) {
-        const int s = c % S::STAGES, turn = c / S::STAGES, half = c & 1;
-        if (c >= 2 && !(ok = all_reached(shared_addr(&sm.sum_empty[half]), ((c >> 1) + 1) & 1))) break;
-        if (!(ok = all_reached(shared_addr(&sm.full[s]), turn & 1))) break;
-        tmem_fence_after();
-        if (elect_one()) {
+  } else if (warp == 1) {                      // ---- products: one thread ----
+    if (elect_one()) {
+      for (int t = first; ok && tile.find(a, sm.tiles, t, FEW_ROWS); t += units) {
+        const uint32_t what = mma_e4m3(PB, (tile.rows + 15) / 16 * 16);
+        for (int b = b0; b < b1; b++, c++) {
+          const int s = c % S::STAGES, turn = c / S::STAGES, buf = c % S::SUMS;
+          if (c >= S::SUMS && !(ok = reached(shared_addr(&sm.sum_empty[buf]), (c / S::SUMS + 1) & 1))) break;
+          if (!(ok = reached(shared_addr(&sm.full[s]), turn & 1))) break;
+          tmem_fence_after();
           const Operand W = operand(shared_addr(sm.w[s]), 0, 1024), X = operand(shared_addr(sm.x[s]), 0, 1024);
 #pragma unroll
-          for (int k = 0; k < 4; k++) mma8_ss(tmem + half * T, W + 32 * k, X + 32 * k, what, k > 0);
+          for (int k = 0; k < 4; k++) mma8_ss(tmem + buf * FEW_ROWS, W + 32 * k, X + 32 * k, what, k > 0);
+          mma_commit(shared_addr(&sm.sum_full[buf]));
           mma_commit(shared_addr(&sm.empty[s]));
-          mma_commit(shared_addr(&sm.sum_full[half]));
         }
-        __syncwarp();
       }
-    if (!ok) {                                 // the products on their way
-      if (elect_one()) mma_commit(shared_addr(&sm.drained));
-      __syncwarp();
-      reached(shared_addr(&sm.drained), 0);
-    }
-  } else if (warp < 4) {                       // ---- factors: the scales of a K block, a row of x each ----
-    constexpr int N = (T + 31) / 32;
-    for (int t = blockIdx.x; ok && tile.find(a, sm.tiles, t, T); t += gridDim.x) {
-      const float *ws = a.w_scale + ((int64_t)tile.group * a.tiles_n + tile.n) * a.blocks;
-      for (int b = 0; b < a.blocks; b++, c++) {
-        if ((c & 1) != warp - 2) continue;
-        float f[N];
-        const float w = ws[b];
-#pragma unroll
-        for (int i = 0; i < N; i++) {
-          const int r = 32 * i + lane;
-          f[i] = r < tile.rows ? a.x_scale[b * a.x_scale_stride + tile.row + r] * w : 0.0f;
-        }
-        const int s = c % S::FACTORS, turn = c / S::FACTORS;
-        if (turn > 0 && !(ok = all_reached(shared_addr(&sm.factor_empty[s]), (turn + 1) & 1))) break;
-#pragma unroll
-        for (int i = 0; i < N; i++)
-          if (32 * i + lane < T) sm.factor[s][32 * i + lane] = f[i];
-        __syncwarp();
-        if (lane == 0) bar_arrive(shared_addr(&sm.factor_full[s]));
+      if (!ok) {                               // the products on their way
+        mma_commit(shared_addr(&sm.drained));
+        reached(shared_addr(&sm.drained), 0);
       }
     }
-  } else {                                     // ---- sums in binary32, outputs: half of a tile's columns, 32 output channels ----
-    constexpr int COLS = T / 2, CHUNK = COLS < 16 ? COLS : 16;
-    const int part = warp % 4, col0 = (warp - 4) / 4 * COLS;
-    for (int t = blockIdx.x; ok && tile.find(a, sm.tiles, t, T); t += gridDim.x) {
-      float sum[COLS];
+  } else if (warp < 4) {                       // ---- factors: of every other K block each, four rows a lane, loaded two K blocks of its own ahead ----
+    // A K block's factors are in their place when sum_full says that its sums are.  The place was the K block's 2 * SUMS in front of it: when the product of
+    // the one SUMS in front has ended, its accumulator had been given back by all who read these factors in front of it.
+    float x[2][4], w[2];
+    ProductTile at;                            // of the K block that is loaded next
+    int t = first, b = b0 + warp - 2, n = warp - 2;
+    bool there = b0 < b1 && at.find(a, sm.tiles, t, FEW_ROWS);
+    auto load = [&](int k) {
+      while (there && b >= b1) {
+        b -= b1 - b0, t += units;
+        there = at.find(a, sm.tiles, t, FEW_ROWS);
+      }
+      if (!there) return false;
+      w[k] = a.w_scale[((int64_t)at.group * a.tiles_n + at.n) * a.blocks + b];
+      const float *px = a.x_scale + b * a.x_scale_stride + at.row + lane;
+#pragma unroll
+      for (int i = 0; i < 4; i++) x[k][i] = 32 * i + lane < at.rows ? px[32 * i] : 0.0f;
+      b += 2;
+      return true;
+    };
+    Patience patience;
+    bool more[2] = {load(0), load(1)};
+    while (more[0]) {
+#pragma unroll
+      for (int k = 0; k < 2; k++) {
+        if (!more[k]) break;
+        const int buf = n % S::SUMS;
+        if (n >= S::SUMS) patience.wait(shared_addr(&sm.sum_full[buf]), (n / S::SUMS + 1) & 1);
+#pragma unroll
+        for (int i = 0; i < 4; i++) sm.factor[n % (2 * S::SUMS)][32 * i + lane] = x[k][i] * w[k];
+        __syncwarp();
+        if (lane == 0) bar_arrive(shared_addr(&sm.sum_full[buf]));
+        n += 2;
+        more[k] = load(k);
+      }
+    }
+    ok = !patience.gone();
+  }
+  // ---- sums in binary32, outputs: half of a tile's rows, 32 output channels ----
+  constexpr int COLS = FEW_ROWS / 2;
+  const int part = warp % 4, col0 = (warp - 4) / 4 * COLS;
+  float sum[COLS];
+  if (warp >= 4) {
+    Patience patience;
+    for (int t = first; tile.find(a, sm.tiles, t, FEW_ROWS); t += units) {
+      const int cols = tile.rows - col0;       // columns of this warp
 #pragma unroll
       for (int i = 0; i < COLS; i++) sum[i] = 0.0f;
-      for (int b = 0; b < a.blocks; b++, c++) {
-        const int half = c & 1, s = c % S::FACTORS;
-        if (!(ok = all_reached(shared_addr(&sm.factor_full[s]), (c / S::FACTORS) & 1))) break;
-        if (!(ok = all_reached(shared_addr(&sm.sum_full[half]), (c >> 1) & 1))) break;
+      for (int b = b0; b < b1; b++, c++) {
+        const int buf = c % S::SUMS;
+        patience.wait(shared_addr(&sm.sum_full[buf]), (c / S::SUMS) & 1);
         tmem_fence_after();
+        const float *f = &sm.factor[c % (2 * S::SUMS)][col0];
 #pragma unroll
-        for (int j = 0; j < COLS; j += CHUNK) {
-          uint32_t d[16];
-          static_assert(CHUNK == 16, "");
-          tmem_load16(tmem + half * T + col0 + j + ((uint32_t)part << 21), d);
-          tmem_wait_loads(d);
+        for (int j = 0; j < COLS; j += 16) {
+          if (j < cols) {
+            uint32_t d[16];
+            tmem_load16(tmem + buf * FEW_ROWS + col0 + j + ((uint32_t)part << 21), d);
+            tmem_wait_loads(d);
 #pragma unroll
-          for (int i = 0; i < 16; i += 4) {
-            const float4 f = *reinterpret_cast<const float4 *>(&sm.factor[s][col0 + j + i]);
-            sum[j + i] = fmaf(__uint_as_float(d[i]), f.x, sum[j + i]);
-            sum[j + i + 1] = fmaf(__uint_as_float(d[i + 1]), f.y, sum[j + i + 1]);
-            sum[j + i + 2] = fmaf(__uint_as_float(d[i + 2]), f.z, sum[j + i + 2]);
-            sum[j + i + 3] = fmaf(__uint_as_float(d[i + 3]), f.w, sum[j + i + 3]);
+            for (int i = 0; i < 16; i += 4) {
+              const float4 x = *reinterpret_cast<const float4 *>(&f[j + i]);
+              const float2 lo = __ffma2_rn(make_float2(__uint_as_float(d[i]), __uint_as_float(d[i + 1])), make_float2(x.x, x.y), make_float2(sum[j + i], sum[j + i + 1]));
+              const float2 hi = __ffma2_rn(make_float2(__uint_as_float(d[i + 2]), __uint_as_float(d[i + 3])), make_float2(x.z, x.w), make_float2(sum[j + i + 2], sum[j + i + 3]));
+              sum[j + i] = lo.x, sum[j + i + 1] = lo.y, sum[j + i + 2] = hi.x, sum[j + i + 3] = hi.y;
+            }
           }
         }
         tmem_fence_before();
         __syncwarp();
-        if (lane == 0) bar_arrive(shared_addr(&sm.sum_empty[half])), bar_arrive(shared_addr(&sm.factor_empty[s]));
+        if (lane == 0) bar_arrive(shared_addr(&sm.sum_empty[buf]));
       }
-      const int n = tile.n * PB + 32 * part + lane;
-      if (ok && n < a.outs) {
+      ok = !patience.gone();
+      if (a.split > 1) break;                  // (one tile)
+      const int n = tile.n * PB + 32 * part;
+      T *dst = static_cast<T *>(a.out) + (int64_t)(tile.row + col0) * a.out_stride + n;
 #pragma unroll
-        for (int i = 0; i < COLS; i++)
-          if (col0 + i < tile.rows) {
-            const int64_t at = (int64_t)(tile.row + col0 + i) * a.out_stride + n;
-            if (a.type == LQ_F32) static_cast<float *>(a.out)[at] = sum[i];
-            else if (a.type == LQ_F16) static_cast<__half *>(a.out)[at] = from_float<__half>(sum[i]);
-            else static_cast<__nv_bfloat16 *>(a.out)[at] = from_float<__nv_bfloat16>(sum[i]);
-          }
+      for (int j = 0; j < COLS; j += 16)
+        if (ok && j < cols && n < a.outs) store_columns<WIDE>(sm.out[warp - 4], dst + j * a.out_stride, a.out_stride, sum + j, min(cols - j, 16), a.outs - n, lane);
+    }
+  }
+  if (a.split > 1) {                           // (every CTA of the cluster has the same tile, and there is one)
+    float *const parts = reinterpret_cast<float *>(raw);
+    tile.find(a, sm.tiles, first, FEW_ROWS);
+    const int share = (tile.rows + a.split - 1) / a.split;   // rows of a CTA
+    __syncwarp();
+    cluster_sync();                            // nobody's tiles are looked at any more
+    if (warp >= 4) {
+      const uint32_t to = shared_addr(parts + rank * share * PB + 32 * part + lane);
+      int owner = col0 / share, in = col0 - owner * share;
+#pragma unroll
+      for (int i = 0; i < COLS; i++)
+        if (col0 + i < tile.rows) {
+          store_shared_of(shared_of(to + in * PB * 4, owner), sum[i]);
+          if (++in == share) in = 0, owner++;
+        }
+    }
+    __syncwarp();
+    cluster_sync();
+    if (warp >= 4 && __all_sync(0xffffffffu, ok)) {
+      const int rows = min(tile.rows - rank * share, share), n = tile.n * PB + 4 * lane;
+      for (int r = warp - 4; r < rows; r += 8) {
+        float4 v = *reinterpret_cast<const float4 *>(parts + r * PB + 4 * lane);
+        for (int q = 1; q < a.split; q++) {
+          const float4 y = *reinterpret_cast<const float4 *>(parts + (q * share + r) * PB + 4 * lane);
+          v = make_float4(v.x + y.x, v.y + y.y, v.z + y.z, v.w + y.w);
+        }
+        T *dst = static_cast<T *>(a.out) + (int64_t)(tile.row + rank * share + r) * a.out_stride + n;
+        const float x[4] = {v.x, v.y, v.z, v.w};
+        alignas(16) T y[4];
+        pack(x, y);
+        if (WIDE && n + 4 <= a.outs) {
+          store_row<true>(dst, y);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; e++)
+            if (n + e < a.outs) dst[e] = y[e];
+        }
       }
     }
   }
@@ -273,7 +350,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) product_few_kernel(const __gri
   tmem_fence_before();
   __syncthreads();
   tmem_fence_after();
-  if (warp == 1) tmem_free(tmem, 2 * T < 32 ? 32 : 2 * T);
+  if (warp == 1) tmem_free(tmem, S::SUMS * FEW_ROWS);
 }
 
 // ---------------------------------------------------------------------------------------------
