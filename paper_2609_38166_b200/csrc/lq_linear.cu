@@ -140,7 +140,8 @@ static lq_status launch_few_t(const ProductMaps &maps, const ProductArgs &a, int
 static lq_status launch_few(const lq_linear *s, ProductArgs a, const void *x, int64_t x_stride, const void *w, cudaStream_t stream) {
   a.tiles_n = (int)ceil_div(s->out, PB);
   ProductMaps maps{};
-  if (!byte_map(&maps.x, x, s->in, s->rows, 1, x_stride, x_stride * s->rows, FEW_BOX) ||
+  if (!byte_map(&maps.x, x, s->in, s->rows, 1, x_stride, x_stride * s->rows, FEW_ROWS) ||
+      !byte_map(&maps.more, x, s->in, s->rows, 1, x_stride, x_stride * s->rows, FEW_BOX) ||
       !byte_map(&maps.w, w, s->in, s->out, s->groups, s->in, (int64_t)s->in * s->out, PB))
     return LQ_ERR_CUDA;
   const long tiles = (ceil_div(s->rows, FEW_ROWS) + s->groups - 1) * a.tiles_n;   // at most
@@ -169,7 +170,7 @@ static lq_status launch_many(const lq_linear *s, ProductArgs a, const void *x, i
   const long pairs = (ceil_div(s->rows, MANY_ROWS) + s->groups - 1) * a.tiles_n;   // at most
   const unsigned size = type_size(s->type);
   const bool wide = aligned(a.out, 16) && a.out_stride % (16 / size) == 0 && a.out_stride * size * s->rows < (int64_t)1 << 40;   // (what a tensor map can say)
-  if (wide && !byte_map(&maps.out, a.out, (long)s->out * size, s->rows, 1, a.out_stride * size, a.out_stride * size * s->rows, 32, 64)) return LQ_ERR_CUDA;
+  if (wide && !byte_map(&maps.more, a.out, (long)s->out * size, s->rows, 1, a.out_stride * size, a.out_stride * size * s->rows, 32, 64)) return LQ_ERR_CUDA;
   if (s->type == LQ_F32) return wide ? launch_many_t<float, true>(maps, a, pairs, stream) : launch_many_t<float, false>(maps, a, pairs, stream);
   if (s->type == LQ_F16) return wide ? launch_many_t<__half, true>(maps, a, pairs, stream) : launch_many_t<__half, false>(maps, a, pairs, stream);
   return wide ? launch_many_t<__nv_bfloat16, true>(maps, a, pairs, stream) : launch_many_t<__nv_bfloat16, false>(maps, a, pairs, stream);

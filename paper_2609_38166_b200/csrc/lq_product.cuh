@@ -24,7 +24,7 @@ __device__ __forceinline__ bool reached(uint32_t bar, uint32_t parity) {
 }
 
 struct ProductMaps {
-  CUtensorMap x, w, out;
+  CUtensorMap x, w, more;                      // more: x in copies of FEW_BOX rows, or what is written
 };
 struct ProductArgs {
   const float *x_scale, *w_scale;
@@ -64,8 +64,14 @@ struct GroupTiles {
 
   // all threads of the CTA; `rows_per_tile` of T
   __device__ __forceinline__ void find(const ProductArgs &a, int T) {
-    for (int g = threadIdx.x; g <= a.groups; g += blockDim.x) start[g] = a.group_start ? min(max(a.group_start[g], 0), a.rows) : g ? a.rows : 0;
+    if (a.group_start) {
+      for (int g = threadIdx.x; g <= a.groups; g += blockDim.x) start[g] = min(max(a.group_start[g], 0), a.rows);
+      __syncthreads();
+      scan(a, T);
+    }
     __syncthreads();
+  }
+  __device__ __forceinline__ void scan(const ProductArgs &a, int T) {
     if (threadIdx.x < 32) {                    // (running maximum, running sum; 32 groups at a time)
       const int lane = threadIdx.x;
       int high = start[0], sum = 0;
@@ -94,13 +100,17 @@ struct GroupTiles {
       }
       if (lane == 0) first[a.groups] = sum;
     }
-    __syncthreads();
   }
 };
 
 struct ProductTile {
   int group, row, rows, n;                     // rows [row, row + rows), output channels from n * (channels of a tile) on
   __device__ __forceinline__ bool find(const ProductArgs &a, const GroupTiles &gt, int tile, int T) {
+    if (!a.group_start) {
+      const int tiles = (a.rows + T - 1) / T;
+      group = 0, n = tile / tiles, row = (tile - n * tiles) * T, rows = min(a.rows - row, T);
+      return n < a.tiles_n;
+    }
     if (tile >= gt.first[a.groups] * a.tiles_n) return false;
     const int q = tile / a.tiles_n;
     int lo = 0, hi = a.groups;                 // the last group with first <= q
@@ -125,7 +135,7 @@ struct ProductTile {
 // Where there are fewer tiles than SMs, the CTAs of a cluster share a tile's K blocks and add up their sums by way of one another's shared memory, each for
 // some of the rows, in the order of the CTAs.
 // ---------------------------------------------------------------------------------------------
-constexpr int FEW_THREADS = 384, FEW_ROWS = 128, FEW_BOX = 32;   // FEW_BOX: rows to a copy
+constexpr int FEW_THREADS = 384, FEW_ROWS = 128, FEW_BOX = 32;   // FEW_BOX: rows to a copy where there are few
 struct FewShared {
   static constexpr int STAGES = 6, SUMS = 4;
   static constexpr uint32_t W_BYTES = PB * PB, BOX_BYTES = FEW_BOX * PB;
@@ -169,34 +179,47 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) product_few_kernel(const __gri
     if (threadIdx.x == 0) atomicOr(&g_product_error, 2);
     return;
   }
-  if (threadIdx.x == 0) {
-    auto init = [](uint64_t &bar, int count) { bar_init(shared_addr(&bar), count); };
-    for (int i = 0; i < S::STAGES; i++) init(sm.full[i], 1), init(sm.empty[i], 1);
-    for (int i = 0; i < S::SUMS; i++) init(sm.sum_full[i], 2), init(sm.sum_empty[i], 8);
-    init(sm.drained, 1);
+  if (warp == 0) {
+    if (lane < S::STAGES) bar_init(shared_addr(&sm.full[lane]), 2), bar_init(shared_addr(&sm.empty[lane]), 1);
+    else if (lane < S::STAGES + S::SUMS) bar_init(shared_addr(&sm.sum_full[lane - S::STAGES]), 2), bar_init(shared_addr(&sm.sum_empty[lane - S::STAGES]), 8);
+    else if (lane == 31) bar_init(shared_addr(&sm.drained), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  } else if (warp == 1) {
+    tmem_alloc(shared_addr(&sm.tmem), S::SUMS * FEW_ROWS);
+  } else if (threadIdx.x == 64) {
+    tensor_map_prefetch(&maps.w), tensor_map_prefetch(a.rows > 2 * FEW_BOX ? &maps.x : &maps.more);
   }
-  if (warp == 1) tmem_alloc(shared_addr(&sm.tmem), S::SUMS * FEW_ROWS);
   tmem_fence_before();
   sm.tiles.find(a, FEW_ROWS);
   tmem_fence_after();
   const uint32_t tmem = sm.tmem;
+  // The sums of a split tile are handed over in the place of the outputs where they fit, else in that of the weights, when nobody uses them any more.
+  const bool small = (a.rows < FEW_ROWS ? a.rows : FEW_ROWS) + a.split <= (int)sizeof(sm.out) / (PB * 4);
+  if (a.split > 1 && small) cluster_arrive();
   const int rank = a.split > 1 ? cluster_rank() : 0, first = blockIdx.x / a.split, units = gridDim.x / a.split;
   const int b0 = a.blocks * rank / a.split, b1 = a.blocks * (rank + 1) / a.split;   // K blocks of this CTA
   bool ok = true;
   ProductTile tile;
   int c = 0;                                   // K blocks so far
-  if (warp == 0) {                             // ---- tensor copies ----
+  if (warp == 0 || warp == 3) {                // ---- tensor copies: the weights' and the rows', a thread each (a copy takes 200 clocks to issue) ----
     if (lane == 0) {
       for (int t = first; ok && tile.find(a, sm.tiles, t, FEW_ROWS); t += units) {
-        const int boxes = (tile.rows + FEW_BOX - 1) / FEW_BOX;
+        const int boxes = tile.rows > 2 * FEW_BOX ? FEW_ROWS / FEW_BOX : (tile.rows + FEW_BOX - 1) / FEW_BOX;
         for (int b = b0; b < b1; b++, c++) {
           const int s = c % S::STAGES, turn = c / S::STAGES;
           if (turn > 0 && !(ok = reached(shared_addr(&sm.empty[s]), (turn + 1) & 1))) break;
           const uint32_t bar = shared_addr(&sm.full[s]);
-          bar_expect(bar, S::W_BYTES + boxes * S::BOX_BYTES);
-          tensor_g2s(shared_addr(sm.w[s]), &maps.w, b * PB, tile.n * PB, tile.group, bar);
-          for (int i = 0; i < boxes; i++) tensor_g2s(shared_addr(sm.x[s]) + i * S::BOX_BYTES, &maps.x, b * PB, tile.row + i * FEW_BOX, 0, bar);
+          if (warp == 0) {
+            bar_expect(bar, S::W_BYTES);
+            tensor_g2s(shared_addr(sm.w[s]), &maps.w, b * PB, tile.n * PB, tile.group, bar);
+          } else {
+            bar_expect(bar, boxes * S::BOX_BYTES);
+            if (boxes == FEW_ROWS / FEW_BOX) {
+              tensor_g2s(shared_addr(sm.x[s]), &maps.x, b * PB, tile.row, 0, bar);
+            } else {
+              for (int i = 0; i < boxes; i++) tensor_g2s(shared_addr(sm.x[s]) + i * S::BOX_BYTES, &maps.more, b * PB, tile.row + i * FEW_BOX, 0, bar);
+            }
+          }
         }
       }
       if (!ok) {                               // the copies on their way, before their shared memory is gone
@@ -224,31 +247,33 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) product_few_kernel(const __gri
         reached(shared_addr(&sm.drained), 0);
       }
     }
-  } else if (warp < 4) {                       // ---- factors: of every other K block each, four rows a lane, loaded two K blocks of its own ahead ----
+  } else if (warp == 2) {                      // ---- factors: four rows a lane, loaded four K blocks ahead ----
     // A K block's factors are in their place when sum_full says that its sums are.  The place was the K block's 2 * SUMS in front of it: when the product of
     // the one SUMS in front has ended, its accumulator had been given back by all who read these factors in front of it.
-    float x[2][4], w[2];
+    constexpr int AHEAD = 4;
+    float x[AHEAD][4], w[AHEAD];
     ProductTile at;                            // of the K block that is loaded next
-    int t = first, b = b0 + warp - 2, n = warp - 2;
-    bool there = b0 < b1 && at.find(a, sm.tiles, t, FEW_ROWS);
+    int t = first, b = b0, n = 0;
+    bool there = at.find(a, sm.tiles, t, FEW_ROWS), more[AHEAD];
     auto load = [&](int k) {
-      while (there && b >= b1) {
-        b -= b1 - b0, t += units;
+      if (there && b == b1) {
+        b = b0, t += units;
         there = at.find(a, sm.tiles, t, FEW_ROWS);
       }
-      if (!there) return false;
+      more[k] = there;
+      if (!there) return;
       w[k] = a.w_scale[((int64_t)at.group * a.tiles_n + at.n) * a.blocks + b];
       const float *px = a.x_scale + b * a.x_scale_stride + at.row + lane;
 #pragma unroll
       for (int i = 0; i < 4; i++) x[k][i] = 32 * i + lane < at.rows ? px[32 * i] : 0.0f;
-      b += 2;
-      return true;
+      b++;
     };
     Patience patience;
-    bool more[2] = {load(0), load(1)};
+#pragma unroll
+    for (int k = 0; k < AHEAD; k++) load(k);
     while (more[0]) {
 #pragma unroll
-      for (int k = 0; k < 2; k++) {
+      for (int k = 0; k < AHEAD; k++) {
         if (!more[k]) break;
         const int buf = n % S::SUMS;
         if (n >= S::SUMS) patience.wait(shared_addr(&sm.sum_full[buf]), (n / S::SUMS + 1) & 1);
@@ -256,8 +281,8 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) product_few_kernel(const __gri
         for (int i = 0; i < 4; i++) sm.factor[n % (2 * S::SUMS)][32 * i + lane] = x[k][i] * w[k];
         __syncwarp();
         if (lane == 0) bar_arrive(shared_addr(&sm.sum_full[buf]));
-        n += 2;
-        more[k] = load(k);
+        n++;
+        load(k);
       }
     }
     ok = !patience.gone();
@@ -306,23 +331,27 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) product_few_kernel(const __gri
     }
   }
   if (a.split > 1) {                           // (every CTA of the cluster has the same tile, and there is one)
-    float *const parts = reinterpret_cast<float *>(raw);
+    float *const parts = reinterpret_cast<float *>(small ? &sm.out[0][0] : &sm.w[0][0]);
     tile.find(a, sm.tiles, first, FEW_ROWS);
     const int share = (tile.rows + a.split - 1) / a.split;   // rows of a CTA
     __syncwarp();
-    cluster_sync();                            // nobody's tiles are looked at any more
-    if (warp >= 4) {
+    if (!small) cluster_arrive();
+    cluster_wait();
+    if (warp >= 4 && col0 < tile.rows) {
       const uint32_t to = shared_addr(parts + rank * share * PB + 32 * part + lane);
       int owner = col0 / share, in = col0 - owner * share;
+      uint32_t at = shared_of(to + in * PB * 4, owner);
 #pragma unroll
-      for (int i = 0; i < COLS; i++)
-        if (col0 + i < tile.rows) {
-          store_shared_of(shared_of(to + in * PB * 4, owner), sum[i]);
-          if (++in == share) in = 0, owner++;
-        }
+      for (int i = 0; i < COLS; i++) {
+        if (col0 + i >= tile.rows) break;
+        store_shared_of(at, sum[i]);
+        at += PB * 4;
+        if (++in == share) in = 0, at = shared_of(to, ++owner < a.split ? owner : 0);
+      }
     }
     __syncwarp();
-    cluster_sync();
+    cluster_arrive();
+    cluster_wait();
     if (warp >= 4 && __all_sync(0xffffffffu, ok)) {
       const int rows = min(tile.rows - rank * share, share), n = tile.n * PB + 4 * lane;
       for (int r = warp - 4; r < rows; r += 8) {
@@ -545,7 +574,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1) pro
           fence_async_shared();
           __syncwarp();
           if (WIDE && rows == 32) {
-            if (lane == 0) tensor_s2g(&maps.out, shared_addr(stage), (n + N * i) * (int)sizeof(T), row, 0), copies_commit();
+            if (lane == 0) tensor_s2g(&maps.more, shared_addr(stage), (n + N * i) * (int)sizeof(T), row, 0), copies_commit();
           } else {
             copy_sums(stage, static_cast<T *>(a.out) + (int64_t)row * a.out_stride + n + N * i, a.out_stride, rows, a.outs - n - N * i, lane);
             __syncwarp();

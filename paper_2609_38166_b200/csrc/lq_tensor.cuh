@@ -181,9 +181,12 @@ __device__ __forceinline__ uint32_t shared_of(uint32_t addr, uint32_t rank) {
 // (Orders tensor memory's reads behind tmem_fence_before, and nothing that is in memory: with .release.cluster it waits for all of the thread's stores, and a
 // K block of a product took 1.25 us instead of 0.4.)
 __device__ __forceinline__ void bar_arrive_cluster(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
-// All threads of the cluster
+// All threads of the cluster, whole warps
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  cluster_arrive();
+  cluster_wait();
 }
 // To this CTA's shared memory, `bar` in either CTA's
 __device__ __forceinline__ void pair_tensor_g2s(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar) {
