@@ -137,6 +137,24 @@ static lq_status launch_few_t(const ProductMaps &maps, const ProductArgs &a, int
   }
   return LQ_OK;
 }
+// Which kernel: the one whose tiles take fewer rounds over the GPU, as a round of either takes the same time (32 K blocks: 16 - 19 us; 148 tiles of 128 x 128,
+// or 74 pairs of CTAs on 256 x 256), the one for few rows where they tie.  1024 rows x 4096 x 4096: 2 rounds 32.6 us, 1 round 19.3; 192 x 4096 x 12352: 2 rounds
+// 31.9, 1 round 19.1; 512 x 8192 x 1024: a quarter of a round 15.7, 1 round 29.3; 779 x 1296 x 1999: 1 round 12.2 and 15.1.
+// How many rows a group has is known on the device only: half a tile of every group is taken to be empty.  64 groups x 2048 x 1536 of 64 rows each 50 and 59 us, of 128
+// rows 56 and 62, of 192 rows 92 and 64.
+static bool are_few(const lq_linear *s, bool grouped, int split) {
+  const long few = ceil_div(s->out, PB), many = ceil_div(s->out, MANY_OUTS);
+  if (grouped) {
+    const double rows = (double)s->rows / s->groups;
+    return few * (rows / FEW_ROWS + 0.5) / SMS <= many * std::max(1.0, rows / MANY_ROWS + 0.5) / (SMS / 2);
+  }
+  return split > 1 || ceil_div(few * ceil_div(s->rows, FEW_ROWS), SMS) <= ceil_div(many * ceil_div(s->rows, MANY_ROWS), SMS / 2);
+}
+// Few rows: CTAs that share a tile's K blocks.  One row of 4096 x 4096 (32 tiles): 1, 2, 4 CTAs 20, 12, 7.8 us.
+static int split_of(const lq_linear *s, bool grouped) {
+  const long tiles = ceil_div(s->rows, FEW_ROWS) * ceil_div(s->out, PB), blocks = ceil_div(s->in, PB);
+  return grouped ? 1 : (int)std::max(1l, std::min({SMS / tiles, 8l, blocks / 2}));
+}
 static lq_status launch_few(const lq_linear *s, ProductArgs a, const void *x, int64_t x_stride, const void *w, cudaStream_t stream) {
   a.tiles_n = (int)ceil_div(s->out, PB);
   ProductMaps maps{};
@@ -145,7 +163,6 @@ static lq_status launch_few(const lq_linear *s, ProductArgs a, const void *x, in
       !byte_map(&maps.w, w, s->in, s->out, s->groups, s->in, (int64_t)s->in * s->out, PB))
     return LQ_ERR_CUDA;
   const long tiles = (ceil_div(s->rows, FEW_ROWS) + s->groups - 1) * a.tiles_n;   // at most
-  a.split = s->groups == 1 && !a.group_start ? (int)std::max(1l, std::min({SMS / tiles, 8l, (long)a.blocks / 2})) : 1;
   const int grid = (int)std::min<long>(tiles, SMS) * a.split;
   const bool wide = aligned(a.out, 16) && a.out_stride % (16 / type_size(s->type)) == 0;
   if (s->type == LQ_F32) return wide ? launch_few_t<float, true>(maps, a, grid, stream) : launch_few_t<float, false>(maps, a, grid, stream);
@@ -199,8 +216,9 @@ static lq_status product(const lq_linear *s, const uint8_t *x, int64_t x_stride,
   for (const Span &in : {Span{x, x_stride, s->in, s->rows, 1}, Span{x_scale, x_scale_stride, s->rows, blocks, 4},
                          Span{w, s->in, s->in, (long)s->out * s->groups, 1}, Span{w_scale, blocks, blocks, ceil_div(s->out, PB) * s->groups, 4}})
     if (spans_meet(o, in)) return LQ_ERR_UNSUPPORTED;
-  const ProductArgs a{x_scale, w_scale, out, x_scale_stride, out_stride, group_start, s->rows, blocks, s->out, s->groups, s->type, 0, 1};
-  if (s->rows >= 128 * s->groups) return launch_many(s, a, x, x_stride, w, cuda_stream(stream));
+  ProductArgs a{x_scale, w_scale, out, x_scale_stride, out_stride, group_start, s->rows, blocks, s->out, s->groups, s->type, 0, 1};
+  a.split = split_of(s, grouped);
+  if (!are_few(s, grouped, a.split)) return launch_many(s, a, x, x_stride, w, cuda_stream(stream));
   return launch_few(s, a, x, x_stride, w, cuda_stream(stream));
 }
 
