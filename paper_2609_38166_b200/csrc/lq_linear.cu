@@ -120,18 +120,18 @@ static lq_status give_shared(K kernel, size_t bytes, std::atomic<uint64_t> &read
   return LQ_OK;
 }
 
-template <typename T, bool WIDE>
+template <typename T, bool WIDE, int ROWS>
 static lq_status launch_few_t(const ProductMaps &maps, const ProductArgs &a, int grid, cudaStream_t stream) {
   static std::atomic<uint64_t> ready{0};
-  const lq_status rc = give_shared(product_few_kernel<T, WIDE>, sizeof(FewShared), ready);
+  const lq_status rc = give_shared(product_few_kernel<T, WIDE, ROWS>, sizeof(FewShared<ROWS>), ready);
   if (rc != LQ_OK) return rc;
   cudaLaunchAttribute cluster{};
   cluster.id = cudaLaunchAttributeClusterDimension;
   cluster.val.clusterDim.x = a.split, cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
   cudaLaunchConfig_t config{};
-  config.gridDim = dim3(grid), config.blockDim = dim3(FEW_THREADS), config.dynamicSmemBytes = sizeof(FewShared), config.stream = stream;
+  config.gridDim = dim3(grid), config.blockDim = dim3(FEW_THREADS), config.dynamicSmemBytes = sizeof(FewShared<ROWS>), config.stream = stream;
   config.attrs = &cluster, config.numAttrs = 1;
-  if (cudaLaunchKernelEx(&config, product_few_kernel<T, WIDE>, maps, a) != cudaSuccess) {
+  if (cudaLaunchKernelEx(&config, product_few_kernel<T, WIDE, ROWS>, maps, a) != cudaSuccess) {
     cudaGetLastError();
     return LQ_ERR_CUDA;
   }
@@ -151,23 +151,26 @@ static bool are_few(const lq_linear *s, bool grouped, int split) {
   return split > 1 || ceil_div(few * ceil_div(s->rows, FEW_ROWS), SMS) <= ceil_div(many * ceil_div(s->rows, MANY_ROWS), SMS / 2);
 }
 // Few rows: CTAs that share a tile's K blocks.  One row of 4096 x 4096 (32 tiles): 1, 2, 4 CTAs 20, 12, 7.8 us.
-static int split_of(const lq_linear *s, bool grouped) {
-  const long tiles = ceil_div(s->rows, FEW_ROWS) * ceil_div(s->out, PB), blocks = ceil_div(s->in, PB);
+static int split_of(const lq_linear *s, bool grouped, int rows) {
+  const long tiles = ceil_div(s->rows, rows) * ceil_div(s->out, PB), blocks = ceil_div(s->in, PB);
   return grouped ? 1 : (int)std::max(1l, std::min({SMS / tiles, 8l, blocks / 2}));
 }
+template <int ROWS>
 static lq_status launch_few(const lq_linear *s, ProductArgs a, const void *x, int64_t x_stride, const void *w, cudaStream_t stream) {
   a.tiles_n = (int)ceil_div(s->out, PB);
+  a.tiles_m.set((uint32_t)ceil_div(s->rows, ROWS));
+  a.share = a.blocks / a.split, a.more = a.blocks % a.split;
   ProductMaps maps{};
-  if (!byte_map(&maps.x, x, s->in, s->rows, 1, x_stride, x_stride * s->rows, FEW_ROWS) ||
+  if ((ROWS > FEW_BOX && !byte_map(&maps.x, x, s->in, s->rows, 1, x_stride, x_stride * s->rows, ROWS)) ||
       !byte_map(&maps.more, x, s->in, s->rows, 1, x_stride, x_stride * s->rows, FEW_BOX) ||
       !byte_map(&maps.w, w, s->in, s->out, s->groups, s->in, (int64_t)s->in * s->out, PB))
     return LQ_ERR_CUDA;
-  const long tiles = (ceil_div(s->rows, FEW_ROWS) + s->groups - 1) * a.tiles_n;   // at most
-  const int grid = (int)std::min<long>(tiles, SMS) * a.split;
+  const long tiles = (ceil_div(s->rows, ROWS) + s->groups - 1) * a.tiles_n;   // at most
+  const int grid = (int)std::min<long>(tiles, ROWS == FEW_ROWS ? SMS : 2 * SMS) * a.split;
   const bool wide = aligned(a.out, 16) && a.out_stride % (16 / type_size(s->type)) == 0;
-  if (s->type == LQ_F32) return wide ? launch_few_t<float, true>(maps, a, grid, stream) : launch_few_t<float, false>(maps, a, grid, stream);
-  if (s->type == LQ_F16) return wide ? launch_few_t<__half, true>(maps, a, grid, stream) : launch_few_t<__half, false>(maps, a, grid, stream);
-  return wide ? launch_few_t<__nv_bfloat16, true>(maps, a, grid, stream) : launch_few_t<__nv_bfloat16, false>(maps, a, grid, stream);
+  if (s->type == LQ_F32) return wide ? launch_few_t<float, true, ROWS>(maps, a, grid, stream) : launch_few_t<float, false, ROWS>(maps, a, grid, stream);
+  if (s->type == LQ_F16) return wide ? launch_few_t<__half, true, ROWS>(maps, a, grid, stream) : launch_few_t<__half, false, ROWS>(maps, a, grid, stream);
+  return wide ? launch_few_t<__nv_bfloat16, true, ROWS>(maps, a, grid, stream) : launch_few_t<__nv_bfloat16, false, ROWS>(maps, a, grid, stream);
 }
 
 template <typename T, bool WIDE>
@@ -180,6 +183,7 @@ static lq_status launch_many_t(const ProductMaps &maps, const ProductArgs &a, lo
 }
 static lq_status launch_many(const lq_linear *s, ProductArgs a, const void *x, int64_t x_stride, const void *w, cudaStream_t stream) {
   a.tiles_n = (int)ceil_div(s->out, MANY_OUTS);
+  a.tiles_m.set((uint32_t)ceil_div(s->rows, MANY_ROWS));
   ProductMaps maps{};
   if (!byte_map(&maps.x, x, s->in, s->rows, 1, x_stride, x_stride * s->rows, 128) ||
       !byte_map(&maps.w, w, s->in, s->out, s->groups, s->in, (int64_t)s->in * s->out, 128))
@@ -216,10 +220,14 @@ static lq_status product(const lq_linear *s, const uint8_t *x, int64_t x_stride,
   for (const Span &in : {Span{x, x_stride, s->in, s->rows, 1}, Span{x_scale, x_scale_stride, s->rows, blocks, 4},
                          Span{w, s->in, s->in, (long)s->out * s->groups, 1}, Span{w_scale, blocks, blocks, ceil_div(s->out, PB) * s->groups, 4}})
     if (spans_meet(o, in)) return LQ_ERR_UNSUPPORTED;
-  ProductArgs a{x_scale, w_scale, out, x_scale_stride, out_stride, group_start, s->rows, blocks, s->out, s->groups, s->type, 0, 1};
-  a.split = split_of(s, grouped);
+  ProductArgs a{x_scale, w_scale, out, x_scale_stride, out_stride, group_start, s->rows, blocks, s->out, s->groups, s->type, 0, 1, blocks, 0, {}};
+  if (s->rows <= FEW_BOX * (grouped ? s->groups : 1)) {
+    a.split = split_of(s, grouped, FEW_BOX);
+    return launch_few<FEW_BOX>(s, a, x, x_stride, w, cuda_stream(stream));
+  }
+  a.split = split_of(s, grouped, FEW_ROWS);
   if (!are_few(s, grouped, a.split)) return launch_many(s, a, x, x_stride, w, cuda_stream(stream));
-  return launch_few(s, a, x, x_stride, w, cuda_stream(stream));
+  return launch_few<FEW_ROWS>(s, a, x, x_stride, w, cuda_stream(stream));
 }
 
 // lq_check_device / lq_clear_device_flags: the flag of the kernels in this file

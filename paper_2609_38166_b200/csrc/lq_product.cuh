@@ -33,7 +33,8 @@ struct ProductArgs {
   const int32_t *group_start;                  // null: one group of all rows
   int rows, blocks, outs, groups, type;        // blocks: K blocks; outs: output channels
   int tiles_n;                                 // tiles of output channels
-  int split;                                   // CTAs of a cluster that share a tile's K blocks (few rows)
+  int split, share, more;                      // few rows: CTAs of a cluster that share a tile's K blocks, `share` each and one more to the first `more`
+  Divisor tiles_m;                             // without groups: division by the tiles of rows
 };
 
 // The same for warps whose lanes have to stay together: no lane leaves, it goes on with waits of one try each and says so in the end.  (A vote behind every wait
@@ -107,8 +108,7 @@ struct ProductTile {
   int group, row, rows, n;                     // rows [row, row + rows), output channels from n * (channels of a tile) on
   __device__ __forceinline__ bool find(const ProductArgs &a, const GroupTiles &gt, int tile, int T) {
     if (!a.group_start) {
-      const int tiles = (a.rows + T - 1) / T;
-      group = 0, n = tile / tiles, row = (tile - n * tiles) * T, rows = min(a.rows - row, T);
+      group = 0, n = a.tiles_m.quotient(tile), row = (tile - n * a.tiles_m.d) * T, rows = min(a.rows - row, T);
       return n < a.tiles_n;
     }
     if (tile >= gt.first[a.groups] * a.tiles_n) return false;
@@ -131,18 +131,20 @@ struct ProductTile {
 
 // ---------------------------------------------------------------------------------------------
 // Few rows: output channels are the rows of the accumulator (the lanes of tensor memory), rows of x its columns, as many as there are (in steps of 16).
-// The weights are what such a call reads, so all that counts is that they are on their way: up to 96 KB to an SM.
+// The weights are what such a call reads, so all that counts is that they are on their way: 96 KB to an SM, 128 KB with tiles of 32 rows.
 // Where there are fewer tiles than SMs, the CTAs of a cluster share a tile's K blocks and add up their sums by way of one another's shared memory, each for
 // some of the rows, in the order of the CTAs.
 // ---------------------------------------------------------------------------------------------
 constexpr int FEW_THREADS = 384, FEW_ROWS = 128, FEW_BOX = 32;   // FEW_BOX: rows to a copy where there are few
+// ROWS: rows of a tile, FEW_ROWS with one CTA to an SM or FEW_BOX with two
+template <int ROWS>
 struct FewShared {
-  static constexpr int STAGES = 6, SUMS = 4;
+  static constexpr int STAGES = ROWS == FEW_ROWS ? 6 : 4, SUMS = 4;
   static constexpr uint32_t W_BYTES = PB * PB, BOX_BYTES = FEW_BOX * PB;
   uint8_t w[STAGES][W_BYTES];                  // (behind a split tile's products: sums of all CTAs, [CTA][row][128 channels])
-  uint8_t x[STAGES][FEW_ROWS * PB];
+  uint8_t x[STAGES][ROWS * PB];
   uint8_t out[8][16 * 32 * 4];                 // 32 output channels of 16 rows, a warp each
-  float factor[2 * SUMS][FEW_ROWS];
+  float factor[2 * SUMS][ROWS];
   uint64_t full[STAGES], empty[STAGES], sum_full[SUMS], sum_empty[SUMS], drained;
   uint32_t tmem;
   GroupTiles tiles;
@@ -169,66 +171,78 @@ __device__ __forceinline__ void store_columns(uint8_t *stage, T *dst, int64_t st
   __syncwarp();
 }
 
-template <typename T, bool WIDE>
-__global__ void __launch_bounds__(FEW_THREADS, 1) product_few_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs a) {
+template <typename T, bool WIDE, int ROWS>
+__global__ void __launch_bounds__(FEW_THREADS, ROWS == FEW_ROWS ? 1 : 2) product_few_kernel(const __grid_constant__ ProductMaps maps, const ProductArgs a) {
   extern __shared__ __align__(1024) uint8_t raw[];
-  using S = FewShared;
+  using S = FewShared<ROWS>;
   S &sm = *reinterpret_cast<S *>(raw);
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   if (shared_addr(raw) % 1024 != 0) {          // (the swizzled tiles count on it)
     if (threadIdx.x == 0) atomicOr(&g_product_error, 2);
     return;
   }
+  const int rank = a.split > 1 ? cluster_rank() : 0, first = a.split > 1 ? blockIdx.x / a.split : blockIdx.x, units = a.split > 1 ? gridDim.x / a.split : gridDim.x;
+  const int b0 = rank * a.share + min(rank, a.more), b1 = b0 + a.share + (rank < a.more ? 1 : 0);   // K blocks of this CTA
+  bool ok = true;
+  ProductTile tile{};
+  int c = 0;                                   // K blocks so far
+  const int early = a.group_start ? 0 : min(S::STAGES, b1 - b0);
+  auto copy_w = [&](int s, int b) {
+    const uint32_t bar = shared_addr(&sm.full[s]);
+    bar_expect(bar, S::W_BYTES);
+    tensor_g2s(shared_addr(sm.w[s]), &maps.w, b * PB, tile.n * PB, tile.group, bar);
+  };
+  auto copy_x = [&](int s, int b) {
+    const uint32_t bar = shared_addr(&sm.full[s]);
+    if (ROWS > FEW_BOX && tile.rows > 2 * FEW_BOX) {
+      bar_expect(bar, ROWS * PB);
+      tensor_g2s(shared_addr(sm.x[s]), &maps.x, b * PB, tile.row, 0, bar);
+    } else {
+      const int boxes = (tile.rows + FEW_BOX - 1) / FEW_BOX;
+      bar_expect(bar, boxes * S::BOX_BYTES);
+      for (int i = 0; i < boxes; i++) tensor_g2s(shared_addr(sm.x[s]) + i * S::BOX_BYTES, &maps.more, b * PB, tile.row + i * FEW_BOX, 0, bar);
+    }
+  };
   if (warp == 0) {
     if (lane < S::STAGES) bar_init(shared_addr(&sm.full[lane]), 2), bar_init(shared_addr(&sm.empty[lane]), 1);
     else if (lane < S::STAGES + S::SUMS) bar_init(shared_addr(&sm.sum_full[lane - S::STAGES]), 2), bar_init(shared_addr(&sm.sum_empty[lane - S::STAGES]), 8);
     else if (lane == 31) bar_init(shared_addr(&sm.drained), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    __syncwarp();
+    // The first copies are on their way before anything else is set up (groups: before that it is not known which).
+    if (lane == 0 && early > 0) {
+      tile.find(a, sm.tiles, first, ROWS);
+      for (int i = 0; i < early; i++) copy_w(i, b0 + i), copy_x(i, b0 + i);
+    }
   } else if (warp == 1) {
-    tmem_alloc(shared_addr(&sm.tmem), S::SUMS * FEW_ROWS);
+    tmem_alloc(shared_addr(&sm.tmem), S::SUMS * ROWS);
   } else if (threadIdx.x == 64) {
-    tensor_map_prefetch(&maps.w), tensor_map_prefetch(a.rows > 2 * FEW_BOX ? &maps.x : &maps.more);
+    tensor_map_prefetch(ROWS > FEW_BOX && a.rows > 2 * FEW_BOX ? &maps.x : &maps.more);
   }
   tmem_fence_before();
-  sm.tiles.find(a, FEW_ROWS);
+  sm.tiles.find(a, ROWS);
   tmem_fence_after();
   const uint32_t tmem = sm.tmem;
   // The sums of a split tile are handed over in the place of the outputs where they fit, else in that of the weights, when nobody uses them any more.
-  const bool small = (a.rows < FEW_ROWS ? a.rows : FEW_ROWS) + a.split <= (int)sizeof(sm.out) / (PB * 4);
+  const bool small = (a.rows < ROWS ? a.rows : ROWS) + a.split <= (int)sizeof(sm.out) / (PB * 4);
   if (a.split > 1 && small) cluster_arrive();
-  const int rank = a.split > 1 ? cluster_rank() : 0, first = blockIdx.x / a.split, units = gridDim.x / a.split;
-  const int b0 = a.blocks * rank / a.split, b1 = a.blocks * (rank + 1) / a.split;   // K blocks of this CTA
-  bool ok = true;
-  ProductTile tile;
-  int c = 0;                                   // K blocks so far
   if (warp == 0 || warp == 3) {                // ---- tensor copies: the weights' and the rows', a thread each (a copy takes 200 clocks to issue) ----
     if (lane == 0) {
-      for (int t = first; ok && tile.find(a, sm.tiles, t, FEW_ROWS); t += units) {
-        const int boxes = tile.rows > 2 * FEW_BOX ? FEW_ROWS / FEW_BOX : (tile.rows + FEW_BOX - 1) / FEW_BOX;
-        for (int b = b0; b < b1; b++, c++) {
+      c = early;
+      for (int t = first; ok && tile.find(a, sm.tiles, t, ROWS); t += units)
+        for (int b = t == first ? b0 + early : b0; b < b1; b++, c++) {
           const int s = c % S::STAGES, turn = c / S::STAGES;
           if (turn > 0 && !(ok = reached(shared_addr(&sm.empty[s]), (turn + 1) & 1))) break;
-          const uint32_t bar = shared_addr(&sm.full[s]);
-          if (warp == 0) {
-            bar_expect(bar, S::W_BYTES);
-            tensor_g2s(shared_addr(sm.w[s]), &maps.w, b * PB, tile.n * PB, tile.group, bar);
-          } else {
-            bar_expect(bar, boxes * S::BOX_BYTES);
-            if (boxes == FEW_ROWS / FEW_BOX) {
-              tensor_g2s(shared_addr(sm.x[s]), &maps.x, b * PB, tile.row, 0, bar);
-            } else {
-              for (int i = 0; i < boxes; i++) tensor_g2s(shared_addr(sm.x[s]) + i * S::BOX_BYTES, &maps.more, b * PB, tile.row + i * FEW_BOX, 0, bar);
-            }
-          }
+          if (warp == 0) copy_w(s, b);
+          else copy_x(s, b);
         }
-      }
       if (!ok) {                               // the copies on their way, before their shared memory is gone
         for (int i = max(c - S::STAGES, 0); i < c; i++) reached(shared_addr(&sm.full[i % S::STAGES]), (i / S::STAGES) & 1);
       }
     }
   } else if (warp == 1) {                      // ---- products: one thread ----
     if (elect_one()) {
-      for (int t = first; ok && tile.find(a, sm.tiles, t, FEW_ROWS); t += units) {
+      for (int t = first; ok && tile.find(a, sm.tiles, t, ROWS); t += units) {
         const uint32_t what = mma_e4m3(PB, (tile.rows + 15) / 16 * 16);
         for (int b = b0; b < b1; b++, c++) {
           const int s = c % S::STAGES, turn = c / S::STAGES, buf = c % S::SUMS;
@@ -237,7 +251,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) product_few_kernel(const __gri
           tmem_fence_after();
           const Operand W = operand(shared_addr(sm.w[s]), 0, 1024), X = operand(shared_addr(sm.x[s]), 0, 1024);
 #pragma unroll
-          for (int k = 0; k < 4; k++) mma8_ss(tmem + buf * FEW_ROWS, W + 32 * k, X + 32 * k, what, k > 0);
+          for (int k = 0; k < 4; k++) mma8_ss(tmem + buf * ROWS, W + 32 * k, X + 32 * k, what, k > 0);
           mma_commit(shared_addr(&sm.sum_full[buf]));
           mma_commit(shared_addr(&sm.empty[s]));
         }
@@ -247,25 +261,25 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) product_few_kernel(const __gri
         reached(shared_addr(&sm.drained), 0);
       }
     }
-  } else if (warp == 2) {                      // ---- factors: four rows a lane, loaded four K blocks ahead ----
+  } else if (warp == 2) {                      // ---- factors: a lane has every 32nd row, loaded four K blocks ahead ----
     // A K block's factors are in their place when sum_full says that its sums are.  The place was the K block's 2 * SUMS in front of it: when the product of
     // the one SUMS in front has ended, its accumulator had been given back by all who read these factors in front of it.
     constexpr int AHEAD = 4;
-    float x[AHEAD][4], w[AHEAD];
+    float x[AHEAD][ROWS / 32], w[AHEAD];
     ProductTile at;                            // of the K block that is loaded next
     int t = first, b = b0, n = 0;
-    bool there = at.find(a, sm.tiles, t, FEW_ROWS), more[AHEAD];
+    bool there = at.find(a, sm.tiles, t, ROWS), more[AHEAD];
     auto load = [&](int k) {
       if (there && b == b1) {
         b = b0, t += units;
-        there = at.find(a, sm.tiles, t, FEW_ROWS);
+        there = at.find(a, sm.tiles, t, ROWS);
       }
       more[k] = there;
       if (!there) return;
       w[k] = a.w_scale[((int64_t)at.group * a.tiles_n + at.n) * a.blocks + b];
       const float *px = a.x_scale + b * a.x_scale_stride + at.row + lane;
 #pragma unroll
-      for (int i = 0; i < 4; i++) x[k][i] = 32 * i + lane < at.rows ? px[32 * i] : 0.0f;
+      for (int i = 0; i < ROWS / 32; i++) x[k][i] = 32 * i + lane < at.rows ? px[32 * i] : 0.0f;
       b++;
     };
     Patience patience;
@@ -278,7 +292,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) product_few_kernel(const __gri
         const int buf = n % S::SUMS;
         if (n >= S::SUMS) patience.wait(shared_addr(&sm.sum_full[buf]), (n / S::SUMS + 1) & 1);
 #pragma unroll
-        for (int i = 0; i < 4; i++) sm.factor[n % (2 * S::SUMS)][32 * i + lane] = x[k][i] * w[k];
+        for (int i = 0; i < ROWS / 32; i++) sm.factor[n % (2 * S::SUMS)][32 * i + lane] = x[k][i] * w[k];
         __syncwarp();
         if (lane == 0) bar_arrive(shared_addr(&sm.sum_full[buf]));
         n++;
@@ -288,12 +302,12 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) product_few_kernel(const __gri
     ok = !patience.gone();
   }
   // ---- sums in binary32, outputs: half of a tile's rows, 32 output channels ----
-  constexpr int COLS = FEW_ROWS / 2;
+  constexpr int COLS = ROWS / 2;
   const int part = warp % 4, col0 = (warp - 4) / 4 * COLS;
   float sum[COLS];
   if (warp >= 4) {
     Patience patience;
-    for (int t = first; tile.find(a, sm.tiles, t, FEW_ROWS); t += units) {
+    for (int t = first; tile.find(a, sm.tiles, t, ROWS); t += units) {
       const int cols = tile.rows - col0;       // columns of this warp
 #pragma unroll
       for (int i = 0; i < COLS; i++) sum[i] = 0.0f;
@@ -306,7 +320,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) product_few_kernel(const __gri
         for (int j = 0; j < COLS; j += 16) {
           if (j < cols) {
             uint32_t d[16];
-            tmem_load16(tmem + buf * FEW_ROWS + col0 + j + ((uint32_t)part << 21), d);
+            tmem_load16(tmem + buf * ROWS + col0 + j + ((uint32_t)part << 21), d);
             tmem_wait_loads(d);
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
@@ -332,7 +346,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) product_few_kernel(const __gri
   }
   if (a.split > 1) {                           // (every CTA of the cluster has the same tile, and there is one)
     float *const parts = reinterpret_cast<float *>(small ? &sm.out[0][0] : &sm.w[0][0]);
-    tile.find(a, sm.tiles, first, FEW_ROWS);
+    tile.find(a, sm.tiles, first, ROWS);
     const int share = (tile.rows + a.split - 1) / a.split;   // rows of a CTA
     __syncwarp();
     if (!small) cluster_arrive();
@@ -379,7 +393,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 1) product_few_kernel(const __gri
   tmem_fence_before();
   __syncthreads();
   tmem_fence_after();
-  if (warp == 1) tmem_free(tmem, S::SUMS * FEW_ROWS);
+  if (warp == 1) tmem_free(tmem, S::SUMS * ROWS);
 }
 
 // ---------------------------------------------------------------------------------------------
