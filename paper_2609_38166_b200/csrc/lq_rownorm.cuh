@@ -26,64 +26,65 @@ __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d
   return lo | (uint32_t)hi << 16;
 }
 
-// `n` of eight values at channel c of a row, of which the others are 0; all lanes of a warp together, sixteen with the channels of a block.
-template <bool WIDE, typename T>
-__device__ __forceinline__ void norm_store(const NormOut &o, int64_t row, int c, int n, const float (&y)[LINE]) {
+__device__ __forceinline__ float reciprocal_of(float x) {   // within a step
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// `n` of N values at channel c of a row, of which the others are 0; all lanes of a warp together, 128 / N with the channels of a block.
+template <bool WIDE, typename T, int N>
+__device__ __forceinline__ void norm_store(const NormOut &o, int64_t row, int c, int n, const float (&y)[N]) {
   if (o.out && n > 0) {
-    alignas(16) T t[LINE];
+    alignas(16) T t[N];
     pack(y, t);
     T *dst = static_cast<T *>(o.out) + row * o.out_stride + c;
     if (WIDE) {
       store_row<true>(dst, t);
     } else {
 #pragma unroll
-      for (int e = 0; e < LINE; e++)
+      for (int e = 0; e < N; e++)
         if (e < n) dst[e] = t[e];
     }
   }
   if (o.out8) {
     float top = 0.0f;
 #pragma unroll
-    for (int e = 0; e < LINE; e++) top = fmaxf(top, fabsf(y[e]));
+    for (int e = 0; e < N; e++) top = fmaxf(top, fabsf(y[e]));
 #pragma unroll
-    for (int m = 1; m < 16; m *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
-    const float scale = fmaxf(top * (1.0f / E4M3_MAX), LEAST_SCALE), by = 1.0f / scale;   // (an infinity makes all of its block NaN: 0 * inf)
-    uint32_t code[2];
+    for (int m = 1; m < 128 / N; m *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
+    const float scale = fmaxf(top * (1.0f / E4M3_MAX), LEAST_SCALE), by = reciprocal_of(scale);   // (an infinity makes all of its block NaN: 0 * inf)
+    alignas(16) uint32_t code[N / 4];
 #pragma unroll
-    for (int e = 0; e < 2; e++) code[e] = pack_e4m3(y[4 * e] * by, y[4 * e + 1] * by, y[4 * e + 2] * by, y[4 * e + 3] * by);
+    for (int e = 0; e < N / 4; e++) code[e] = pack_e4m3(y[4 * e] * by, y[4 * e + 1] * by, y[4 * e + 2] * by, y[4 * e + 3] * by);
     uint8_t *dst = o.out8 + row * o.out8_stride + c;
     if (WIDE) {
-      if (n > 0) *reinterpret_cast<uint2 *>(dst) = make_uint2(code[0], code[1]);
+      if (n > 0) store_row<true>(dst, reinterpret_cast<const uint8_t(&)[N]>(code));
     } else {
 #pragma unroll
-      for (int e = 0; e < LINE; e++)
+      for (int e = 0; e < N; e++)
         if (e < n) dst[e] = (uint8_t)(code[e / 4] >> 8 * (e % 4));
     }
     if (c % 128 == 0 && n > 0) o.scale[c / 128 * o.scale_stride + row] = scale;
   }
 }
 
-// Eight elements from channel c on; those from `n` on are 0.
-template <bool WIDE, typename T>
-__device__ __forceinline__ void norm_load(const T *src, int n, float (&x)[LINE]) {
-  alignas(16) T t[LINE];
-  if (WIDE) {
-    if (n > 0) load_row<true>(src, t);
+// N elements, of which `n` are there and the others 0.
+template <bool WIDE, typename T, int N>
+__device__ __forceinline__ void norm_load(const T *src, int n, T (&t)[N]) {
+  if (WIDE && n > 0) {
+    load_row<true>(src, t);
   } else {
 #pragma unroll
-    for (int e = 0; e < LINE; e++)
-      if (e < n) t[e] = src[e];
+    for (int e = 0; e < N; e++) {
+      t[e] = from_float<T>(0.0f);
+      if (!WIDE && e < n) t[e] = src[e];
+    }
   }
-  unpack(t, x);
-#pragma unroll
-  for (int e = 0; e < LINE; e++) x[e] = e < n ? x[e] : 0.0f;
 }
 
-// What a sum of squares of `count` channels makes of a norm.
-__device__ __forceinline__ float norm_factor(int norm, float squares, int count, float eps) {
-  if (norm == LQ_NORM_NONE) return 1.0f;
-  return rsqrtf((norm == LQ_NORM_RMS ? squares / (float)count : squares) + eps);
-}
+// What a sum of squares makes of a norm.
+__device__ __forceinline__ float norm_factor(float squares, float of, float eps) { return rsqrtf(fmaf(squares, of, eps)); }   // of: 1 / dim (RMS) or 1
 
 // ---- whole rows: h = x + residual, y = norm(h) w ----
 struct AddArgs {
@@ -93,35 +94,44 @@ struct AddArgs {
   int64_t x_stride, residual_stride;
   NormOut o;
   int tokens, dim, norm;
-  float eps;
+  float eps, of;
 };
 
-// blockDim: (threads of a row, rows)
+// blockDim: (threads of a row, rows).  A thread has V pieces; all of them are asked for before the first is written back: 16384 rows x 4096 channels, bf16 to
+// 8 bits with the residual, 84 -> 78 us, with a reciprocal for the quotient 72, 6.5 TB/s, the measured copy rate.
 template <typename T, bool WIDE, int V>
 __global__ void __launch_bounds__(512) norm_add_kernel(const AddArgs a) {
   __shared__ float part[16];
   const int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
   const bool there = row < a.tokens;
+  const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
+  T *r = static_cast<T *>(a.residual) + row * a.residual_stride;
+  alignas(16) T raw[V][LINE], more[V][LINE];
   float h[V][LINE];
   float squares = 0.0f;
 #pragma unroll
   for (int v = 0; v < V; v++) {
     const int c = (v * blockDim.x + threadIdx.x) * LINE, n = there ? min(a.dim - c, LINE) : 0;
-    norm_load<WIDE>(static_cast<const T *>(a.x) + row * a.x_stride + c, n, h[v]);
-    if (a.residual) {
-      T *r = static_cast<T *>(a.residual) + row * a.residual_stride + c;
-      float more[LINE];
-      norm_load<WIDE>(r, n, more);
+    norm_load<WIDE>(x + c, n, raw[v]);
+    if (a.residual) norm_load<WIDE>(r + c, n, more[v]);
+  }
 #pragma unroll
-      for (int e = 0; e < LINE; e++) h[v][e] += more[e];
+  for (int v = 0; v < V; v++) {
+    const int c = (v * blockDim.x + threadIdx.x) * LINE, n = there ? min(a.dim - c, LINE) : 0;
+    unpack(raw[v], h[v]);
+    if (a.residual) {
+      float y[LINE];
+      unpack(more[v], y);
+#pragma unroll
+      for (int e = 0; e < LINE; e++) h[v][e] += y[e];
       alignas(16) T t[LINE];
       pack(h[v], t);
       if (WIDE) {
-        if (n > 0) store_row<true>(r, t);
+        if (n > 0) store_row<true>(r + c, t);
       } else {
 #pragma unroll
         for (int e = 0; e < LINE; e++)
-          if (e < n) r[e] = t[e];
+          if (e < n) r[c + e] = t[e];
       }
     }
 #pragma unroll
@@ -136,7 +146,7 @@ __global__ void __launch_bounds__(512) norm_add_kernel(const AddArgs a) {
     __syncthreads();
     squares = part[first];
     for (int w = 1; w < warps; w++) squares += part[first + w];
-    factor = norm_factor(a.norm, squares, a.dim, a.eps);
+    factor = norm_factor(squares, a.of, a.eps);
   }
 #pragma unroll
   for (int v = 0; v < V; v++) {
@@ -161,47 +171,53 @@ struct GatedArgs {
   int64_t x_stride, z_stride;
   NormOut o;
   int tokens, heads, dim, norm, silu;
-  float eps;
+  float eps, of;
   int warps;                                  // warps of a row
   Divisor by_warps;
 };
 
-constexpr int GATED_THREADS = 256;
+constexpr int GATED_THREADS = 128, GATED_LINE = 16;   // channels of a lane
 
 __device__ __forceinline__ float gate_of(float z, int silu) {   // 1 / (1 + exp(-z)), times z; a quotient that overflows is a 0
-  float e, r;
+  float e;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.44269504088896340736f));
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+  const float r = reciprocal_of(1.0f + e);
   return silu ? z * r : r;
 }
 
-// A warp has 256 channels of a row: a head of 256, two of 128 or four of 64.
+// A warp has 512 channels of a row.  Sixteen channels to a lane, for what a lane does for all of them together (sums over lanes, scale, addresses) is as much
+// as what it does for eight: 16384 rows x 32 heads x 128 channels of bf16 to 8 bits 80 -> 65 us; ten CTAs to an SM 62.6, 5.4 TB/s, of binary32 79, 5.9 TB/s.  What is
+// left are two MUFU operations an element (30 us) next to the memory; four rows to a warp, or eight channels and four rows, take longer.
 template <typename X, typename T, bool WIDE>
-__global__ void __launch_bounds__(GATED_THREADS) norm_gate_kernel(const GatedArgs a) {
+__global__ void __launch_bounds__(GATED_THREADS, 10) norm_gate_kernel(const GatedArgs a) {
+  constexpr int N = GATED_LINE;
   const int lane = threadIdx.x % 32;
-  const uint32_t unit = blockIdx.x * (GATED_THREADS / 32) + threadIdx.x / 32;
-  const int64_t row = a.by_warps.quotient(unit);
-  if (row >= a.tokens) return;
-  const int c = ((unit - (uint32_t)row * a.warps) * 32 + lane) * LINE, n = c < a.heads * a.dim ? LINE : 0;
-  float x[LINE], z[LINE];
-  norm_load<WIDE>(static_cast<const X *>(a.x) + row * a.x_stride + c, n, x);
-  norm_load<WIDE>(static_cast<const T *>(a.z) + row * a.z_stride + c, n, z);
+  const uint32_t unit = blockIdx.x * (GATED_THREADS / 32) + threadIdx.x / 32, row = a.by_warps.quotient(unit);
+  if (row >= (uint32_t)a.tokens) return;
+  const int c = ((unit - row * a.warps) * 32 + lane) * N, n = c < a.heads * a.dim ? N : 0;
+  alignas(16) X xs[N];
+  alignas(16) T zs[N];
+  norm_load<WIDE>(static_cast<const X *>(a.x) + row * a.x_stride + c, n, xs);
+  norm_load<WIDE>(static_cast<const T *>(a.z) + row * a.z_stride + c, n, zs);
+  float x[N], z[N];
+  unpack(xs, x);
   float factor = 1.0f;
   if (a.norm != LQ_NORM_NONE) {
     float squares = 0.0f;
 #pragma unroll
-    for (int e = 0; e < LINE; e++) squares = fmaf(x[e], x[e], squares);
-    for (int m = 1; m < a.dim / LINE; m *= 2) squares += __shfl_xor_sync(0xffffffffu, squares, m);
-    factor = norm_factor(a.norm, squares, a.dim, a.eps);
+    for (int e = 0; e < N; e++) squares = fmaf(x[e], x[e], squares);
+    for (int m = 1; m < a.dim / N; m *= 2) squares += __shfl_xor_sync(0xffffffffu, squares, m);
+    factor = norm_factor(squares, a.of, a.eps);
   }
   if (a.norm == LQ_NORM_RMS && a.w) {
-    float w[LINE];
-    norm_load<WIDE>(a.w + c % a.dim, LINE, w);
+    float w[N];
+    norm_load<WIDE>(a.w + c % a.dim, N, w);
 #pragma unroll
-    for (int e = 0; e < LINE; e++) x[e] *= w[e];
+    for (int e = 0; e < N; e++) x[e] *= w[e];
   }
+  unpack(zs, z);
 #pragma unroll
-  for (int e = 0; e < LINE; e++) x[e] *= factor * gate_of(z[e], a.silu);
+  for (int e = 0; e < N; e++) x[e] *= factor * gate_of(z[e], a.silu);
   norm_store<WIDE, T>(a.o, row, c, n, x);
 }
 
