@@ -428,12 +428,19 @@ __device__ __forceinline__ void stage_sums(uint8_t *stage, const float2 *v, int 
   }
 }
 // From there to rows of which `rows`, and output channels of which `n` are there: neighbouring lanes write neighbouring channels.
-template <typename T>
+template <bool WIDE, typename T>
 __device__ __forceinline__ void copy_sums(const uint8_t *stage, T *dst, int64_t stride, int rows, int n, int lane) {
   constexpr int N = 64 / sizeof(T), F = 16 / sizeof(T);
-  if (lane >= N || lane >= n) return;
-#pragma unroll 1
-  for (int r = 0; r < rows; r++) dst[r * stride + lane] = reinterpret_cast<const T *>(stage + 64 * r + 16 * ((lane / F) ^ (r / 2 % 4)))[lane % F];
+  if (WIDE && n >= N) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const int r = 8 * i + lane / 4, u = lane % 4;
+      if (r < rows) *reinterpret_cast<uint4 *>(dst + r * stride + u * F) = *reinterpret_cast<const uint4 *>(stage + 64 * r + 16 * (u ^ (r / 2 % 4)));
+    }
+  } else if (lane < N && lane < n) {
+#pragma unroll 4
+    for (int r = 0; r < rows; r++) dst[r * stride + lane] = reinterpret_cast<const T *>(stage + 64 * r + 16 * ((lane / F) ^ (r / 2 % 4)))[lane % F];
+  }
 }
 
 template <typename T, bool WIDE>
@@ -549,6 +556,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1) pro
     const uint32_t full = shared_addr(&sm.sum_full[0]), empty = shared_of(shared_addr(&sm.sum_empty[0]), 0);
     Patience patience;
     for (int t = first; tile.find(a, sm.tiles, t, MANY_ROWS); t += units) {
+      const int rows = min(tile.rows - 128 * rank - 32 * part, 32);
       float2 sum[64];
 #pragma unroll
       for (int i = 0; i < 64; i++) sum[i] = make_float2(0.0f, 0.0f);
@@ -557,6 +565,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1) pro
         const int buf = c & 1;
         patience.wait(full + 8 * buf, (c >> 1) & 1);
         tmem_fence_after();
+        if (rows <= 0) {                       // (none of the warp's rows)
+          tmem_fence_before();
+          if (lane == 0) bar_arrive_cluster(empty + 8 * buf);
+          continue;
+        }
         uint32_t d[2][16];
         tmem_load16(from + buf * MANY_OUTS, d[0]);
         const float f = sm.factor[c & 3][half][32 * part + lane];
@@ -574,7 +587,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1) pro
           for (int i = 0; i < 8; i++) sum[8 * j + i] = __ffma2_rn(make_float2(__uint_as_float(d[j & 1][2 * i]), __uint_as_float(d[j & 1][2 * i + 1])), ff, sum[8 * j + i]);
         }
       }
-      const int n = tile.n * MANY_OUTS + 128 * half, row = tile.row + 128 * rank + 32 * part, rows = min(tile.rows - 128 * rank - 32 * part, 32);
+      const int n = tile.n * MANY_OUTS + 128 * half, row = tile.row + 128 * rank + 32 * part;
       ok = !patience.gone();
       constexpr int N = 64 / sizeof(T);
 #pragma unroll
@@ -590,7 +603,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1) pro
           if (WIDE && rows == 32) {
             if (lane == 0) tensor_s2g(&maps.more, shared_addr(stage), (n + N * i) * (int)sizeof(T), row, 0), copies_commit();
           } else {
-            copy_sums(stage, static_cast<T *>(a.out) + (int64_t)row * a.out_stride + n + N * i, a.out_stride, rows, a.outs - n - N * i, lane);
+            copy_sums<WIDE>(stage, static_cast<T *>(a.out) + (int64_t)row * a.out_stride + n + N * i, a.out_stride, rows, a.outs - n - N * i, lane);
             __syncwarp();
           }
         }
