@@ -498,7 +498,7 @@ lq_status lq_norm_gate(const lq_gated *shape, const void *o, int64_t o_stride, c
  *   x   : e4m3 [rows][in], strided rows, 16-byte aligned, stride a multiple of 16      x_scale : fp32 [ceil(in/128)][x_scale_stride]
  *   w   : e4m3 [out][in], dense, 16-byte aligned                                       w_scale : fp32 [ceil(out/128)][ceil(in/128)]
  *   out : [rows][out] of `type`, strided rows
- * `in` is a multiple of 16.
+ * `in` is a multiple of 16; in and out are at most 2^20, in * out and rows * x_stride below 2^40 (LQ_ERR_UNSUPPORTED beyond).
  * lq_product_groups: the rows of group g, group_start[g] to group_start[g+1] - 1 (int32 [groups + 1] in device memory, not decreasing), take
  * weight g: w [groups][out][in], w_scale [groups][ceil(out/128)][ceil(in/128)].  Groups may be empty; rows in front of group_start[0] and from
  * group_start[groups] on belong to nobody: they are not written, and what they hold does not matter.  At most LQ_MOST_GROUPS groups.

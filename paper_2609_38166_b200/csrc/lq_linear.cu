@@ -208,7 +208,8 @@ static lq_status product(const lq_linear *s, const uint8_t *x, int64_t x_stride,
   if (bad_count(s->rows) || s->in <= 0 || s->out <= 0 || s->groups <= 0 || s->type < LQ_BF16 || s->type > LQ_F32) return LQ_ERR_SHAPE;
   if (!grouped && s->groups != 1) return LQ_ERR_SHAPE;
   if (s->in % 16 != 0 || s->in > MOST_CHANNELS || s->out > MOST_CHANNELS || s->groups > MOST_GROUPS || s->rows > MOST_ROWS) return LQ_ERR_UNSUPPORTED;
-  if ((ceil_div(s->rows, 16) + s->groups) * ceil_div(s->out, PB) > INT32_MAX - 1024) return LQ_ERR_UNSUPPORTED;   // tiles
+  if ((ceil_div(s->rows, FEW_BOX) + s->groups) * ceil_div(s->out, PB) > INT32_MAX - 1024) return LQ_ERR_UNSUPPORTED;   // tiles
+  if ((int64_t)s->in * s->out >= (int64_t)1 << 40) return LQ_ERR_UNSUPPORTED;   // (what a tensor map can say)
   if (s->rows == 0) return LQ_OK;
   if ((rc = check_arrays(16, {x, w})) != LQ_OK) return rc;
   if ((rc = check_arrays(4, {x_scale, w_scale})) != LQ_OK) return rc;

@@ -555,6 +555,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1) pro
     const uint32_t from = tmem + 128 * half + ((uint32_t)part << 21);
     const uint32_t full = shared_addr(&sm.sum_full[0]), empty = shared_of(shared_addr(&sm.sum_empty[0]), 0);
     Patience patience;
+    int turns = 0;                             // copies so far
     for (int t = first; tile.find(a, sm.tiles, t, MANY_ROWS); t += units) {
       const int rows = min(tile.rows - 128 * rank - 32 * part, 32);
       float2 sum[64];
@@ -593,15 +594,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1) pro
 #pragma unroll
       for (int i = 0; i < 128 / N; i++)
         if (ok && rows > 0 && n + N * i < a.outs) {
-          uint8_t *const stage = sm.out[warp - 4][i % 2];
-          if (WIDE && rows == 32) copies_read<1>();   // (the one in front of the last was from this place)
+          // (a copy writes whole pieces of 16 bytes, and all rows)
+          const bool copied = WIDE && rows == 32 && n + N * (i + 1) <= a.outs;
+          uint8_t *const stage = sm.out[warp - 4][turns & 1];
+          if (copied) copies_read<1>();        // (the last but one was from this place)
           else copies_read<0>();
           __syncwarp();
           stage_sums<T>(stage, sum + N / 2 * i, lane);
           fence_async_shared();
           __syncwarp();
-          if (WIDE && rows == 32) {
+          if (copied) {
             if (lane == 0) tensor_s2g(&maps.more, shared_addr(stage), (n + N * i) * (int)sizeof(T), row, 0), copies_commit();
+            turns++;
           } else {
             copy_sums<WIDE>(stage, static_cast<T *>(a.out) + (int64_t)row * a.out_stride + n + N * i, a.out_stride, rows, a.outs - n - N * i, lane);
             __syncwarp();

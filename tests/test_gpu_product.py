@@ -37,7 +37,8 @@ def run(rows, cin, cout, dtype=torch.bfloat16, starts=None, groups=1, pad=(0, 0,
     ds = torch.full((s.shape[0], rows + pad[1]), float("nan"), device="cuda")[:, :rows]
     ds.copy_(s)
     buf = torch.full((rows + 2 * guard, cout + pad[2]), FILL, dtype=dtype, device="cuda")
-    out = buf[guard:guard + rows, pad[2] // 2:pad[2] // 2 + cout]
+    at = 8 if pad[2] >= 16 else 0 if pad[2] % 8 else pad[2] // 2
+    out = buf[guard:guard + rows, at:at + cout]
     sh = lq.ProductShape(rows, cin, cout, groups=groups, type=lq.TYPES[dtype])
     if starts is None:
         lq.product(sh, dx, ds, w[0].cuda(), ws[0].cuda(), out)
@@ -48,7 +49,7 @@ def run(rows, cin, cout, dtype=torch.bfloat16, starts=None, groups=1, pad=(0, 0,
     want, size = ref.product(x, s, w, ws, starts)
     close(got, want, size, dtype, cin)
     rest = buf.cpu()
-    rest[guard:guard + rows, pad[2] // 2:pad[2] // 2 + cout] = FILL
+    rest[guard:guard + rows, at:at + cout] = FILL
     assert (rest == FILL).all()
 
 
@@ -137,3 +138,18 @@ def test_the_same_call_gives_the_same_bits():
         for _ in range(5):
             lq.product(sh, x, s, w[0], ws[0], b)
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows", [5, 100, 300])
+@pytest.mark.parametrize("cout", [100, 1001])
+def test_rows_of_outputs_that_end_inside_a_piece(dtype, rows, cout):
+    """Rows that start at multiples of 16 bytes and end elsewhere: what lies behind them stays."""
+    run(rows, 256, cout, dtype, pad=(0, 0, -cout % 8 + 8))
+    run(rows, 256, cout, dtype, starts=[0, rows // 3, rows - 1], groups=2, pad=(0, 0, -cout % 8 + 8))
+
+
+@pytest.mark.parametrize("rows,cout", [(20000, 288), (20000, 32), (15000, 480)])
+def test_many_short_products(rows, cout):
+    """Tiles with an odd number of pieces of outputs, one after another in the same places of shared memory."""
+    run(rows, 128, cout)
