@@ -1,5 +1,10 @@
 // Products of e4m3 rows with e4m3 weights, scales for each 128 channels of a row and for each block of 128 x 128 of the weights:
 //     out[t][n] = sum_b xs[b][t] ws[n / 128][b] sum_{k in block b} x[t][k] w[n][k]
+//
+// The inner sums are tcgen05 products (kind::f8f6f4) of one K block, 128 channels, in tensor memory; its binary32 accumulator loses nothing to speak of (all of 32
+// to 4096 channels: off by 0.64 of 2^-23 of the sum over magnitudes at most).  The outer sum is taken in registers: every K block is read out of tensor memory and added with one
+// multiply-add an element, its factor xs ws.  So unlike a product without scales each K block is handed over twice, and that is what bounds the
+// large ones: see the kernel for many rows.  Nothing is kept between calls and there is no workspace.
 #pragma once
 #include "lq_rows.cuh"
 #include "lq_tensor.cuh"
@@ -23,20 +28,6 @@ __device__ __forceinline__ bool reached(uint32_t bar, uint32_t parity) {
   return true;
 }
 
-struct ProductMaps {
-  CUtensorMap x, w, more;                      // more: x in copies of FEW_BOX rows, or what is written
-};
-struct ProductArgs {
-  const float *x_scale, *w_scale;
-  void *out;
-  int64_t x_scale_stride, out_stride;
-  const int32_t *group_start;                  // null: one group of all rows
-  int rows, blocks, outs, groups, type;        // blocks: K blocks; outs: output channels
-  int tiles_n;                                 // tiles of output channels
-  int split, share, more;                      // few rows: CTAs of a cluster that share a tile's K blocks, `share` each and one more to the first `more`
-  Divisor tiles_m;                             // without groups: division by the tiles of rows
-};
-
 // The same for warps whose lanes have to stay together: no lane leaves, it goes on with waits of one try each and says so in the end.  (A vote behind every wait
 // and what hangs on it made a K block of a product 15 % longer.)
 struct Patience {
@@ -54,6 +45,20 @@ struct Patience {
     __syncwarp();
   }
   __device__ __forceinline__ bool gone() const { return __any_sync(0xffffffffu, limit == 1); }
+};
+
+struct ProductMaps {
+  CUtensorMap x, w, more;                      // more: x in copies of FEW_BOX rows, or what is written
+};
+struct ProductArgs {
+  const float *x_scale, *w_scale;
+  void *out;
+  int64_t x_scale_stride, out_stride;
+  const int32_t *group_start;                  // null: one group of all rows
+  int rows, blocks, outs, groups, type;        // blocks: K blocks; outs: output channels
+  int tiles_n;                                 // tiles of output channels
+  int split, share, more;                      // few rows: CTAs of a cluster that share a tile's K blocks, `share` each and one more to the first `more`
+  Divisor tiles_m;                             // without groups: division by the tiles of rows
 };
 
 // The tiles of all groups: a group's tiles of rows, for one tile of output channels after another (those that run at the same time have
@@ -131,9 +136,11 @@ struct ProductTile {
 
 // ---------------------------------------------------------------------------------------------
 // Few rows: output channels are the rows of the accumulator (the lanes of tensor memory), rows of x its columns, as many as there are (in steps of 16).
-// The weights are what such a call reads, so all that counts is that they are on their way: 96 KB to an SM, 128 KB with tiles of 32 rows.
+// The weights are what such a call reads, so all that counts is that they are on their way: 96 KB to an SM, 128 KB with tiles of 32 rows (two CTAs).
 // Where there are fewer tiles than SMs, the CTAs of a cluster share a tile's K blocks and add up their sums by way of one another's shared memory, each for
-// some of the rows, in the order of the CTAs.
+// some of the rows, in the order of the CTAs.  Four accumulators, so that no hand-over is waited for; a K block's factors arrive on the barrier of its sums.
+// Weights from memory (not L2): 128 groups of 0 - 100 rows x 2048 x 1536 68 us, 5.9 TB/s; one row of 4096 x 4096 8 us, of 4096 x 12352 14.5 us, 3.5 TB/s: 97 CTAs with 64 KB on
+// their way each, and 4 us until the first K block is there and after the last.
 // ---------------------------------------------------------------------------------------------
 constexpr int FEW_THREADS = 384, FEW_ROWS = 128, FEW_BOX = 32;   // FEW_BOX: rows to a copy where there are few
 // ROWS: rows of a tile, FEW_ROWS with one CTA to an SM or FEW_BOX with two
@@ -398,8 +405,17 @@ __global__ void __launch_bounds__(FEW_THREADS, ROWS == FEW_ROWS ? 1 : 2) product
 
 // ---------------------------------------------------------------------------------------------
 // Many rows: rows of x are the rows of the accumulator, a row's factor is one number of its thread.  Two CTAs of a cluster work on one tile of 256 rows and
-// 256 output channels: either has 128 rows of x and of the weights in its shared memory and 128 rows of the sums in its tensor memory.
-// Two accumulators: one is taken over while the next K block's product goes to the other.
+// 256 output channels: either has 128 rows of x and of the weights in its shared memory and 128 rows of the sums in its tensor memory, which halves what a tile
+// takes from L2 (64 KB a K block; at 13 TB/s that alone is 0.36 us, the products 0.28 us).  Two accumulators: one is taken over while the next K block's
+// product goes to the other.
+//   warp 0       tensor copies of this CTA's half of either operand, four to five K blocks ahead
+//   warp 1       one thread of the first CTA issues the products of both
+//   warps 2, 3   factors, to shared memory; they arrive on the barrier of the sums, so that there is one wait for both
+//   warps 4-11   a row and half of the output channels to a thread: sums in 128 registers; outputs by way of shared memory and tensor copies
+// A K block takes 0.49 us: 64 multiply-adds of pairs a thread (two warps of a scheduler 300 clocks, 370 with the loads of tensor memory, which also compete with the products
+// for it), the two barriers and the products' own 512 - 590 clocks in turn on two accumulators.  8192 x 4096 x 12352 352 us, 2.36 PFLOP/s (432 us, 1.92, in a
+// long loop under the power cap; the library's product with one scale for all 290 and 335 us); tensor pipe active 59 %.
+// Without any hand-over it would be 10 % less.  Halves of 128 output channels, sixteen warps for the sums or wider loads of tensor memory gave nothing.
 // ---------------------------------------------------------------------------------------------
 constexpr int MANY_THREADS = 384, MANY_ROWS = 256, MANY_OUTS = 256;
 struct ManyShared {

@@ -1,7 +1,7 @@
 // Norms in front of a projection and behind the recurrence, with 8-bit outputs: whole rows with the residual's addition, heads with a gate.
 //
 // Every element is read and written once and a row (a head) stays in registers between its sum of squares and its outputs: bound by memory.  A thread
-// has pieces of eight consecutive channels, so that sixteen neighbouring lanes have a block of 128 and its largest value is a butterfly over them.
+// has pieces of eight (heads: sixteen) consecutive channels, so that neighbouring lanes have a block of 128 and its largest value is a butterfly over them.
 #pragma once
 #include "lq_rows.cuh"
 
@@ -83,6 +83,41 @@ __device__ __forceinline__ void norm_load(const T *src, int n, T (&t)[N]) {
   }
 }
 
+// The same for rows of any alignment: a lane has every 32nd of the warp's 32 * N channels from c on, so that neighbouring lanes still have neighbours:
+// 16384 rows x 2001 channels of bf16 to 8 bits 74 us, with eight neighbours to a lane, one by one, 141.
+template <typename T, int N>
+__device__ __forceinline__ void norm_load_spread(const T *src, int n, int lane, T (&t)[N]) {   // n: channels from c on
+#pragma unroll
+  for (int e = 0; e < N; e++) {
+    t[e] = from_float<T>(0.0f);
+    if (32 * e + lane < n) t[e] = src[32 * e + lane];
+  }
+}
+template <typename T, int N>
+__device__ __forceinline__ void norm_store_spread(const NormOut &o, int64_t row, int c, int n, int lane, const float (&y)[N]) {
+  if (o.out) {
+    T *dst = static_cast<T *>(o.out) + row * o.out_stride + c;
+#pragma unroll
+    for (int e = 0; e < N; e++)
+      if (32 * e + lane < n) dst[32 * e + lane] = from_float<T>(y[e]);
+  }
+  if (o.out8) {
+    uint8_t *dst = o.out8 + row * o.out8_stride + c;
+#pragma unroll
+    for (int b = 0; b < N; b += 4) {          // a block of 128
+      float top = fmaxf(fmaxf(fabsf(y[b]), fabsf(y[b + 1])), fmaxf(fabsf(y[b + 2]), fabsf(y[b + 3])));
+#pragma unroll
+      for (int m = 1; m < 32; m *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
+      const float scale = fmaxf(top * (1.0f / E4M3_MAX), LEAST_SCALE), by = reciprocal_of(scale);
+      const uint32_t code = pack_e4m3(y[b] * by, y[b + 1] * by, y[b + 2] * by, y[b + 3] * by);
+#pragma unroll
+      for (int e = 0; e < 4; e++)
+        if (32 * (b + e) + lane < n) dst[32 * (b + e) + lane] = (uint8_t)(code >> 8 * e);
+      if (lane == 0 && 32 * b < n) o.scale[(c / 128 + b / 4) * o.scale_stride + row] = scale;
+    }
+  }
+}
+
 // What a sum of squares makes of a norm.
 __device__ __forceinline__ float norm_factor(float squares, float of, float eps) { return rsqrtf(fmaf(squares, of, eps)); }   // of: 1 / dim (RMS) or 1
 
@@ -109,15 +144,21 @@ __global__ void __launch_bounds__(512) norm_add_kernel(const AddArgs a) {
   alignas(16) T raw[V][LINE], more[V][LINE];
   float h[V][LINE];
   float squares = 0.0f;
+  const int lane = threadIdx.x % 32;
+  // a piece's first channel (of the warp's, where it is spread), and how many are there
+  auto channel = [&](int v) { return (v * (int)blockDim.x + (int)threadIdx.x - (WIDE ? 0 : lane)) * LINE; };
+  auto count = [&](int v) { return there ? a.dim - channel(v) : 0; };
+  auto load = [&](const auto *src, int v, auto &t) {
+    if constexpr (WIDE) norm_load<true>(src + channel(v), count(v), t);
+    else norm_load_spread(src + channel(v), count(v), lane, t);
+  };
 #pragma unroll
   for (int v = 0; v < V; v++) {
-    const int c = (v * blockDim.x + threadIdx.x) * LINE, n = there ? min(a.dim - c, LINE) : 0;
-    norm_load<WIDE>(x + c, n, raw[v]);
-    if (a.residual) norm_load<WIDE>(r + c, n, more[v]);
+    load(x, v, raw[v]);
+    if (a.residual) load(r, v, more[v]);
   }
 #pragma unroll
   for (int v = 0; v < V; v++) {
-    const int c = (v * blockDim.x + threadIdx.x) * LINE, n = there ? min(a.dim - c, LINE) : 0;
     unpack(raw[v], h[v]);
     if (a.residual) {
       float y[LINE];
@@ -126,12 +167,12 @@ __global__ void __launch_bounds__(512) norm_add_kernel(const AddArgs a) {
       for (int e = 0; e < LINE; e++) h[v][e] += y[e];
       alignas(16) T t[LINE];
       pack(h[v], t);
-      if (WIDE) {
-        if (n > 0) store_row<true>(r + c, t);
+      if constexpr (WIDE) {
+        if (count(v) > 0) store_row<true>(r + channel(v), t);
       } else {
 #pragma unroll
         for (int e = 0; e < LINE; e++)
-          if (e < n) r[c + e] = t[e];
+          if (32 * e + lane < count(v)) r[channel(v) + 32 * e + lane] = t[e];
       }
     }
 #pragma unroll
@@ -142,7 +183,7 @@ __global__ void __launch_bounds__(512) norm_add_kernel(const AddArgs a) {
 #pragma unroll
     for (int m = 1; m < 32; m *= 2) squares += __shfl_xor_sync(0xffffffffu, squares, m);
     const int warps = blockDim.x / 32, first = threadIdx.y * warps;
-    if (threadIdx.x % 32 == 0) part[first + threadIdx.x / 32] = squares;
+    if (lane == 0) part[first + threadIdx.x / 32] = squares;
     __syncthreads();
     squares = part[first];
     for (int w = 1; w < warps; w++) squares += part[first + w];
@@ -150,17 +191,17 @@ __global__ void __launch_bounds__(512) norm_add_kernel(const AddArgs a) {
   }
 #pragma unroll
   for (int v = 0; v < V; v++) {
-    const int c = (v * blockDim.x + threadIdx.x) * LINE, n = there ? min(a.dim - c, LINE) : 0;
-    float w[LINE];
     if (a.norm == LQ_NORM_RMS && a.w) {
-      norm_load<WIDE>(a.w + c, n, w);
+      float w[LINE];
+      load(a.w, v, w);
 #pragma unroll
       for (int e = 0; e < LINE; e++) h[v][e] *= factor * w[e];
     } else {
 #pragma unroll
       for (int e = 0; e < LINE; e++) h[v][e] *= factor;
     }
-    norm_store<WIDE, T>(a.o, row, c, n, h[v]);
+    if constexpr (WIDE) norm_store<true, T>(a.o, row, channel(v), count(v), h[v]);
+    else norm_store_spread<T>(a.o, row, channel(v), count(v), lane, h[v]);
   }
 }
 
