@@ -448,6 +448,7 @@ lq_status lq_scan_step(const lq_scan *shape, const lq_scan_io *io, float *o, int
  *
  * A row of e4m3 codes has a scale for every block of 128 consecutive channels (the last block of a row may be shorter):
  *     value = code * scale,     scale = max(max_block |y|, 448 * 2^-100) / 448,     code = y / scale rounded to e4m3 (nearest even)
+ * Arrays need the alignment of their elements only, except for x and w of the products.
  * scale lies block by block: fp32 [ceil(channels/128)][scale_stride], the scales of neighbouring rows side by side, scale_stride at least
  * the number of rows.  A block with an infinity stands for NaN throughout, a NaN for itself alone.  Codes are the 8-bit patterns of e4m3
  * (torch.float8_e4m3fn).
@@ -468,8 +469,22 @@ typedef struct {
   int type;    /* lq_type of x, residual and out */
   float eps;
 } lq_add;
-lq_status lq_norm_add(const lq_add *shape, const void *x, int64_t x_stride, void *residual, int64_t residual_stride, const float *w,
-                      void *out, int64_t out_stride, uint8_t *out8, int64_t out8_stride, float *scale, int64_t scale_stride, lq_stream stream);
+typedef struct {
+  const void *x;         /* lq_norm_gate: o              */
+  int64_t x_stride;
+  void *residual;        /* lq_norm_add, in and out      */
+  int64_t residual_stride;
+  const void *z;         /* lq_norm_gate                 */
+  int64_t z_stride;
+  const float *w;
+  void *out;
+  int64_t out_stride;
+  uint8_t *out8;
+  int64_t out8_stride;
+  float *scale;          /* where out8 is not null       */
+  int64_t scale_stride;
+} lq_norm_io;            /* what a form does not have is not looked at */
+lq_status lq_norm_add(const lq_add *shape, const lq_norm_io *io, lq_stream stream);
 
 /*
  * lq_norm_gate: the outputs of the recurrence normalised per head, weighted and gated:
@@ -488,8 +503,7 @@ typedef struct {
   int type;    /* lq_type of z and out  */
   float eps;
 } lq_gated;
-lq_status lq_norm_gate(const lq_gated *shape, const void *o, int64_t o_stride, const void *z, int64_t z_stride, const float *w,
-                       void *out, int64_t out_stride, uint8_t *out8, int64_t out8_stride, float *scale, int64_t scale_stride, lq_stream stream);
+lq_status lq_norm_gate(const lq_gated *shape, const lq_norm_io *io, lq_stream stream);
 
 /*
  * lq_product: rows of e4m3 codes times e4m3 weights, whose scales are of blocks of 128 output by 128 input channels:
@@ -511,10 +525,19 @@ typedef struct {
   int groups;   /* lq_product: 1             */
   int type;     /* lq_type of out            */
 } lq_linear;
-lq_status lq_product(const lq_linear *shape, const uint8_t *x, int64_t x_stride, const float *x_scale, int64_t x_scale_stride, const uint8_t *w,
-                     const float *w_scale, void *out, int64_t out_stride, lq_stream stream);
-lq_status lq_product_groups(const lq_linear *shape, const uint8_t *x, int64_t x_stride, const float *x_scale, int64_t x_scale_stride, const uint8_t *w,
-                            const float *w_scale, void *out, int64_t out_stride, const int32_t *group_start, lq_stream stream);
+typedef struct {
+  const uint8_t *x;
+  int64_t x_stride;
+  const float *x_scale;
+  int64_t x_scale_stride;
+  const uint8_t *w;
+  const float *w_scale;
+  void *out;
+  int64_t out_stride;
+  const int32_t *group_start;   /* lq_product: not looked at */
+} lq_product_io;
+lq_status lq_product(const lq_linear *shape, const lq_product_io *io, lq_stream stream);
+lq_status lq_product_groups(const lq_linear *shape, const lq_product_io *io, lq_stream stream);
 
 /*
  * Device-side error flags of the current device (0 = none), written to *flags (a host pointer).  Waits inside

@@ -34,6 +34,8 @@ struct NormIo {
   NormOut o;
 };
 
+static NormOut norm_out(const lq_norm_io *n) { return {n->out, n->out8, n->scale, n->out_stride, n->out8_stride, n->scale_stride}; }
+
 static lq_status check_norm_io(const NormIo &io, long tokens, long width, int type, bool in_place) {
   lq_status rc;
   const unsigned size = type_size(type);
@@ -201,16 +203,20 @@ static lq_status launch_many(const lq_linear *s, ProductArgs a, const void *x, i
   return wide ? launch_many_t<__nv_bfloat16, true>(maps, a, pairs, stream) : launch_many_t<__nv_bfloat16, false>(maps, a, pairs, stream);
 }
 
-static lq_status product(const lq_linear *s, const uint8_t *x, int64_t x_stride, const float *x_scale, int64_t x_scale_stride, const uint8_t *w,
-                         const float *w_scale, void *out, int64_t out_stride, const int32_t *group_start, bool grouped, lq_stream stream) {
+static lq_status product(const lq_linear *s, const lq_product_io *io, bool grouped, lq_stream stream) {
   lq_status rc;
-  if (!s) return LQ_ERR_NULL;
+  if (!s || !io) return LQ_ERR_NULL;
   if (bad_count(s->rows) || s->in <= 0 || s->out <= 0 || s->groups <= 0 || s->type < LQ_BF16 || s->type > LQ_F32) return LQ_ERR_SHAPE;
   if (!grouped && s->groups != 1) return LQ_ERR_SHAPE;
   if (s->in % 16 != 0 || s->in > MOST_CHANNELS || s->out > MOST_CHANNELS || s->groups > MOST_GROUPS || s->rows > MOST_ROWS) return LQ_ERR_UNSUPPORTED;
   if ((ceil_div(s->rows, FEW_BOX) + s->groups) * ceil_div(s->out, PB) > INT32_MAX - 1024) return LQ_ERR_UNSUPPORTED;   // tiles
   if ((int64_t)s->in * s->out >= (int64_t)1 << 40) return LQ_ERR_UNSUPPORTED;   // (what a tensor map can say)
   if (s->rows == 0) return LQ_OK;
+  const uint8_t *x = io->x, *w = io->w;
+  const float *x_scale = io->x_scale, *w_scale = io->w_scale;
+  void *out = io->out;
+  const int64_t x_stride = io->x_stride, x_scale_stride = io->x_scale_stride, out_stride = io->out_stride;
+  const int32_t *group_start = grouped ? io->group_start : nullptr;
   if ((rc = check_arrays(16, {x, w})) != LQ_OK) return rc;
   if ((rc = check_arrays(4, {x_scale, w_scale})) != LQ_OK) return rc;
   if ((rc = check_arrays(type_size(s->type), {out})) != LQ_OK) return rc;
@@ -248,37 +254,35 @@ using namespace lq;
 
 extern "C" {
 
-lq_status lq_norm_add(const lq_add *s, const void *x, int64_t x_stride, void *residual, int64_t residual_stride, const float *w, void *out,
-                      int64_t out_stride, uint8_t *out8, int64_t out8_stride, float *scale, int64_t scale_stride, lq_stream stream) {
-  if (!s) return LQ_ERR_NULL;
+lq_status lq_norm_add(const lq_add *s, const lq_norm_io *n, lq_stream stream) {
+  if (!s || !n) return LQ_ERR_NULL;
   if (bad_count(s->tokens) || s->dim <= 0 || s->norm < LQ_NORM_NONE || s->norm > LQ_NORM_RMS || s->type < LQ_BF16 || s->type > LQ_F32) return LQ_ERR_SHAPE;
   if (s->dim > LQ_NORM_ADD_MOST || s->tokens > MOST_ROWS) return LQ_ERR_UNSUPPORTED;
   if (s->tokens == 0) return LQ_OK;
   const unsigned size = type_size(s->type);
-  const NormIo io{{x, residual}, {x_stride, residual_stride}, {size, size}, true, w, {out, out8, scale, out_stride, out8_stride, scale_stride}};
+  const NormIo io{{n->x, n->residual}, {n->x_stride, n->residual_stride}, {size, size}, true, n->w, norm_out(n)};
   const lq_status rc = check_norm_io(io, s->tokens, s->dim, s->type, true);
   if (rc != LQ_OK) return rc;
-  const AddArgs a{x, residual, w, x_stride, residual_stride, io.o, s->tokens, s->dim, s->norm, s->eps, s->norm == LQ_NORM_RMS ? 1.0f / s->dim : 1.0f};
+  const AddArgs a{n->x, n->residual, n->w, n->x_stride, n->residual_stride, io.o, s->tokens, s->dim, s->norm, s->eps, s->norm == LQ_NORM_RMS ? 1.0f / s->dim : 1.0f};
   const bool wide = wide_norm(io, s->dim, s->type, LINE);
   if (s->type == LQ_F32) return wide ? launch_add<float, true>(a, cuda_stream(stream)) : launch_add<float, false>(a, cuda_stream(stream));
   if (s->type == LQ_F16) return wide ? launch_add<__half, true>(a, cuda_stream(stream)) : launch_add<__half, false>(a, cuda_stream(stream));
   return wide ? launch_add<__nv_bfloat16, true>(a, cuda_stream(stream)) : launch_add<__nv_bfloat16, false>(a, cuda_stream(stream));
 }
 
-lq_status lq_norm_gate(const lq_gated *s, const void *o, int64_t o_stride, const void *z, int64_t z_stride, const float *w, void *out,
-                       int64_t out_stride, uint8_t *out8, int64_t out8_stride, float *scale, int64_t scale_stride, lq_stream stream) {
-  if (!s) return LQ_ERR_NULL;
+lq_status lq_norm_gate(const lq_gated *s, const lq_norm_io *n, lq_stream stream) {
+  if (!s || !n) return LQ_ERR_NULL;
   if (bad_count(s->tokens) || s->heads <= 0 || s->dim <= 0 || s->norm < LQ_NORM_NONE || s->norm > LQ_NORM_RMS) return LQ_ERR_SHAPE;
   if ((s->silu != 0 && s->silu != 1) || s->type < LQ_BF16 || s->type > LQ_F32 || s->o_type < LQ_BF16 || s->o_type > LQ_F32) return LQ_ERR_SHAPE;
   const long warps = ceil_div((long)s->heads * s->dim, 32 * GATED_LINE);
   if ((s->dim != 64 && s->dim != 128 && s->dim != 256) || s->heads > (1 << 16) || warps * s->tokens > MOST_ROWS) return LQ_ERR_UNSUPPORTED;
   if (s->tokens == 0) return LQ_OK;
-  if (!z) return LQ_ERR_NULL;
+  if (!n->z) return LQ_ERR_NULL;
   const long width = (long)s->heads * s->dim;
-  const NormIo io{{o, z}, {o_stride, z_stride}, {type_size(s->o_type), type_size(s->type)}, false, w, {out, out8, scale, out_stride, out8_stride, scale_stride}};
+  const NormIo io{{n->x, n->z}, {n->x_stride, n->z_stride}, {type_size(s->o_type), type_size(s->type)}, false, n->w, norm_out(n)};
   const lq_status rc = check_norm_io(io, s->tokens, width, s->type, false);
   if (rc != LQ_OK) return rc;
-  GatedArgs a{o, z, w, o_stride, z_stride, io.o, s->tokens, s->heads, s->dim, s->norm, s->silu, s->eps, s->norm == LQ_NORM_RMS ? 1.0f / s->dim : 1.0f, (int)warps, {}};
+  GatedArgs a{n->x, n->z, n->w, n->x_stride, n->z_stride, io.o, s->tokens, s->heads, s->dim, s->norm, s->silu, s->eps, s->norm == LQ_NORM_RMS ? 1.0f / s->dim : 1.0f, (int)warps, {}};
   a.by_warps.set((uint32_t)warps);
   const bool wide = wide_norm(io, width, s->type, GATED_LINE);
   if (s->o_type == LQ_F32) return launch_gate<float>(a, s->type, wide, cuda_stream(stream));
@@ -286,14 +290,8 @@ lq_status lq_norm_gate(const lq_gated *s, const void *o, int64_t o_stride, const
   return launch_gate<__nv_bfloat16>(a, s->type, wide, cuda_stream(stream));
 }
 
-lq_status lq_product(const lq_linear *shape, const uint8_t *x, int64_t x_stride, const float *x_scale, int64_t x_scale_stride, const uint8_t *w,
-                     const float *w_scale, void *out, int64_t out_stride, lq_stream stream) {
-  return product(shape, x, x_stride, x_scale, x_scale_stride, w, w_scale, out, out_stride, nullptr, false, stream);
-}
+lq_status lq_product(const lq_linear *shape, const lq_product_io *io, lq_stream stream) { return product(shape, io, false, stream); }
 
-lq_status lq_product_groups(const lq_linear *shape, const uint8_t *x, int64_t x_stride, const float *x_scale, int64_t x_scale_stride, const uint8_t *w,
-                            const float *w_scale, void *out, int64_t out_stride, const int32_t *group_start, lq_stream stream) {
-  return product(shape, x, x_stride, x_scale, x_scale_stride, w, w_scale, out, out_stride, group_start, true, stream);
-}
+lq_status lq_product_groups(const lq_linear *shape, const lq_product_io *io, lq_stream stream) { return product(shape, io, true, stream); }
 
 }  // extern "C"

@@ -90,10 +90,7 @@ def lib() -> C.CDLL:
         L.lq_norm_rotate.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp]
         L.lq_scan_prompt.argtypes = [vp, vp, vp, i64, vp, vp]
         L.lq_scan_step.argtypes = [vp, vp, vp, i64, vp]
-        L.lq_norm_add.argtypes = [vp, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp]
-        L.lq_norm_gate.argtypes = [vp, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp]
-        L.lq_product.argtypes = [vp, vp, i64, vp, i64, vp, vp, vp, i64, vp]
-        L.lq_product_groups.argtypes = [vp, vp, i64, vp, i64, vp, vp, vp, i64, vp, vp]
+        L.lq_norm_add.argtypes = L.lq_norm_gate.argtypes = L.lq_product.argtypes = L.lq_product_groups.argtypes = [vp] * 3
         for name in ("lq_conv_prompt", "lq_conv_step", "lq_norm_rotate", "lq_scan_prompt", "lq_scan_step", "lq_norm_add", "lq_norm_gate", "lq_product",
                      "lq_product_groups"):
             getattr(L, name).restype = C.c_int
@@ -512,6 +509,17 @@ class _Gated(C.Structure):
     _fields_ = [(n, C.c_int) for n in ("tokens", "heads", "dim", "norm", "silu", "o_type", "type")] + [("eps", C.c_float)]
 
 
+class _NormIo(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("x_stride", C.c_int64), ("residual", C.c_void_p), ("residual_stride", C.c_int64), ("z", C.c_void_p), ("z_stride", C.c_int64),
+                ("w", C.c_void_p), ("out", C.c_void_p), ("out_stride", C.c_int64), ("out8", C.c_void_p), ("out8_stride", C.c_int64), ("scale", C.c_void_p),
+                ("scale_stride", C.c_int64)]
+
+
+class _ProductIo(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("x_stride", C.c_int64), ("x_scale", C.c_void_p), ("x_scale_stride", C.c_int64), ("w", C.c_void_p), ("w_scale", C.c_void_p),
+                ("out", C.c_void_p), ("out_stride", C.c_int64), ("group_start", C.c_void_p)]
+
+
 class _Linear(C.Structure):
     _fields_ = [(n, C.c_int) for n in ("rows", "in_", "out", "groups", "type")]
 
@@ -577,6 +585,8 @@ class ProductShape(_Kept):
 
 
 _SCAN_IO = struct.Struct("=3Q3q2Q2q8Q")        # lq_scan_io, as _ScanIo
+_NORM_IO = struct.Struct("=QqQqQqQQqQqQq")     # lq_norm_io, as _NormIo
+_PRODUCT_IO = struct.Struct("=QqQqQQQqQ")      # lq_product_io, as _ProductIo
 _device = torch._C._cuda_getDevice
 
 
@@ -589,6 +599,11 @@ def _rows(t, what: str, dtype, shape, device: int):
     """(address, row stride) of a tensor of ``shape``, [rows, ...], and ``dtype`` whose rows are contiguous, on the current device."""
     if t is None or t.dtype is not dtype or t.shape != shape or t.get_device() != device:
         _refuse(t, what, (dtype, shape))
+    if len(shape) == 2:                      # (most of them: a call is marshalled in half the time)
+        stride, one = t.stride()
+        if one != 1 and shape[1] != 1 and shape[0] > 0:
+            _refuse(t, what, (dtype, shape, "contiguous rows"))
+        return t.data_ptr(), stride if shape[0] > 1 else shape[1]
     if t.is_contiguous():
         return t.data_ptr(), t.stride(0) if shape[0] > 1 else math.prod(shape[1:])
     stride, run = t.stride(), 1
@@ -701,11 +716,12 @@ def scan_step(sh: ScanShape, q, k, v, beta, alpha, o, S, slots=None, A=None, dt_
         _check(rc, "lq_scan_step")
 
 
-def _norm_out(out, out8, scale, dt, rows, scales, d: int):
-    """The six arguments of a norm's outputs."""
-    none = (None, 0)
-    return (*(none if out is None else _rows(out, "out", dt, rows, d)), *(none if out8 is None else _rows(out8, "out8", E4M3, rows, d)),
-            *(none if scale is None else _rows(scale, "scale", torch.float32, scales, d)))
+def _norm_io(d: int, x, residual, z, w, dim, out, out8, scale, dt, rows, scales) -> bytes:
+    """lq_norm_io; x, residual and z as (address, stride)."""
+    po, so = (0, 0) if out is None else _rows(out, "out", dt, rows, d)
+    p8, s8 = (0, 0) if out8 is None else _rows(out8, "out8", E4M3, rows, d)
+    ps, ss = (0, 0) if scale is None else _rows(scale, "scale", torch.float32, scales, d)
+    return _NORM_IO.pack(*x, *residual, *z, _dense(w, "w", torch.float32, dim, d) or 0, po, so, p8, s8, ps, ss)
 
 
 def norm_add(sh: AddShape, x, residual=None, w=None, out=None, out8=None, scale=None, stream=None) -> None:
@@ -713,9 +729,9 @@ def norm_add(sh: AddShape, x, residual=None, w=None, out=None, out8=None, scale=
     ``out8`` float8_e4m3fn [tokens, dim] with ``scale`` fp32 [ceil(dim/128), tokens]; ``out`` or ``out8`` may be None.  Rows of all may be strided."""
     ref, (dt, rows, dim, scales) = sh.kept()
     d = _device()
-    px, sx = _rows(x, "x", dt, rows, d)
-    pr, sr = (None, 0) if residual is None else _rows(residual, "residual", dt, rows, d)
-    rc = (_lib or lib()).lq_norm_add(ref, px, sx, pr, sr, _dense(w, "w", torch.float32, dim, d), *_norm_out(out, out8, scale, dt, rows, scales, d), _stream(stream))
+    px = _rows(x, "x", dt, rows, d)
+    pr = (0, 0) if residual is None else _rows(residual, "residual", dt, rows, d)
+    rc = (_lib or lib()).lq_norm_add(ref, _norm_io(d, px, pr, (0, 0), w, dim, out, out8, scale, dt, rows, scales), _stream(stream))
     if rc:
         _check(rc, "lq_norm_add")
 
@@ -725,9 +741,9 @@ def norm_gate(sh: GatedShape, o, z, w=None, out=None, out8=None, scale=None, str
     [tokens, heads * dim] with ``scale`` fp32 [ceil(heads * dim / 128), tokens]; ``out`` or ``out8`` may be None.  Rows of all may be strided."""
     ref, (odt, dt, heads, rows, dim, scales) = sh.kept()
     d = _device()
-    po, so = _rows(o, "o", odt, heads, d)
-    pz, sz = _rows(z, "z", dt, heads, d)
-    rc = (_lib or lib()).lq_norm_gate(ref, po, so, pz, sz, _dense(w, "w", torch.float32, dim, d), *_norm_out(out, out8, scale, dt, rows, scales, d), _stream(stream))
+    po = _rows(o, "o", odt, heads, d)
+    pz = _rows(z, "z", dt, heads, d)
+    rc = (_lib or lib()).lq_norm_gate(ref, _norm_io(d, po, (0, 0), pz, w, dim, out, out8, scale, dt, rows, scales), _stream(stream))
     if rc:
         _check(rc, "lq_norm_gate")
 
@@ -737,10 +753,9 @@ def product(sh: ProductShape, x, x_scale, w, w_scale, out, stream=None) -> None:
     three may be strided), ``w`` float8_e4m3fn [channels_out, channels_in], ``w_scale`` fp32 [ceil(channels_out/128), ceil(channels_in/128)]."""
     ref, (dt, rows, scales, weights, w_scales, outs, _, _, _) = sh.kept()
     d, f32 = _device(), torch.float32
-    px, sx = _rows(x, "x", E4M3, rows, d)
-    ps, ss = _rows(x_scale, "x_scale", f32, scales, d)
-    po, so = _rows(out, "out", dt, outs, d)
-    rc = (_lib or lib()).lq_product(ref, px, sx, ps, ss, _dense(w, "w", E4M3, weights, d), _dense(w_scale, "w_scale", f32, w_scales, d), po, so, _stream(stream))
+    io = _PRODUCT_IO.pack(*_rows(x, "x", E4M3, rows, d), *_rows(x_scale, "x_scale", f32, scales, d), _dense(w, "w", E4M3, weights, d) or 0,
+                          _dense(w_scale, "w_scale", f32, w_scales, d) or 0, *_rows(out, "out", dt, outs, d), 0)
+    rc = (_lib or lib()).lq_product(ref, io, _stream(stream))
     if rc:
         _check(rc, "lq_product")
 
@@ -750,11 +765,10 @@ def product_groups(sh: ProductShape, x, x_scale, w, w_scale, out, group_start, s
     ceil(channels_in/128)]; ``group_start`` int32 [groups + 1]."""
     ref, (dt, rows, scales, _, _, outs, weights, w_scales, starts) = sh.kept()
     d, f32 = _device(), torch.float32
-    px, sx = _rows(x, "x", E4M3, rows, d)
-    ps, ss = _rows(x_scale, "x_scale", f32, scales, d)
-    po, so = _rows(out, "out", dt, outs, d)
-    rc = (_lib or lib()).lq_product_groups(ref, px, sx, ps, ss, _dense(w, "w", E4M3, weights, d), _dense(w_scale, "w_scale", f32, w_scales, d), po, so,
-                                           _dense(group_start, "group_start", torch.int32, starts, d), _stream(stream))
+    io = _PRODUCT_IO.pack(*_rows(x, "x", E4M3, rows, d), *_rows(x_scale, "x_scale", f32, scales, d), _dense(w, "w", E4M3, weights, d) or 0,
+                          _dense(w_scale, "w_scale", f32, w_scales, d) or 0, *_rows(out, "out", dt, outs, d),
+                          _dense(group_start, "group_start", torch.int32, starts, d) or 0)
+    rc = (_lib or lib()).lq_product_groups(ref, io, _stream(stream))
     if rc:
         _check(rc, "lq_product_groups")
 

@@ -19,29 +19,31 @@ def L():
     return lq.lib()
 
 
-def add(L, sh, x=X, xs=None, r=R, rs=None, w=W, out=OUT, outs=None, out8=OUT8, out8s=None, scale=SCALE, scales=None):
+def add(L, sh, x=X, xs=None, r=R, rs=None, w=W, out=OUT, outs=None, out8=OUT8, out8s=None, scale=SCALE, scales=None, no_io=False):
     d = lambda v: v if v is not None else sh.dim if sh else 0                     # noqa: E731
-    return L.lq_norm_add(C.byref(sh.c()) if sh else None, x, d(xs), r, d(rs), w, out, d(outs), out8, d(out8s), scale,
-                         scales if scales is not None else sh.tokens if sh else 0, None)
+    io = lq._NormIo(x=x, x_stride=d(xs), residual=r, residual_stride=d(rs), w=w, out=out, out_stride=d(outs), out8=out8, out8_stride=d(out8s), scale=scale,
+                    scale_stride=scales if scales is not None else sh.tokens if sh else 0)
+    return L.lq_norm_add(C.byref(sh.c()) if sh else None, None if no_io else C.byref(io), None)
 
 
-def gate(L, sh, o=X, os=None, z=R, zs=None, w=W, out=OUT, outs=None, out8=OUT8, out8s=None, scale=SCALE, scales=None):
+def gate(L, sh, o=X, os=None, z=R, zs=None, w=W, out=OUT, outs=None, out8=OUT8, out8s=None, scale=SCALE, scales=None, no_io=False):
     d = lambda v: v if v is not None else sh.heads * sh.dim if sh else 0          # noqa: E731
-    return L.lq_norm_gate(C.byref(sh.c()) if sh else None, o, d(os), z, d(zs), w, out, d(outs), out8, d(out8s), scale,
-                          scales if scales is not None else sh.tokens if sh else 0, None)
+    io = lq._NormIo(x=o, x_stride=d(os), z=z, z_stride=d(zs), w=w, out=out, out_stride=d(outs), out8=out8, out8_stride=d(out8s), scale=scale,
+                    scale_stride=scales if scales is not None else sh.tokens if sh else 0)
+    return L.lq_norm_gate(C.byref(sh.c()) if sh else None, None if no_io else C.byref(io), None)
 
 
-def product(L, sh, x=X, xs=None, s=SCALE, ss=None, w=W, ws=R, out=OUT, outs=None, start=None, groups=False):
-    args = [C.byref(sh.c()) if sh else None, x, xs if xs is not None else sh.channels_in if sh else 0, s, ss if ss is not None else sh.rows if sh else 0, w, ws, out,
-            outs if outs is not None else sh.channels_out if sh else 0]
-    return L.lq_product_groups(*args, start, None) if groups else L.lq_product(*args, None)
+def product(L, sh, x=X, xs=None, s=SCALE, ss=None, w=W, ws=R, out=OUT, outs=None, start=None, groups=False, no_io=False):
+    io = lq._ProductIo(x=x, x_stride=xs if xs is not None else sh.channels_in if sh else 0, x_scale=s, x_scale_stride=ss if ss is not None else sh.rows if sh else 0, w=w,
+                       w_scale=ws, out=out, out_stride=outs if outs is not None else sh.channels_out if sh else 0, group_start=start)
+    return (L.lq_product_groups if groups else L.lq_product)(C.byref(sh.c()) if sh else None, None if no_io else C.byref(io), None)
 
 
 @pytest.mark.parametrize("call,sh", [(add, lq.AddShape(40, 256)), (gate, lq.GatedShape(40, 2, dim=128))], ids=["add", "gate"])
 def test_norm_refusals(L, call, sh):
     rep = lambda **kw: dataclasses.replace(sh, **kw)                              # noqa: E731
     first, second = ("x", "r") if call is add else ("o", "z")
-    assert call(L, None) == NULL
+    assert call(L, None) == NULL and call(L, sh, no_io=True) == NULL
     for bad in (rep(tokens=-1), rep(dim=0), rep(dim=-1), rep(norm=-1), rep(norm=3), rep(type=-1), rep(type=3)):
         assert call(L, bad) == SHAPE, bad
     if call is add:
@@ -74,7 +76,7 @@ def test_product_refusals(L):
     rep = lambda **kw: dataclasses.replace(sh, **kw)                              # noqa: E731
     for groups in (False, True):
         go = lambda of, **kw: product(L, of, groups=groups, **{"start": X << 4, **kw})   # noqa: E731
-        assert go(None) == NULL
+        assert go(None) == NULL and go(sh, no_io=True) == NULL
         for bad in (rep(rows=-1), rep(channels_in=0), rep(channels_out=0), rep(groups=0), rep(groups=-1), rep(type=3), rep(type=-1)):
             assert go(bad) == SHAPE, bad
         for bad in (rep(channels_in=250), rep(channels_in=8), rep(channels_in=2 ** 20 + 16), rep(channels_out=2 ** 20 + 1), rep(rows=2 ** 31 - 1),
@@ -143,6 +145,23 @@ def check(call, args, required):
 
 def zeros(*shape, dtype=torch.bfloat16):
     return torch.zeros(shape).to(dtype)
+
+
+def test_packed_arguments_are_the_structs(host):
+    f32 = torch.float32
+    assert lq._NORM_IO.size == C.sizeof(lq._NormIo) and lq._PRODUCT_IO.size == C.sizeof(lq._ProductIo)
+    names = [n for n, _ in lq._NormIo._fields_]
+    io = lq._NormIo.from_buffer_copy(lq._NORM_IO.pack(*range(1, 14)))
+    assert [getattr(io, n) for n in names] == list(range(1, 14))
+    names = [n for n, _ in lq._ProductIo._fields_]
+    io = lq._ProductIo.from_buffer_copy(lq._PRODUCT_IO.pack(*range(1, 10)))
+    assert [getattr(io, n) for n in names] == list(range(1, 10))
+    x, r = zeros(5, 300), zeros(5, 320)[:, 10:310]
+    out8, scale, w = zeros(5, 300, dtype=lq.E4M3), zeros(3, 8, dtype=f32)[:, :5], zeros(300, dtype=f32)
+    got = lq._NormIo.from_buffer_copy(lq._norm_io(-1, lq._rows(x, "x", x.dtype, (5, 300), -1), lq._rows(r, "r", r.dtype, (5, 300), -1), (0, 0), w, (300,), None, out8, scale,
+                                                  x.dtype, (5, 300), (3, 5)))
+    assert (got.x, got.x_stride, got.residual, got.residual_stride, got.z, got.w) == (x.data_ptr(), 300, r.data_ptr(), 320, None, w.data_ptr())
+    assert (got.out, got.out8, got.out8_stride, got.scale, got.scale_stride) == (None, out8.data_ptr(), 300, scale.data_ptr(), 8)
 
 
 def test_binding_norms(host):
