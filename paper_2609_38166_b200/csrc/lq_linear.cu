@@ -10,6 +10,25 @@ namespace lq {
 
 constexpr int SMS = 148;
 
+// A launch that may begin while the kernel in front of it on the stream is still draining; its kernel executes griddepcontrol.wait before its first access to
+// global memory.  cluster: CTAs of a cluster, 0: what the kernel says.
+template <typename K, typename... Args>
+static lq_status launch_dependent(K kernel, dim3 grid, dim3 block, size_t smem, cudaStream_t stream, int cluster, const Args &...args) {
+  cudaLaunchAttribute attrs[2] = {};
+  attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attrs[0].val.programmaticStreamSerializationAllowed = 1;
+  attrs[1].id = cudaLaunchAttributeClusterDimension;
+  attrs[1].val.clusterDim.x = cluster, attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t config = {};
+  config.gridDim = grid, config.blockDim = block, config.dynamicSmemBytes = smem, config.stream = stream;
+  config.attrs = attrs, config.numAttrs = cluster > 0 ? 2 : 1;
+  if (cudaLaunchKernelEx(&config, kernel, args...) != cudaSuccess) {
+    cudaGetLastError();
+    return LQ_ERR_CUDA;
+  }
+  return LQ_OK;
+}
+
 // ---- norms ----
 
 // The memory from the first to the last element of an array of strided rows.
@@ -78,18 +97,14 @@ static lq_status launch_add(const AddArgs &a, cudaStream_t stream) {
   const int threads = (int)ceil_div(ceil_div(pieces, v), 32) * 32, rows = std::max(1, 256 / threads);
   const dim3 block(threads, rows);
   const long grid = ceil_div(a.tokens, rows);
-  if (v == 1) norm_add_kernel<T, WIDE, 1><<<grid, block, 0, stream>>>(a);
-  else if (v == 2) norm_add_kernel<T, WIDE, 2><<<grid, block, 0, stream>>>(a);
-  else norm_add_kernel<T, WIDE, 4><<<grid, block, 0, stream>>>(a);
-  return launched();
+  const auto kernel = v == 1 ? norm_add_kernel<T, WIDE, 1> : v == 2 ? norm_add_kernel<T, WIDE, 2> : norm_add_kernel<T, WIDE, 4>;
+  return launch_dependent(kernel, dim3((unsigned)grid), block, 0, stream, 0, a);
 }
 
 template <typename X, typename T>
 static lq_status launch_gate(const GatedArgs &a, bool wide, cudaStream_t stream) {
   const long grid = ceil_div((long)a.tokens * a.warps, GATED_THREADS / 32);
-  if (wide) norm_gate_kernel<X, T, true><<<grid, GATED_THREADS, 0, stream>>>(a);
-  else norm_gate_kernel<X, T, false><<<grid, GATED_THREADS, 0, stream>>>(a);
-  return launched();
+  return launch_dependent(wide ? norm_gate_kernel<X, T, true> : norm_gate_kernel<X, T, false>, dim3((unsigned)grid), dim3(GATED_THREADS), 0, stream, 0, a);
 }
 template <typename X>
 static lq_status launch_gate(const GatedArgs &a, int type, bool wide, cudaStream_t stream) {
@@ -131,17 +146,7 @@ static lq_status launch_few_t(const ProductMaps &maps, const ProductArgs &a, int
   static std::atomic<uint64_t> ready{0};
   const lq_status rc = give_shared(product_few_kernel<T, WIDE, ROWS>, sizeof(FewShared<ROWS>), ready);
   if (rc != LQ_OK) return rc;
-  cudaLaunchAttribute cluster{};
-  cluster.id = cudaLaunchAttributeClusterDimension;
-  cluster.val.clusterDim.x = a.split, cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
-  cudaLaunchConfig_t config{};
-  config.gridDim = dim3(grid), config.blockDim = dim3(FEW_THREADS), config.dynamicSmemBytes = sizeof(FewShared<ROWS>), config.stream = stream;
-  config.attrs = &cluster, config.numAttrs = 1;
-  if (cudaLaunchKernelEx(&config, product_few_kernel<T, WIDE, ROWS>, maps, a) != cudaSuccess) {
-    cudaGetLastError();
-    return LQ_ERR_CUDA;
-  }
-  return LQ_OK;
+  return launch_dependent(product_few_kernel<T, WIDE, ROWS>, dim3(grid), dim3(FEW_THREADS), sizeof(FewShared<ROWS>), stream, a.split, maps, a);
 }
 // Which kernel: the one whose tiles take fewer rounds over the GPU, as a round of either takes the same time (32 K blocks: 16 - 19 us; 148 tiles of 128 x 128,
 // or 74 pairs of CTAs on 256 x 256), the one for few rows where they tie.  1024 rows x 4096 x 4096: 2 rounds 32.6 us, 1 round 19.3; 192 x 4096 x 12352: 2 rounds
@@ -184,8 +189,7 @@ static lq_status launch_many_t(const ProductMaps &maps, const ProductArgs &a, lo
   static std::atomic<uint64_t> ready{0};
   const lq_status rc = give_shared(product_many_kernel<T, WIDE>, sizeof(ManyShared), ready);
   if (rc != LQ_OK) return rc;
-  product_many_kernel<T, WIDE><<<2 * (int)std::min<long>(pairs, SMS / 2), MANY_THREADS, sizeof(ManyShared), stream>>>(maps, a);
-  return launched();
+  return launch_dependent(product_many_kernel<T, WIDE>, dim3(2 * (unsigned)std::min<long>(pairs, SMS / 2)), dim3(MANY_THREADS), sizeof(ManyShared), stream, 0, maps, a);
 }
 static lq_status launch_many(const lq_linear *s, ProductArgs a, const void *x, int64_t x_stride, const void *w, cudaStream_t stream) {
   a.tiles_n = (int)ceil_div(s->out, MANY_OUTS);

@@ -5,7 +5,9 @@
 // to 4096 channels: off by 0.64 of 2^-23 of the sum over magnitudes at most).  The outer sum is taken in registers: every K block is read out of tensor memory and added with one
 // multiply-add an element, its factor xs ws.  So unlike a product without scales each K block is handed over twice, and that is what bounds the
 // large ones: see the kernel for many rows.  Nothing is kept between calls and there is no workspace.
+// Both kernels are programmatic dependents and let theirs come up at once, where room appears: one row of 4096 x 4096 8.0 -> 7.3 us, 64 rows 10.9 -> 9.8.
 #pragma once
+#include "lq_dependent.cuh"
 #include "lq_rows.cuh"
 #include "lq_tensor.cuh"
 
@@ -216,6 +218,7 @@ __global__ void __launch_bounds__(FEW_THREADS, ROWS == FEW_ROWS ? 1 : 2) product
     else if (lane == 31) bar_init(shared_addr(&sm.drained), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     __syncwarp();
+    grid_dependency_wait();
     // The first copies are on their way before anything else is set up (groups: before that it is not known which).
     if (lane == 0 && early > 0) {
       tile.find(a, sm.tiles, first, ROWS);
@@ -226,6 +229,8 @@ __global__ void __launch_bounds__(FEW_THREADS, ROWS == FEW_ROWS ? 1 : 2) product
   } else if (threadIdx.x == 64) {
     tensor_map_prefetch(ROWS > FEW_BOX && a.rows > 2 * FEW_BOX ? &maps.x : &maps.more);
   }
+  grid_dependency_wait();                      // (nothing in front of here looks at what another kernel may be writing)
+  grid_dependents_may_start();
   tmem_fence_before();
   sm.tiles.find(a, ROWS);
   tmem_fence_after();
@@ -477,6 +482,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1) pro
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) pair_tmem_alloc(shared_addr(&sm.tmem), 512);
+  grid_dependency_wait();
+  grid_dependents_may_start();
   tmem_fence_before();
   sm.tiles.find(a, MANY_ROWS);
   cluster_sync();

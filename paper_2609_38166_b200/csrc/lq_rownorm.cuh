@@ -3,6 +3,7 @@
 // Every element is read and written once and a row (a head) stays in registers between its sum of squares and its outputs: bound by memory.  A thread
 // has pieces of eight (heads: sixteen) consecutive channels, so that neighbouring lanes have a block of 128 and its largest value is a butterfly over them.
 #pragma once
+#include "lq_dependent.cuh"
 #include "lq_rows.cuh"
 
 namespace lq {
@@ -137,6 +138,7 @@ struct AddArgs {
 template <typename T, bool WIDE, int V>
 __global__ void __launch_bounds__(512) norm_add_kernel(const AddArgs a) {
   __shared__ float part[16];
+  grid_dependency_wait();
   const int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
   const bool there = row < a.tokens;
   const T *x = static_cast<const T *>(a.x) + row * a.x_stride;
@@ -232,6 +234,7 @@ __device__ __forceinline__ float gate_of(float z, int silu) {   // 1 / (1 + exp(
 template <typename X, typename T, bool WIDE>
 __global__ void __launch_bounds__(GATED_THREADS, 10) norm_gate_kernel(const GatedArgs a) {
   constexpr int N = GATED_LINE;
+  grid_dependency_wait();
   const int lane = threadIdx.x % 32;
   const uint32_t unit = blockIdx.x * (GATED_THREADS / 32) + threadIdx.x / 32, row = a.by_warps.quotient(unit);
   if (row >= (uint32_t)a.tokens) return;

@@ -179,3 +179,28 @@ def test_slices_side_by_side_in_one_buffer():
     lq.norm_add(add, x, out8=h8, scale=scale)
     lq.product(sh, h8, scale, w, ws, out)
     assert torch.equal(own8.view(torch.uint8), h8.view(torch.uint8)) and torch.equal(own_scale, scale) and torch.equal(own, out)
+
+
+@pytest.mark.parametrize("rows", [1, 30, 300, 5000])
+def test_calls_right_behind_one_another(rows):
+    """Every call takes what the one in front of it has just written, into the same arrays over and over: as with a wait between all of them."""
+    g = torch.Generator().manual_seed(rows)
+    x0 = torch.randn((rows, HIDDEN), generator=g).bfloat16().cuda()
+    w, ws = weight(g, HIDDEN, HIDDEN)
+
+    def chain(wait):
+        x, r = x0.clone(), torch.zeros_like(x0)
+        h8, hs = torch.empty((rows, HIDDEN), dtype=ref.E4M3, device="cuda"), torch.empty((HIDDEN // 128, rows), device="cuda")
+        add, sh = lq.AddShape(rows, HIDDEN), lq.ProductShape(rows, HIDDEN, HIDDEN)
+        for _ in range(30):
+            for call in (lambda: lq.norm_add(add, x, residual=r, out8=h8, scale=hs), lambda: lq.product(sh, h8, hs, w, ws, x)):
+                call()
+                if wait:
+                    torch.cuda.synchronize()
+        return x, r
+
+    slow = chain(True)
+    for _ in range(3):
+        for a, b in zip(slow, chain(False)):
+            assert torch.equal(a, b)
+    assert torch.isfinite(slow[0].float()).all() and lq.check_device() == 0
