@@ -70,7 +70,7 @@ struct GroupTiles {
   int first[MOST_GROUPS + 1];                  // tiles of rows in front of a group
   int start[MOST_GROUPS + 1];
 
-  // all threads of the CTA; `rows_per_tile` of T
+  // all threads of the CTA; T: rows of a tile
   __device__ __forceinline__ void find(const ProductArgs &a, int T) {
     if (a.group_start) {
       for (int g = threadIdx.x; g <= a.groups; g += blockDim.x) start[g] = min(max(a.group_start[g], 0), a.rows);
@@ -237,6 +237,7 @@ __global__ void __launch_bounds__(FEW_THREADS, ROWS == FEW_ROWS ? 1 : 2) product
   const uint32_t tmem = sm.tmem;
   // The sums of a split tile are handed over in the place of the outputs where they fit, else in that of the weights, when nobody uses them any more.
   const bool small = (a.rows < ROWS ? a.rows : ROWS) + a.split <= (int)sizeof(sm.out) / (PB * 4);
+  __syncwarp();
   if (a.split > 1 && small) cluster_arrive();
   if (warp == 0 || warp == 3) {                // ---- tensor copies: the weights' and the rows', a thread each (a copy takes 200 clocks to issue) ----
     if (lane == 0) {
@@ -413,7 +414,7 @@ __global__ void __launch_bounds__(FEW_THREADS, ROWS == FEW_ROWS ? 1 : 2) product
 // 256 output channels: either has 128 rows of x and of the weights in its shared memory and 128 rows of the sums in its tensor memory, which halves what a tile
 // takes from L2 (64 KB a K block; at 13 TB/s that alone is 0.36 us, the products 0.28 us).  Two accumulators: one is taken over while the next K block's
 // product goes to the other.
-//   warp 0       tensor copies of this CTA's half of either operand, four to five K blocks ahead
+//   warp 0       tensor copies of this CTA's half of either operand, up to five K blocks ahead
 //   warp 1       one thread of the first CTA issues the products of both
 //   warps 2, 3   factors, to shared memory; they arrive on the barrier of the sums, so that there is one wait for both
 //   warps 4-11   a row and half of the output channels to a thread: sums in 128 registers; outputs by way of shared memory and tensor copies
@@ -486,6 +487,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1) pro
   grid_dependents_may_start();
   tmem_fence_before();
   sm.tiles.find(a, MANY_ROWS);
+  __syncwarp();
   cluster_sync();
   tmem_fence_after();
   const uint32_t tmem = sm.tmem;
