@@ -204,3 +204,35 @@ def test_calls_right_behind_one_another(rows):
         for a, b in zip(slow, chain(False)):
             assert torch.equal(a, b)
     assert torch.isfinite(slow[0].float()).all() and lq.check_device() == 0
+
+
+def test_rows_beyond_two_to_the_31_elements():
+    """70000 rows, 32768 elements apart: the same bits as of rows side by side."""
+    rows, far, cin, cout = 70000, 32768, 128, 48
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn((rows, cin), generator=g, device="cuda").bfloat16()
+    w, ws = weight(torch.Generator().manual_seed(2), cout, cin)
+    add, gated, sh = lq.AddShape(rows, cin), lq.GatedShape(rows, 1, o_type=lq.BF16), lq.ProductShape(rows, cin, cout)
+
+    def chain(of, of8):
+        o, z, y, y8 = of(cin), of(cin), of(cout), of8(cin)
+        scale = torch.empty((1, rows), device="cuda")
+        lq.norm_add(add, x, out=o)
+        z.copy_(x.flip(0))
+        lq.norm_gate(gated, o[:, None], z[:, None], out8=y8, scale=scale)
+        lq.product(sh, y8, scale, w, ws, y)
+        lq.norm_add(add, o, out=o)
+        return [t.contiguous().view(torch.uint8) for t in (o, y, y8)]
+
+    here = chain(lambda n: torch.empty((rows, n), dtype=torch.bfloat16, device="cuda"), lambda n: torch.empty((rows, n), dtype=ref.E4M3, device="cuda"))
+    buf, buf8 = torch.empty((rows, far), dtype=torch.bfloat16, device="cuda"), torch.empty((rows, far), dtype=torch.uint8, device="cuda")
+    at = iter((0, 512, 1024))
+
+    def apart(n):
+        k = next(at)
+        return buf[:, k:k + n]
+
+    there = chain(apart, lambda n: buf8[:, 256:256 + n].view(ref.E4M3))
+    for a, b in zip(here, there):
+        assert torch.equal(a, b)
+    assert lq.check_device() == 0
