@@ -249,8 +249,11 @@ __global__ void __launch_bounds__(FEW_THREADS, ROWS == FEW_ROWS ? 1 : 2) product
           if (warp == 0) copy_w(s, b);
           else copy_x(s, b);
         }
-      if (!ok) {                               // the copies on their way, before their shared memory is gone
+      // Before their shared memory is gone: the copies on their way, or the products' arrivals that no copy waits for any more.
+      if (!ok) {
         for (int i = max(c - S::STAGES, 0); i < c; i++) reached(shared_addr(&sm.full[i % S::STAGES]), (i / S::STAGES) & 1);
+      } else if (warp == 0) {
+        for (int i = max(c - S::STAGES, 0); ok && i < c; i++) ok = reached(shared_addr(&sm.empty[i % S::STAGES]), (i / S::STAGES) & 1);
       }
     }
   } else if (warp == 1) {                      // ---- products: one thread ----
@@ -507,7 +510,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MANY_THREADS, 1) pro
             pair_tensor_g2s(shared_addr(sm.x[s]), &maps.x, b * PB, tile.row + 128 * rank, 0, bar);
             pair_tensor_g2s(shared_addr(sm.w[s]), &maps.w, b * PB, tile.n * MANY_OUTS + 128 * rank, tile.group, bar);
           }
-        if (!ok && rank == 0) {                // the copies on their way, before their shared memory is gone
+        // Before their shared memory is gone: the copies on their way, or the products' arrivals (in either CTA) that no copy waits for any more.
+        if (ok) {
+          for (int i = max(c - S::STAGES, 0); ok && i < c; i++) ok = reached(shared_addr(&sm.empty[i % S::STAGES]), (i / S::STAGES) & 1);
+        } else if (rank == 0) {
           for (int i = max(c - S::STAGES, 0); i < c; i++) reached(shared_addr(&sm.full[i % S::STAGES]), (i / S::STAGES) & 1);
         }
       }
