@@ -368,7 +368,7 @@ __device__ __forceinline__ bool take(ScanShared &sm, ScanItem &it, int &t, int l
 template <bool OUT>
 __device__ __forceinline__ void scan_copies(ScanShared &sm, const ScanMaps &maps, const ScanArgs &a, const ScanPlan &plan) {
   ScanItem it;
-  int c = 0, asked[3] = {0, 0, 0};             // blocks; tiles of K, Q, V that have been asked for
+  int c = 0, ns = 0, asked[3] = {0, 0, 0};     // blocks; states that they are given; tiles of K, Q, V that have been asked for
   bool ok = true;
   if (a.sq.tokens > 0) {                       // (without rows there are no maps)
     tensor_map_prefetch(&maps.k);
@@ -402,9 +402,19 @@ __device__ __forceinline__ void scan_copies(ScanShared &sm, const ScanMaps &maps
       if (OUT && !copy(&maps.q, sm.q, hq, row, sm.q_full, sm.q_empty, asked[1])) break;   // (Q is through first)
       if (!copy(&maps.k, sm.k, hq, row, sm.k_full, sm.k_empty, asked[0])) break;
       if (!copy(&maps.v, sm.v, it.h, row, sm.v_full, sm.v_empty, asked[2])) break;
+      ns += OUT && (it.state() || row > it.row);
     }
   }
-  if (!ok) {                                   // the copies that nobody waited for: the last two of each kind
+  if (ok && c > 0) {                           // the products' arrivals that nobody waits for any more, before their barriers are gone: in the order in which they come
+    for (int i = max(c - 2, 0); ok && i < c; i++) {
+      const int r = i & 1, parity = (i >> 1) & 1;
+      ok = (!OUT || wait_one(sm.q_empty[r], parity)) && wait_one(sm.k_empty[r], parity);
+      // (behind those: of the phase before have all been waited for, or the last block's products would not have been issued)
+      if (i == c - 1) ok = ok && (ns == 0 || wait_one(sm.s_empty, (ns + 1) & 1)) && wait_one(sm.w_empty[0], 1) && wait_one(sm.w_empty[1], 1);
+      ok = ok && wait_one(sm.v_empty[r], parity);
+    }
+    if (!ok) atomicOr(&g_ops_error, 1);
+  } else if (!ok) {                            // the copies that nobody waited for: the last two of each kind
     atomicOr(&g_ops_error, 1);
     auto landed = [](uint64_t (&full)[2], int n) {
       for (int i = max(n - 2, 0); i < n; i++)
