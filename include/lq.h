@@ -459,6 +459,7 @@ lq_status lq_scan_step(const lq_scan *shape, const lq_scan_io *io, float *o, int
  *   x, out, residual : [tokens][dim] of `type`, strided rows; residual null: h = x.  out may be x (same pointer and stride)
  *   out8             : e4m3 [tokens][dim], strided rows, with `scale`.  Either out or out8 may be null
  *   w                : fp32 [dim] or null (1; LQ_NORM_RMS only)
+ * Apart from that no output (residual is one) may overlap an input or another output.
  * dim at most LQ_NORM_ADD_MOST.  With LQ_NORM_NONE and no residual it turns rows of any origin into 8-bit ones.
  */
 #define LQ_NORM_ADD_MOST 16384
@@ -492,7 +493,7 @@ lq_status lq_norm_add(const lq_add *shape, const lq_norm_io *io, lq_stream strea
  * in binary32 (f: within 2^-21 + 2^-23 |z| of itself, relative, and 0 where it is below 2^-119), outputs as in lq_norm_add with rows of heads * dim channels.
  *   o : [tokens][heads][dim] of `o_type` - binary32 from lq_decode_step and lq_scan_step, bf16 from lq_scan_prompt; strided rows
  *   z : [tokens][heads][dim] of `type`, strided rows      w : fp32 [dim] or null (1; LQ_NORM_RMS only)
- * No output may overlap an input.
+ * No output may overlap an input or another output.
  */
 typedef struct {
   int tokens, heads;
@@ -516,7 +517,7 @@ lq_status lq_norm_gate(const lq_gated *shape, const lq_norm_io *io, lq_stream st
  * lq_product_groups: the rows of group g, group_start[g] to group_start[g+1] - 1 (int32 [groups + 1] in device memory, not decreasing), take
  * weight g: w [groups][out][in], w_scale [groups][ceil(out/128)][ceil(in/128)].  Groups may be empty; rows in front of group_start[0] and from
  * group_start[groups] on belong to nobody: they are not written, and what they hold does not matter.  At most LQ_MOST_GROUPS groups.
- * out must not overlap an input.  The order of all sums depends on the shapes and on group_start alone: the same call gives the same bits again.
+ * out must not overlap an input, group_start among them.  The order of all sums depends on the shapes and on group_start alone: the same call gives the same bits again.
  */
 #define LQ_MOST_GROUPS 1024
 typedef struct {

@@ -50,6 +50,7 @@ struct NormIo {
   unsigned in_size[2];
   bool written;                                // the second input is an output too
   const float *w;
+  long weights;                                // elements of w that are read
   NormOut o;
 };
 
@@ -70,12 +71,14 @@ static lq_status check_norm_io(const NormIo &io, long tokens, long width, int ty
   const Span out[3] = {{io.o.out, io.o.out_stride, width, tokens, size},
                        {io.o.out8, io.o.out8_stride, width, tokens, 1},
                        {io.o.out8 ? io.o.scale : nullptr, io.o.scale_stride, tokens, ceil_div(width, 128), 4}};
-  if (io.written && spans_meet(in[0], in[1])) return LQ_ERR_UNSUPPORTED;
+  const Span w{io.weights ? io.w : nullptr, io.weights, io.weights, 1, 4};
+  if (io.written && (spans_meet(in[0], in[1]) || spans_meet(w, in[1]))) return LQ_ERR_UNSUPPORTED;
   for (int i = 0; i < 3; i++) {
     for (int j = 0; j < 2; j++)
       if (!(in_place && i == 0 && j == 0 && out[0].p == in[0].p && out[0].stride == in[0].stride) && spans_meet(out[i], in[j])) return LQ_ERR_UNSUPPORTED;
     for (int j = 0; j < i; j++)
       if (spans_meet(out[i], out[j])) return LQ_ERR_UNSUPPORTED;
+    if (spans_meet(w, out[i])) return LQ_ERR_UNSUPPORTED;
   }
   return LQ_OK;
 }
@@ -233,7 +236,8 @@ static lq_status product(const lq_linear *s, const lq_product_io *io, bool group
   const int blocks = (int)ceil_div(s->in, PB);
   const Span o{out, out_stride, s->out, s->rows, size};
   for (const Span &in : {Span{x, x_stride, s->in, s->rows, 1}, Span{x_scale, x_scale_stride, s->rows, blocks, 4},
-                         Span{w, s->in, s->in, (long)s->out * s->groups, 1}, Span{w_scale, blocks, blocks, ceil_div(s->out, PB) * s->groups, 4}})
+                         Span{w, s->in, s->in, (long)s->out * s->groups, 1}, Span{w_scale, blocks, blocks, ceil_div(s->out, PB) * s->groups, 4},
+                         Span{group_start, s->groups + 1, s->groups + 1, 1, 4}})
     if (spans_meet(o, in)) return LQ_ERR_UNSUPPORTED;
   ProductArgs a{x_scale, w_scale, out, x_scale_stride, out_stride, group_start, s->rows, blocks, s->out, s->groups, s->type, 0, 1, blocks, 0, {}};
   if (s->rows <= FEW_BOX * (grouped ? s->groups : 1)) {
@@ -264,7 +268,7 @@ lq_status lq_norm_add(const lq_add *s, const lq_norm_io *n, lq_stream stream) {
   if (s->dim > LQ_NORM_ADD_MOST || s->tokens > MOST_ROWS) return LQ_ERR_UNSUPPORTED;
   if (s->tokens == 0) return LQ_OK;
   const unsigned size = type_size(s->type);
-  const NormIo io{{n->x, n->residual}, {n->x_stride, n->residual_stride}, {size, size}, true, n->w, norm_out(n)};
+  const NormIo io{{n->x, n->residual}, {n->x_stride, n->residual_stride}, {size, size}, true, n->w, s->norm == LQ_NORM_RMS ? s->dim : 0, norm_out(n)};
   const lq_status rc = check_norm_io(io, s->tokens, s->dim, s->type, true);
   if (rc != LQ_OK) return rc;
   const AddArgs a{n->x, n->residual, n->w, n->x_stride, n->residual_stride, io.o, s->tokens, s->dim, s->norm, s->eps, s->norm == LQ_NORM_RMS ? 1.0f / s->dim : 1.0f};
@@ -283,7 +287,7 @@ lq_status lq_norm_gate(const lq_gated *s, const lq_norm_io *n, lq_stream stream)
   if (s->tokens == 0) return LQ_OK;
   if (!n->z) return LQ_ERR_NULL;
   const long width = (long)s->heads * s->dim;
-  const NormIo io{{n->x, n->z}, {n->x_stride, n->z_stride}, {type_size(s->o_type), type_size(s->type)}, false, n->w, norm_out(n)};
+  const NormIo io{{n->x, n->z}, {n->x_stride, n->z_stride}, {type_size(s->o_type), type_size(s->type)}, false, n->w, s->norm == LQ_NORM_RMS ? s->dim : 0, norm_out(n)};
   const lq_status rc = check_norm_io(io, s->tokens, width, s->type, false);
   if (rc != LQ_OK) return rc;
   GatedArgs a{n->x, n->z, n->w, n->x_stride, n->z_stride, io.o, s->tokens, s->heads, s->dim, s->norm, s->silu, s->eps, s->norm == LQ_NORM_RMS ? 1.0f / s->dim : 1.0f, (int)warps, {}};
