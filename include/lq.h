@@ -448,6 +448,8 @@ lq_status lq_scan_step(const lq_scan *shape, const lq_scan_io *io, float *o, int
  *
  * A row of e4m3 codes has a scale for every block of 128 consecutive channels (the last block of a row may be shorter):
  *     value = code * scale,     scale = max(max_block |y|, 448 * 2^-100) / 448,     code = y / scale rounded to e4m3 (nearest even)
+ * in binary32: the scale is within 2^-23 of that (relative), and what is rounded to e4m3 within 2^-22 of y / scale, so that a value as close as that to
+ * the middle between two codes may get either; beyond 448 it is 448.
  * Arrays need the alignment of their elements only, except for x and w of the products.
  * scale lies block by block: fp32 [ceil(channels/128)][scale_stride], the scales of neighbouring rows side by side, scale_stride at least
  * the number of rows.  A block with an infinity stands for NaN throughout, a NaN for itself alone.  Codes are the 8-bit patterns of e4m3
