@@ -492,7 +492,8 @@ lq_status lq_norm_add(const lq_add *shape, const lq_norm_io *io, lq_stream strea
 /*
  * lq_norm_gate: the outputs of the recurrence normalised per head, weighted and gated:
  *     y = norm(o) * w * f(z),     f(z) = z / (1 + exp(-z)) (silu) or 1 / (1 + exp(-z))
- * in binary32 (f: within 2^-21 + 2^-23 |z| of itself, relative, and 0 where it is below 2^-119), outputs as in lq_norm_add with rows of heads * dim channels.
+ * in binary32 (f: within 2^-21 + 2^-23 |z| of itself, relative, with LQ_F32 for `type` within 2^-21, and 0 where it is below 2^-119), outputs as in
+ * lq_norm_add with rows of heads * dim channels.
  *   o : [tokens][heads][dim] of `o_type` - binary32 from lq_decode_step and lq_scan_step, bf16 from lq_scan_prompt; strided rows
  *   z : [tokens][heads][dim] of `type`, strided rows      w : fp32 [dim] or null (1; LQ_NORM_RMS only)
  * No output may overlap an input or another output.

@@ -221,18 +221,23 @@ struct GatedArgs {
 
 constexpr int GATED_THREADS = 128, GATED_LINE = 16;   // channels of a lane
 
-__device__ __forceinline__ float gate_of(float z, int silu) {   // 1 / (1 + exp(-z)), times z; a quotient that overflows is a 0
+// 1 / (1 + exp(-z)), times z; a quotient that overflows is a 0.  In front of 8 and 16 bits the exponential is an approximation whose argument is rounded, 2^-21 +
+// 2^-23 |z| off with the rest; where z and out are binary32 it is within 2^-22, and the whole within 2^-21 whatever z is.
+template <typename T>
+__device__ __forceinline__ float gate_of(float z, int silu) {
   float e;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.44269504088896340736f));
+  if constexpr (std::is_same_v<T, float>) e = expf(-z);
+  else asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.44269504088896340736f));
   const float r = reciprocal_of(1.0f + e);
   return silu ? z * r : r;
 }
 
 // A warp has 512 channels of a row.  Sixteen channels to a lane, for what a lane does for all of them together (sums over lanes, scale, addresses) is as much
-// as what it does for eight: 16384 rows x 32 heads x 128 channels of bf16 to 8 bits 80 -> 65 us; ten CTAs to an SM 62.6, 5.4 TB/s, of binary32 79, 5.9 TB/s.  What is
+// as what it does for eight: 16384 rows x 32 heads x 128 channels of bf16 to 8 bits 80 -> 65 us; ten CTAs to an SM 62.6, 5.4 TB/s, of binary32 79, 5.9 TB/s (z and out of
+// binary32, nine to an SM, for the registers of the other exponential: 137 us, 5.9 TB/s; ten 153).  What is
 // left are two MUFU operations an element (30 us) next to the memory; four rows to a warp, or eight channels and four rows, take longer.
 template <typename X, typename T, bool WIDE>
-__global__ void __launch_bounds__(GATED_THREADS, 10) norm_gate_kernel(const GatedArgs a) {
+__global__ void __launch_bounds__(GATED_THREADS, sizeof(T) == 4 ? 9 : 10) norm_gate_kernel(const GatedArgs a) {
   constexpr int N = GATED_LINE;
   grid_dependency_wait();
   const int lane = threadIdx.x % 32;
@@ -261,7 +266,7 @@ __global__ void __launch_bounds__(GATED_THREADS, 10) norm_gate_kernel(const Gate
   }
   unpack(zs, z);
 #pragma unroll
-  for (int e = 0; e < N; e++) x[e] *= factor * gate_of(z[e], a.silu);
+  for (int e = 0; e < N; e++) x[e] *= factor * gate_of<T>(z[e], a.silu);
   norm_store<WIDE, T>(a.o, row, c, n, x);
 }
 
