@@ -512,7 +512,8 @@ lq_status lq_norm_gate(const lq_gated *shape, const lq_norm_io *io, lq_stream st
 /*
  * lq_product: rows of e4m3 codes times e4m3 weights, whose scales are of blocks of 128 output by 128 input channels:
  *     out[t][n] = sum_b x_scale[b][t] w_scale[n/128][b] sum_{k in block b} x[t][k] w[n][k]
- * The sum over a block is the tensor cores' (binary32 accumulator), the sum over blocks binary32; rounded once to `type`.
+ * The sum over a block is the tensor cores' (binary32 accumulator; off by 37 * 2^-23 of the sum over magnitudes at most, by one where the products are of
+ * one size), the sum over blocks binary32; rounded once to `type`.
  *   x   : e4m3 [rows][in], strided rows, 16-byte aligned, stride a multiple of 16      x_scale : fp32 [ceil(in/128)][x_scale_stride]
  *   w   : e4m3 [out][in], dense, 16-byte aligned                                       w_scale : fp32 [ceil(out/128)][ceil(in/128)]
  *   out : [rows][out] of `type`, strided rows

@@ -187,3 +187,26 @@ def test_what_is_not_finite_stays_in_its_row(kernel, rows, cin, cout, starts):
     same = torch.ones(rows, dtype=torch.bool, device="cuda")
     same[bad] = False
     assert torch.equal(call.out[same], clean[same])
+
+
+@pytest.mark.parametrize("codes,steps", [("of one size", 1), ("of every size", 37), ("one and the rest", 37)])
+@pytest.mark.parametrize("kernel,rows,cout", [(MANY, 16384, 2048), (FEW, 40, 2048)])
+def test_sums_of_a_block(kernel, rows, cout, codes, steps):
+    """One K block and factors of 1: outputs are the accumulators.  An instruction adds 32 products to the sum so far; terms are cut off 2^-25 below the largest of
+    them, 33 * 2^-25 of it in all, and the sum at 2^-23 of itself: 9.25 * 2^-23 of the sum over magnitudes, four times 37.  Where they are of one size, next to nothing
+    is cut off: a step in all."""
+    call = Call(rows, 128, cout, torch.float32, True)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    if codes != "of one size":
+        for t in (call.x, call.w):
+            any_ = torch.randint(0, 256, t.shape, generator=g, device="cuda", dtype=torch.uint8)
+            any_[any_ % 128 == 127] = 0                                           # (NaN)
+            t.view(torch.uint8).copy_(any_)
+    if codes == "one and the rest":                                               # 127 of the smallest
+        call.x.view(torch.uint8).copy_(1 + 128 * (torch.arange(128, device="cuda") % 3 == 0).to(torch.uint8))
+        call.x.view(torch.uint8)[:, 77] = 0x7E
+    call.s.fill_(1.0), call.ws.fill_(1.0)
+    assert launched(call)[0] == kernel
+    call()
+    want, size = definition(call.x, call.s, call.w, call.ws, [0, rows])
+    assert ((call.out.double() - want).abs() <= steps * 2.0 ** -23 * size).all()
