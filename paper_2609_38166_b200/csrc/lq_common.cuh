@@ -186,12 +186,6 @@ __device__ __forceinline__ float dot128_shared(const float *a, const float *b, i
   return tree16(block8(a2, b2));
 }
 
-// When the dependents may start: allowed at the very beginning, their CTAs come up one by one wherever room appears, so that
-// the few with work to do share an SM and the decode CTAs fill the gaps that boundary CTAs of another size leave.  With little
-// work (fewer boundaries than boundary CTAs, Params.overlap == 0) they start when the kernel ahead has ended, evenly over the
-// SMs: step at 32 x 32 heads 24.5 -> 19.0 us, 77 x 12 heads (W = 13) 22.0 -> 17.6 us.  With more, when every CTA has come to
-// its last head, which hides their start: 256 x 32 heads 64.7 us at the beginning or the end, 63.9 us at the last head.
-
 // Phase timing (development aid, compiled in with -DLQ_TIMING only): clock cycles per phase of the decode
 // warps, summed over all heads by lane 0 of each warp (slots 0..15: stream warp, 16..31: dot warp; 32..: thread 0 of the boundary kernel's CTAs).
 #ifdef LQ_TIMING

@@ -239,7 +239,7 @@ static lq_status product(const lq_linear *s, const lq_product_io *io, bool group
                          Span{w, s->in, s->in, (long)s->out * s->groups, 1}, Span{w_scale, blocks, blocks, ceil_div(s->out, PB) * s->groups, 4},
                          Span{group_start, s->groups + 1, s->groups + 1, 1, 4}})
     if (spans_meet(o, in)) return LQ_ERR_UNSUPPORTED;
-  ProductArgs a{x_scale, w_scale, out, x_scale_stride, out_stride, group_start, s->rows, blocks, s->out, s->groups, s->type, 0, 1, blocks, 0, {}};
+  ProductArgs a{x_scale, w_scale, out, x_scale_stride, out_stride, group_start, s->rows, blocks, s->out, s->groups, 0, 1, blocks, 0, {}};
   if (s->rows <= FEW_BOX * (grouped ? s->groups : 1)) {
     a.split = split_of(s, grouped, FEW_BOX);
     return launch_few<FEW_BOX>(s, a, x, x_stride, w, cuda_stream(stream));

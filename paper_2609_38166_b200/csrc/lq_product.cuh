@@ -58,7 +58,7 @@ struct ProductArgs {
   void *out;
   int64_t x_scale_stride, out_stride;
   const int32_t *group_start;                  // null: one group of all rows
-  int rows, blocks, outs, groups, type;        // blocks: K blocks; outs: output channels
+  int rows, blocks, outs, groups;              // blocks: K blocks; outs: output channels
   int tiles_n;                                 // tiles of output channels
   int split, share, more;                      // few rows: CTAs of a cluster that share a tile's K blocks, `share` each and one more to the first `more`
   Divisor tiles_m;                             // without groups: division by the tiles of rows
