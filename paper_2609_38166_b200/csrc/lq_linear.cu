@@ -93,8 +93,7 @@ static bool wide_norm(const NormIo &io, long width, int type, int line) {
 
 template <typename T, bool WIDE>
 static lq_status launch_add(const AddArgs &a, cudaStream_t stream) {
-  // two pieces to a thread, one where there are fewer rows than SMs (4096 channels, 1 row: 3.3 -> 2.9 us; 16384 rows
-  // with one, two, four pieces: 105, 84, 126 us)
+  // two pieces to a thread, one where there are fewer rows than SMs (4096 channels, one row with one, two, four pieces: 2.2, 2.5, 3.2 us; 16384 rows: 99, 73, 75 us)
   const long pieces = ceil_div(a.dim, LINE);
   const int v = pieces > 1024 ? 4 : pieces > 512 || a.tokens > SMS ? 2 : 1;
   const int threads = (int)ceil_div(ceil_div(pieces, v), 32) * 32, rows = std::max(1, 256 / threads);
@@ -151,11 +150,12 @@ static lq_status launch_few_t(const ProductMaps &maps, const ProductArgs &a, int
   if (rc != LQ_OK) return rc;
   return launch_dependent(product_few_kernel<T, WIDE, ROWS>, dim3(grid), dim3(FEW_THREADS), sizeof(FewShared<ROWS>), stream, a.split, maps, a);
 }
-// Which kernel: the one whose tiles take fewer rounds over the GPU, as a round of either takes the same time (32 K blocks: 16 - 19 us; 148 tiles of 128 x 128,
-// or 74 pairs of CTAs on 256 x 256), the one for few rows where they tie.  1024 rows x 4096 x 4096: 2 rounds 32.6 us, 1 round 19.3; 192 x 4096 x 12352: 2 rounds
-// 31.9, 1 round 19.1; 512 x 8192 x 1024: a quarter of a round 15.7, 1 round 29.3; 779 x 1296 x 1999: 1 round 12.2 and 15.1.
-// How many rows a group has is known on the device only: half a tile of every group is taken to be empty.  64 groups x 2048 x 1536 of 64 rows each 50 and 59 us, of 128
-// rows 56 and 62, of 192 rows 92 and 64.
+// Which kernel: the one whose tiles take fewer rounds over the GPU, as a round of either takes the same time (32 K blocks: 14 - 18 us; 148 tiles of 128 x 128,
+// or 74 pairs of CTAs on 256 x 256), the one for few rows where they tie.  Few and many, us: 1024 rows x 4096 x 4096: 2 rounds 30.8, 1 round 17.7; 192 x 4096 x 12352: 2
+// rounds 30.2, 1 round 17.7; 512 x 8192 x 1024: a quarter of a round 14.2, 1 round 28.2; 779 x 1296 x 1999, 1 round each: 11.2 and 10.6.
+// How many rows a group has is known on the device only: half a tile of every group is taken to be empty.  64 groups x 2048 x 1536 of 64 rows each 47 and 54 us, of 128
+// rows 54 and 57 (which the rule gives away), of 192 rows 90 and 60.  What it costs where the rows lie unevenly: 4096 rows of 128 groups, on average 32 (tiles of 32 rows;
+// others at best), evenly 71 us (71), all in one group 41 (23); 8192 rows, on average 64 (tiles of 128 rows), evenly 84 (84), all in one 53 (31), half of them in one 67 (66).
 static bool are_few(const lq_linear *s, bool grouped, int split) {
   const long few = ceil_div(s->out, PB), many = ceil_div(s->out, MANY_OUTS);
   if (grouped) {
@@ -164,7 +164,9 @@ static bool are_few(const lq_linear *s, bool grouped, int split) {
   }
   return split > 1 || ceil_div(few * ceil_div(s->rows, FEW_ROWS), SMS) <= ceil_div(many * ceil_div(s->rows, MANY_ROWS), SMS / 2);
 }
-// Few rows: CTAs that share a tile's K blocks.  One row of 4096 x 4096 (32 tiles): 1, 2, 4 CTAs 20, 12, 7.8 us.
+// Few rows: CTAs that share a tile's K blocks.  One row of 4096 x 4096 (32 tiles), weights from memory: 1, 2, 4 CTAs 11.7, 8.6, 7.0 us.  As many as 148 places have room
+// for, also where two CTAs with tiles of 32 rows fit an SM: one row of 4096 x 8192 (64 tiles) with two 10.3, with four 9.4; 16 x 12352 x 4096 with four 13.6, eight 12.8;
+// but 4096 x 12352 (97 tiles) alone 13.4, with two 14.6, and 64 x 4096 x 4096 (tiles of 128 rows) with four 9.5, six 17.0.
 static int split_of(const lq_linear *s, bool grouped, int rows) {
   const long tiles = ceil_div(s->rows, rows) * ceil_div(s->out, PB), blocks = ceil_div(s->in, PB);
   return grouped ? 1 : (int)std::max(1l, std::min({SMS / tiles, 8l, blocks / 2}));
