@@ -457,7 +457,8 @@ lq_status lq_scan_step(const lq_scan *shape, const lq_scan_io *io, float *o, int
  *
  * lq_norm_add: the residual's addition and the norm of whole rows, in one pass:
  *     h = x + residual,  residual <- h,    y = norm(h) * w,     norm: LQ_NORM_NONE, LQ_NORM_L2 or LQ_NORM_RMS over `dim` channels
- * in binary32 (y from h before it is rounded); residual and out are rounded to `type` once, out8 and scale as above.
+ * in binary32 (y from h before it is rounded; a row whose sum of squares is beyond binary32 becomes 0); residual and out are rounded to `type` once, out8
+ * and scale as above.
  *   x, out, residual : [tokens][dim] of `type`, strided rows; residual null: h = x.  out may be x (same pointer and stride)
  *   out8             : e4m3 [tokens][dim], strided rows, with `scale`.  Either out or out8 may be null
  *   w                : fp32 [dim] or null (1; LQ_NORM_RMS only)

@@ -210,3 +210,29 @@ def test_sums_of_a_block(kernel, rows, cout, codes, steps):
     call()
     want, size = definition(call.x, call.s, call.w, call.ws, [0, rows])
     assert ((call.out.double() - want).abs() <= steps * 2.0 ** -23 * size).all()
+
+
+@pytest.mark.parametrize("share", range(2, 9))
+def test_clusters_of_every_size(share):
+    """A tile's K blocks shared by 2 to 8 CTAs, evenly and not."""
+    for cin in (256 * share, 256 * share + 16):
+        for rows in (5, 40, 128):
+            Call(rows, cin, 250, torch.bfloat16, True, seed=cin).check()
+
+
+def test_weights_beyond_two_to_the_32_bytes():
+    """600 groups of 8 MB: rows in the first, in one on either side of 2^32 bytes, and in the last."""
+    groups, cin, cout, rows = 600, 2048, 4096, 60
+    assert groups * cin * cout > 2 ** 32
+    x, s, w, ws = operands(rows, cin, cout, 4, 4)
+    big = torch.full((groups, cout, cin), 0x7F, dtype=torch.uint8, device="cuda").view(ref.E4M3)   # (NaN)
+    scales = torch.full((groups, cout // 128, cin // 128), float("nan"), device="cuda")
+    at = [0, 511, 512, 599]
+    for k, n in enumerate(at):
+        big[n], scales[n] = w[k], ws[k]
+    cuts = [0, 13, 20, 45, rows]
+    starts = [cuts[sum(n < m for n in at)] for m in range(groups + 1)]
+    out = torch.empty((rows, cout), dtype=torch.float32, device="cuda")
+    lq.product_groups(lq.ProductShape(rows, cin, cout, groups=groups, type=lq.F32), x, s, big, scales, out, torch.tensor(starts, dtype=torch.int32, device="cuda"))
+    want, size = definition(x, s, w, ws, cuts)
+    assert ref.off(out, want, torch.float32, (128 + cin // 128 + 2) * 2.0 ** -23 * size) <= 1 and lq.check_device() == 0
