@@ -8,7 +8,10 @@
 // definition's.  A copy's place holds NaN from when it is asked for until it has come, an accumulator from when its product is issued until it is through: who looks
 // too early, or overwrites what is still read, gets wrong numbers.  Nothing may arrive in the shared memory of a CTA that has left or has not begun.
 //
-// Usage: product_roles FIRST_SEED SEEDS
+// With `lose` one of the copies never comes: waits run out (a wait that nothing can end any more is told so, one after another), and the kernel has to end, say so and
+// leave nothing on its way behind.
+//
+// Usage: product_roles FIRST_SEED SEEDS [lose]
 #include <stdarg.h>
 #include <stdio.h>
 #include <stdlib.h>
@@ -30,6 +33,7 @@ using namespace lq;
 
 static std::mt19937 rng;
 static std::string what;                      // the run, for messages
+static int copies, lost = -1;                 // copies so far; the one that never comes
 
 [[noreturn]] static void fail(const char *f, ...) {
   va_list a;
@@ -63,6 +67,7 @@ struct Fiber {
   std::vector<char> stack;
   State state;
   uint32_t bar, parity;
+  bool in_vain;                               // the wait has run out
   unsigned cluster_turn;
   std::deque<std::shared_ptr<int>> groups;    // of copies out of shared memory: how many are not through
   int loose, but;                             // copies of no group yet; groups that a wait lets be
@@ -194,15 +199,16 @@ void bar_expect(uint32_t bar, uint32_t bytes) {
   bar_arrive(bar);
 }
 bool bar_try(uint32_t bar, uint32_t parity) {
-  now->bar = bar, now->parity = parity;
+  now->bar = bar, now->parity = parity, now->in_vain = false;
   block(AT_BAR);                              // (gets its turn while the barrier says that it is passed)
-  return true;
+  return !now->in_vain;
 }
 void tensor_g2s(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar) {
   const Map m = map_of(map);
   CHECK(x % 16 == 0 && dst % (8 * m.width) == 0, "a copy that is not aligned");
   yield();
   memset(shared_at(dst), 0xFF, m.rows * m.width);
+  if (copies++ == lost) return;
   loose.push_back([=] {
     uint8_t *to = shared_at(dst);
     for (int r = 0; r < m.rows; r++)
@@ -403,7 +409,24 @@ static void run_cluster(int number, int size, int grid, std::function<void()> ke
       if (!ctas[c].queue.empty()) may(ctas[c].queue_weight, 1000 + c);
     }
     if (!loose.empty()) may(loose_weight, 2000);
-    if (who.empty()) break;
+    if (who.empty()) {                        // (all lanes of a warp that wait for the same give up together, as those of a real one do)
+      if (lost < 0 || lost >= copies) break;
+      std::vector<int> waiting;
+      for (int c = 0; c < size; c++)
+        for (int w = 0; w < WARPS; w++)
+          for (int l = 0; l < 32; l++)
+            if (ctas[c].fibers[32 * w + l].state == AT_BAR) {
+              waiting.push_back(c * WARPS + w);
+              break;
+            }
+      if (waiting.empty()) break;
+      const int n = waiting[rng() % waiting.size()];
+      for (int l = 0; l < 32; l++) {
+        Fiber &f = ctas[n / WARPS].fibers[n % WARPS * 32 + l];
+        if (f.state == AT_BAR) f.in_vain = true, f.state = READY;
+      }
+      continue;
+    }
     const double x = std::uniform_real_distribution<double>(0, sum)(rng);
     size_t i = 0;
     while (i + 1 < who.size() && who[i].first < x) i++;
@@ -504,7 +527,8 @@ static void run_as(Kernel kernel, const char *type, bool wide) {
       else if (kernel == FEW_LARGE) wide ? product_few_kernel<T, true, FEW_ROWS>(maps, a) : product_few_kernel<T, false, FEW_ROWS>(maps, a);
       else wide ? product_few_kernel<T, true, FEW_BOX>(maps, a) : product_few_kernel<T, false, FEW_BOX>(maps, a);
     });
-  CHECK(g_product_error == 0, "flags %d", g_product_error);
+  const bool whole = lost < 0 || lost >= copies;
+  CHECK(g_product_error == (whole ? 0 : 1), "flags %d", g_product_error);
   std::vector<uint8_t> want(mem.size() * 16, 0xA5);
   T *const e = reinterpret_cast<T *>(want.data() + ((uint8_t *)o - (uint8_t *)mem.data()));
   for (int g = 0; g < groups; g++)
@@ -518,14 +542,19 @@ static void run_as(Kernel kernel, const char *type, bool wide) {
         }
         e[(int64_t)r * out_stride + n] = from_float<T>(s);
       }
+  if (!whole) {                               // (no output is valid; all of them lie where outputs belong)
+    for (int g = 0; g < groups; g++)
+      for (int r = grouped ? start[g] : 0; r < (grouped ? start[g + 1] : rows); r++) std::copy_n(&o[(int64_t)r * out_stride], out, &e[(int64_t)r * out_stride]);
+  }
   for (int64_t i = 0; i < (int64_t)(rows + 1) * out_stride; i++)
     CHECK(memcmp(&o[i], &e[i], sizeof(T)) == 0, "output %d of row %d is %g, not %g", (int)(i % out_stride), (int)(i / out_stride), to_float(o[i]), to_float(e[i]));
   CHECK(memcmp(mem.data(), want.data(), want.size()) == 0, "memory next to the outputs is written");
 }
 
-static void run(unsigned seed) {
+static void run(unsigned seed, bool lose) {
   rng.seed(seed);
   what = "seed " + std::to_string(seed) + ": ";
+  copies = 0, lost = lose ? rng() % 30 : -1;
   const Kernel kernel = (Kernel)(seed % 3);
   const bool wide = seed / 3 % 2;
   if (seed / 6 % 3 == 0) run_as<float>(kernel, "f32", wide);
@@ -535,8 +564,9 @@ static void run(unsigned seed) {
 
 int main(int argc, char **argv) {
   const unsigned first = argc > 1 ? atoi(argv[1]) : 0, n = argc > 2 ? atoi(argv[2]) : 18;
+  const bool lose = argc > 3 && argv[3] == std::string("lose");
   find_values();
-  for (unsigned s = first; s < first + n; s++) run(s);
+  for (unsigned s = first; s < first + n; s++) run(s, lose);
   printf("%u runs\n", n);
   return 0;
 }

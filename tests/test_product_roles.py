@@ -14,7 +14,8 @@ CUDA = os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "include")
 CHANGES = {
     "lq_dependent.cuh": [],
     "lq_rows.cuh": [(r'asm\("cvt\.rn\.(bf16|f16)x2\.f32 %0, %1, %2;" : "=r"\(two\) : "f"\((.*?)\), "f"\((.*?)\)\);', r"two = two_\1(\3, \2);", 2)],
-    "lq_product.cuh": [(r"extern __shared__ __align__\(1024\) uint8_t raw\[\];", "uint8_t *const raw = cta_memory();", 2),
+    "lq_product.cuh": [(r"PRODUCT_WAIT_LIMIT = 1 << 20;", "PRODUCT_WAIT_LIMIT = 3;", 1),
+                       (r"extern __shared__ __align__\(1024\) uint8_t raw\[\];", "uint8_t *const raw = cta_memory();", 2),
                        (r'asm volatile\("st\.shared::cluster\.f32.*?"memory"\);', "store_cluster(addr, x);", 1)],
 }
 
@@ -38,4 +39,10 @@ def roles(tmp_path_factory):
 @pytest.mark.parametrize("seed", range(0, 144, 18))
 def test_any_order(roles, seed):
     out = subprocess.run([roles, str(seed), "18"], capture_output=True, text=True, timeout=600)
+    assert out.returncode == 0, out.stdout
+
+
+@pytest.mark.parametrize("seed", range(0, 72, 18))
+def test_a_copy_that_never_comes(roles, seed):
+    out = subprocess.run([roles, str(seed), "18", "lose"], capture_output=True, text=True, timeout=600)
     assert out.returncode == 0, out.stdout
