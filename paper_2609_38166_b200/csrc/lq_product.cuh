@@ -142,7 +142,7 @@ struct ProductTile {
 // The weights are what such a call reads, so all that counts is that they are on their way: 96 KB to an SM, 128 KB with tiles of 32 rows (two CTAs).
 // Where there are fewer tiles than SMs, the CTAs of a cluster share a tile's K blocks and add up their sums by way of one another's shared memory, each for
 // some of the rows, in the order of the CTAs.  Four accumulators, so that no hand-over is waited for; a K block's factors arrive on the barrier of its sums.
-// Weights from memory (not L2): 128 groups of 0 - 100 rows x 2048 x 1536 68 us, 5.9 TB/s; one row of 4096 x 4096 8 us, of 4096 x 12352 14.5 us, 3.5 TB/s: 97 CTAs with 64 KB on
+// Weights from memory (not L2): 128 groups of 0 - 100 rows x 2048 x 1536 68 us, 5.9 TB/s; one row of 4096 x 4096 7.1 us, of 4096 x 12352 13.5 us, 3.8 TB/s: 97 CTAs with 64 KB on
 // their way each, and 4 us until the first K block is there and after the last.
 // ---------------------------------------------------------------------------------------------
 constexpr int FEW_THREADS = 384, FEW_ROWS = 128, FEW_BOX = 32;   // FEW_BOX: rows to a copy where there are few
